@@ -315,6 +315,81 @@ int32_t akvs_op_residual_stats(int32_t dtype, int32_t kv_format, const void* cac
 int32_t akvs_op_quantize(int32_t dtype, const void* x, int32_t n, int32_t n_kv_heads, int32_t head_dim,
                          int32_t bits, void* codes, void* meta, void* stream);
 
+/* ------------------------------------------------------------------------------------
+ * Answering from a context cache: what follows a prefill, layer by layer.  The context K/V of
+ * one layer are the slice out_k[l], out_v[l] of akvs_prefill_corrected (K after RoPE), so the
+ * arrays below need no copy of them.
+ *
+ * Common to the four: `*_ld` are strides in ELEMENTS of the type dtype names, between rows
+ * (tokens); the heads of a row lie back to back.  Tensors that dtype names, and the bytes of
+ * their strides, are 16-byte aligned (AKVS_ERR_INVALID_ARG).  Outputs overlap no input and no
+ * other output, unless stated (AKVS_ERR_INVALID_ARG).  dtype outside the three types:
+ * AKVS_ERR_UNSUPPORTED; a stride shorter than its row, n_q_heads no multiple of n_kv_heads or
+ * more than 128 query heads per kv head: AKVS_ERR_SHAPE.  All are asynchronous, read nothing
+ * on the host, and may be captured into a CUDA graph after one eager call.  Arrays of lengths,
+ * offsets and key ranges are device memory and are read when the kernels run.
+ * ------------------------------------------------------------------------------------ */
+
+/* RMSNorm of every query and key head with its own gain, then RoPE, in one pass:
+ *   y = x * rsqrt(mean(x^2) + eps) * gain   over the head_dim values of a head,
+ * then the rotate-half rotation of akvs_op_rope at pos[row] (any 32-bit position).  q [n][n_q]
+ * [hd] and k [n][n_kv][hd] may be column ranges of one projection's output (q_ld, k_ld); gains
+ * are float [head_dim]; all arithmetic is float, with one rounding at the end.  q_out / k_out
+ * may be q / k with the same stride.  One of the head counts may be 0.
+ * head_dim 32, 64, 128 or 256 (else AKVS_ERR_UNSUPPORTED); eps >= 0, rope_base > 0, finite. */
+int32_t akvs_op_qk_norm_rope(int32_t dtype, const void* q, int64_t q_ld, const void* k, int64_t k_ld,
+                             const float* q_gain, const float* k_gain, const int32_t* pos, int32_t n,
+                             int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float eps, float rope_base,
+                             void* q_out, int64_t q_out_ld, void* k_out, int64_t k_out_ld, void* stream);
+
+/* Attention of S sequences over one context that they share and over their own tokens.
+ *   q [R][n_q][hd]; context K/V [P][n_kv][hd]; own K/V [S][cap][n_kv][hd] (tokens own_ld, slots
+ *   own_seq_ld apart), of which sequence s holds the first own_len[s].
+ *   q_off NULL: row s is the one new token of sequence s (R >= S).  Otherwise rows q_off[s] ..
+ *   q_off[s+1] - 1 are the new tokens of sequence s, its last ones: device [S+1], non-decreasing.
+ * Row i of the n rows of a sequence sees the whole context and the first own_len[s] - (n - 1 - i)
+ * of its sequence's tokens (its own K/V are expected in the slot already).  What a row does not
+ * see never reaches it, NaN and infinities included.  Scores are scaled by 1/sqrt(head_dim).
+ *   out [R][n_q][hd], contiguous; lse float [R][n_q]: log of the row's sum of exponentials.
+ * A row that sees nothing gives zeros and lse = -inf; rows of no sequence are left as they were.
+ * Values of own_len outside [0, cap] and of q_off outside [0, R] are clamped, a range that runs
+ * backwards is empty; ranges must not overlap.  P = 0 or cap = 0 (then own_k, own_v and own_len
+ * may be NULL) are allowed.  head_dim 64 or 128.
+ * scratch: device, 256-byte aligned, akvs_op_attention_shared_scratch_bytes(...) bytes (else
+ * AKVS_ERR_WORKSPACE; may be NULL when P = 0); two calls that may overlap on the GPU need two. */
+int64_t akvs_op_attention_shared_scratch_bytes(int32_t R, int32_t P, int32_t n_q_heads, int32_t n_kv_heads,
+                                               int32_t head_dim);
+int32_t akvs_op_attention_shared(int32_t dtype, const void* q, int64_t q_ld, int32_t R, const void* ctx_k,
+                                 const void* ctx_v, int64_t ctx_ld, int32_t P, const void* own_k, const void* own_v,
+                                 int64_t own_ld, int64_t own_seq_ld, int32_t S, int32_t cap, const int32_t* own_len,
+                                 const int32_t* q_off, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                 void* out, float* lse, void* scratch, int64_t scratch_bytes, void* stream);
+
+/* Attention weight received by every key: mass_out[h][j] = mass_in[h][j] + the sum, over rows r
+ * with k_lo[r] <= j <= k_hi[r] and the query heads i that read kv head h, of
+ * exp(q_ri . k_jh / sqrt(head_dim) - lse[r][i]).  q [R][n_q][hd], k [T][n_kv][hd]; lse float
+ * [R][n_q] as akvs_op_attention_shared gives it (a row with lse = -inf adds nothing); k_lo,
+ * k_hi: device [R], in any order.  mass_in, mass_out: float [n_kv][T]; mass_in may be NULL
+ * (zeros) or mass_out itself.  Sums run in a fixed order: equal calls give equal bits.
+ * head_dim 64 or 128. */
+int32_t akvs_op_attention_mass(int32_t dtype, const void* q, int64_t q_ld, const void* k, int64_t k_ld,
+                               const float* lse, const int32_t* k_lo, const int32_t* k_hi, int32_t R, int32_t T,
+                               int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const float* mass_in,
+                               float* mass_out, void* stream);
+
+/* Shrinks a cache of T tokens to `budget` tokens per layer and kv head: the first n_sink and the
+ * last n_recent tokens stay, then the heaviest of the others (ties to the smaller index; a NaN
+ * mass is the lightest of all).  mass float [n_layers][n_kv][T]; k, v [n_layers][T][n_kv][hd]
+ * (tokens tok_ld, layers layer_ld elements apart).  Outputs, contiguous, in ascending token
+ * order: idx int32 [n_layers][n_kv][budget] (the token each slot came from), k_out, v_out
+ * [n_layers][budget][n_kv][hd], mass_out [n_layers][n_kv][budget].  K keeps the rotation of its
+ * old position, so the result is a context for akvs_op_attention_shared as it stands.
+ * budget > T or n_sink + n_recent > budget: AKVS_ERR_SHAPE; n_layers * n_kv > 65535:
+ * AKVS_ERR_TOO_LARGE.  head_dim 64 or 128. */
+int32_t akvs_op_evict(int32_t dtype, const float* mass, const void* k, const void* v, int64_t layer_ld, int64_t tok_ld,
+                      int32_t n_layers, int32_t T, int32_t n_kv_heads, int32_t head_dim, int32_t budget, int32_t n_sink,
+                      int32_t n_recent, int32_t* idx, void* k_out, void* v_out, float* mass_out, void* stream);
+
 /* ====================================================================================
  * NOT PART OF THE SERVING SURFACE.  Test and measurement hooks: process-wide state, not
  * thread-safe, no paper passage behind any of them.  A serving caller needs none of these.

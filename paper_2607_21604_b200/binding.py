@@ -26,7 +26,9 @@ EXPORTS = ["akvs_workspace_bytes", "akvs_debug_set_linear_algo", "akvs_launch_co
            "akvs_prof_reset", "akvs_prof_read", "akvs_encode_units", "akvs_select_probes", "akvs_prefill_corrected",
            "akvs_free", "akvs_check", "akvs_op_linear", "akvs_op_linear_residual", "akvs_op_rope", "akvs_op_attention",
            "akvs_op_scratch_bytes", "akvs_op_select", "akvs_op_select_static", "akvs_op_correct_layer",
-           "akvs_op_quantize", "akvs_op_residual_stats", "akvs_debug_correct_repeat", "akvs_debug_wait_timeout"]
+           "akvs_op_quantize", "akvs_op_residual_stats", "akvs_op_qk_norm_rope", "akvs_op_attention_shared",
+           "akvs_op_attention_shared_scratch_bytes", "akvs_op_attention_mass", "akvs_op_evict",
+           "akvs_debug_correct_repeat", "akvs_debug_wait_timeout"]
 STATIC_MAX_CTX, STATIC_MAX_UNITS = 16384, 1024
 
 
@@ -74,6 +76,13 @@ def _load():
     lib.akvs_op_scratch_bytes.restype = C.c_int64
     lib.akvs_launch_count.restype = C.c_int64
     lib.akvs_free.restype = None
+    P, I, L, F = C.c_void_p, C.c_int32, C.c_int64, C.c_float
+    lib.akvs_op_qk_norm_rope.argtypes = [I, P, L, P, L, P, P, P, I, I, I, I, F, F, P, L, P, L, P]
+    lib.akvs_op_attention_shared_scratch_bytes.restype = L
+    lib.akvs_op_attention_shared_scratch_bytes.argtypes = [I] * 5
+    lib.akvs_op_attention_shared.argtypes = [I, P, L, I, P, P, L, I, P, P, L, L, I, I, P, P, I, I, I, P, P, P, L, P]
+    lib.akvs_op_attention_mass.argtypes = [I, P, L, P, L, P, P, P, I, I, I, I, I, P, P, P]
+    lib.akvs_op_evict.argtypes = [I, P, P, P, L, L, I, I, I, I, I, I, I, P, P, P, P, P]
     return lib
 
 
@@ -462,3 +471,169 @@ def op_quantize(x, bits):
     _chk(lib.akvs_op_quantize(dtype, _ptr(x), n, nkv, hd, bits, _ptr(codes), _ptr(meta), _stream()),
          "akvs_op_quantize")
     return codes, meta
+
+
+# ------------------------------------------------------------------ answering from a context cache
+
+_CODE = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+def _refuse(where, code=-1):
+    raise AkvsError(code, where)
+
+
+def _on_device(where, *tensors):
+    """All tensors on the current CUDA device: the stream the call runs on is that device's."""
+    dev = None
+    for t in tensors:
+        if not t.is_cuda:
+            _refuse(where)
+        if dev is None:
+            dev = torch.cuda.current_device()
+        if t.get_device() != dev:
+            _refuse(where)
+
+
+def _heads_packed(where, *tensors):
+    """The last two dimensions (head, value) of each lie back to back."""
+    for t in tensors:
+        hd = t.shape[-1]
+        if (t.shape[-1] > 1 and t.stride(-1) != 1) or (t.shape[-2] > 1 and t.stride(-2) != hd):
+            _refuse(where, -2)
+
+
+def _ld(t, dim=0):
+    """Stride between rows; a dimension of one row has none of its own."""
+    return t.stride(dim) if t.shape[dim] > 1 else t.shape[-1] * t.shape[-2]
+
+
+def _dense(where, dtype, *tensors):
+    for t in tensors:
+        if t.dtype != dtype:
+            _refuse(where, -4)
+        if not t.is_contiguous():
+            _refuse(where, -2)
+
+
+def op_qk_norm_rope(q, k, q_gain, k_gain, pos, eps, base, q_out=None, k_out=None):
+    """RMSNorm of every head of q [n][n_q][hd] and k [n][n_kv][hd] (gains float [hd]), then RoPE at
+    pos [n]; rows may be strided (column ranges of one projection).  q_out / k_out may be q / k."""
+    w = "akvs_op_qk_norm_rope"
+    _on_device(w, q, k, q_gain, k_gain, pos)
+    n, nq, hd = q.shape
+    if k.dtype != q.dtype or q.dtype not in _CODE:
+        _refuse(w, -4)
+    if k.shape[0] != n or k.shape[2] != hd or pos.shape != (n,) or q_gain.shape != (hd,) or k_gain.shape != (hd,):
+        _refuse(w, -2)
+    _dense(w, torch.float32, q_gain, k_gain)
+    _dense(w, torch.int32, pos)
+    q_out = torch.empty((n, nq, hd), dtype=q.dtype, device=q.device) if q_out is None else q_out
+    k_out = torch.empty(k.shape, dtype=q.dtype, device=q.device) if k_out is None else k_out
+    if q_out.shape != q.shape or k_out.shape != k.shape:
+        _refuse(w, -2)
+    if q_out.dtype != q.dtype or k_out.dtype != q.dtype:
+        _refuse(w, -4)
+    _on_device(w, q_out, k_out)
+    _heads_packed(w, q, k, q_out, k_out)
+    _chk(lib.akvs_op_qk_norm_rope(_CODE[q.dtype], q.data_ptr(), _ld(q), k.data_ptr(), _ld(k), q_gain.data_ptr(),
+                                  k_gain.data_ptr(), pos.data_ptr(), n, nq, k.shape[1], hd, eps, base,
+                                  q_out.data_ptr(), _ld(q_out), k_out.data_ptr(), _ld(k_out), _stream()), w)
+    return q_out, k_out
+
+
+def op_attention_shared_scratch(R, P, n_q, n_kv, hd, device="cuda"):
+    return alloc_workspace(lib.akvs_op_attention_shared_scratch_bytes(R, P, n_q, n_kv, hd), device)
+
+
+def op_attention_shared(q, ctx_k, ctx_v, own_k, own_v, own_len, q_off=None, out=None, lse=None, scratch=None):
+    """Attention of q [R][n_q][hd] over the shared context [P][n_kv][hd] and each sequence's own
+    tokens [S][cap][n_kv][hd], of which own_len [S] are filled.  q_off [S+1] gives the rows of each
+    sequence (None: one row each).  Returns (out, lse); rows of no sequence keep what `out` and
+    `lse` held (zeros where this call allocates them)."""
+    w = "akvs_op_attention_shared"
+    _on_device(w, q, ctx_k, ctx_v, own_k, own_v, own_len)
+    (R, nq, hd), (P, nkv, _), (S, cap, _, _) = q.shape, ctx_k.shape, own_k.shape
+    dt = q.dtype
+    if dt not in _CODE or ctx_k.dtype != dt or ctx_v.dtype != dt or own_k.dtype != dt or own_v.dtype != dt:
+        _refuse(w, -4)
+    if (ctx_k.shape[2] != hd or ctx_v.shape != ctx_k.shape or own_k.shape[2:] != (nkv, hd) or own_v.shape != own_k.shape
+            or own_len.shape != (S,) or ctx_k.stride() != ctx_v.stride() or own_k.stride() != own_v.stride()):
+        _refuse(w, -2)
+    _dense(w, torch.int32, own_len)
+    if q_off is not None:
+        _on_device(w, q_off)
+        _dense(w, torch.int32, q_off)
+        if q_off.shape != (S + 1,):
+            _refuse(w, -2)
+    fresh = torch.empty if q_off is None and R == S else torch.zeros
+    out = fresh((R, nq, hd), dtype=dt, device=q.device) if out is None else out
+    lse = fresh((R, nq), dtype=torch.float32, device=q.device) if lse is None else lse
+    _on_device(w, out, lse)
+    if out.shape != q.shape or lse.shape != (R, nq):
+        _refuse(w, -2)
+    _dense(w, dt, out)
+    _dense(w, torch.float32, lse)
+    _heads_packed(w, q, ctx_k, own_k)
+    if scratch is None:
+        need = lib.akvs_op_attention_shared_scratch_bytes(R, P, nq, nkv, hd)
+        scratch = torch.empty(max(need, 0), dtype=torch.uint8, device=q.device)
+    else:
+        _on_device(w, scratch)
+    _chk(lib.akvs_op_attention_shared(_CODE[dt], q.data_ptr(), _ld(q), R, ctx_k.data_ptr(), ctx_v.data_ptr(), _ld(ctx_k),
+                                      P, own_k.data_ptr(), own_v.data_ptr(), _ld(own_k, 1), own_k.stride(0), S, cap,
+                                      own_len.data_ptr(), q_off.data_ptr() if q_off is not None else None, nq, nkv, hd,
+                                      out.data_ptr(), lse.data_ptr(), scratch.data_ptr(), scratch.numel(), _stream()), w)
+    return out, lse
+
+
+def op_attention_mass(q, k, lse, k_lo, k_hi, mass=None, out=None):
+    """mass [n_kv][T] (None: zeros) plus the attention weight that the rows q [R][n_q][hd] with
+    log-sum-exp lse [R][n_q] put on the keys k [T][n_kv][hd] in k_lo[r] .. k_hi[r].  `out` may be
+    `mass`."""
+    w = "akvs_op_attention_mass"
+    _on_device(w, q, k, lse, k_lo, k_hi)
+    (R, nq, hd), (T, nkv, _) = q.shape, k.shape
+    if q.dtype not in _CODE or k.dtype != q.dtype:
+        _refuse(w, -4)
+    if k.shape[2] != hd or lse.shape != (R, nq) or k_lo.shape != (R,) or k_hi.shape != (R,):
+        _refuse(w, -2)
+    out = torch.empty((nkv, T), dtype=torch.float32, device=q.device) if out is None else out
+    for t in (mass, out):
+        if t is not None:
+            _on_device(w, t)
+            _dense(w, torch.float32, t)
+            if t.shape != (nkv, T):
+                _refuse(w, -2)
+    _dense(w, torch.float32, lse)
+    _dense(w, torch.int32, k_lo, k_hi)
+    _heads_packed(w, q, k)
+    _chk(lib.akvs_op_attention_mass(_CODE[q.dtype], q.data_ptr(), _ld(q), k.data_ptr(), _ld(k), lse.data_ptr(),
+                                    k_lo.data_ptr(), k_hi.data_ptr(), R, T, nq, nkv, hd,
+                                    mass.data_ptr() if mass is not None else None, out.data_ptr(), _stream()), w)
+    return out
+
+
+def op_evict(mass, k, v, budget, n_sink=0, n_recent=0):
+    """Keeps `budget` tokens per layer and kv head of k, v [L][T][n_kv][hd] by mass [L][n_kv][T]: the
+    first n_sink, the last n_recent and the heaviest others.  Returns (idx [L][n_kv][budget],
+    k_out, v_out [L][budget][n_kv][hd], mass_out [L][n_kv][budget]), tokens ascending."""
+    w = "akvs_op_evict"
+    _on_device(w, mass, k, v)
+    (L, nkv, T), hd = mass.shape, k.shape[-1]
+    if k.dtype not in _CODE or v.dtype != k.dtype:
+        _refuse(w, -4)
+    if k.shape != (L, T, nkv, hd) or v.shape != k.shape or v.stride() != k.stride():
+        _refuse(w, -2)
+    if not 0 <= budget <= T or n_sink < 0 or n_recent < 0:
+        _refuse(w, -2 if budget > T else -1)
+    _dense(w, torch.float32, mass)
+    _heads_packed(w, k)
+    idx = torch.empty((L, nkv, budget), dtype=torch.int32, device=k.device)
+    k_out = torch.empty((L, budget, nkv, hd), dtype=k.dtype, device=k.device)
+    v_out, m_out = torch.empty_like(k_out), torch.empty((L, nkv, budget), dtype=torch.float32, device=k.device)
+    tok_ld = _ld(k, 1)
+    layer_ld = k.stride(0) if L > 1 else T * tok_ld
+    _chk(lib.akvs_op_evict(_CODE[k.dtype], mass.data_ptr(), k.data_ptr(), v.data_ptr(), layer_ld, tok_ld, L, T, nkv, hd,
+                           budget, n_sink, n_recent, idx.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
+                           m_out.data_ptr(), _stream()), w)
+    return idx, k_out, v_out, m_out

@@ -71,6 +71,22 @@ static inline size_t dtype_size(int dtype) { return dtype == AKVS_F32 ? 4 : 2; }
 static inline int64_t akvs_align_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 static inline int akvs_cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
+// Argument checks of the entry points: 16-byte alignment, and whether two ranges of bytes meet.
+static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+static inline bool bytes_overlap(const void* a, int64_t na, const void* b, int64_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return na > 0 && nb > 0 && x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
+}
+// n rows of `w` bytes, `ld` bytes apart, against n rows of another tensor.  Column ranges of one
+// tensor (equal strides) may interleave without meeting.
+static inline bool rows_overlap(const void* a, int64_t lda, int64_t wa, const void* b, int64_t ldb, int64_t wb, int64_t n) {
+  if (n <= 0 || !bytes_overlap(a, (n - 1) * lda + wa, b, (n - 1) * ldb + wb)) return false;
+  if (lda != ldb) return true;
+  int64_t d = (int64_t)(reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(a)) % lda;
+  if (d < 0) d += lda;                            // b's column offset inside a's rows
+  return d < wa || d + wb > lda;
+}
+
 // ---------------------------------------------------------------------------------------
 // 16-byte vector access: VEC elements of T <-> float registers.
 // ---------------------------------------------------------------------------------------

@@ -1,0 +1,261 @@
+// Eviction from a cache by accumulated attention weight.  Per layer and kv head the first
+// `n_sink` and the last `n_recent` tokens stay, and of the others the heaviest until `budget`
+// tokens are kept (ties to the smaller index); the kept tokens' K, V and mass are packed in
+// ascending token order.
+//
+// select_kernel finds the threshold: a cluster of C CTAs owns one (layer, head) row of masses,
+// keeps it in shared memory as order-preserving 32-bit keys, and fixes the key of the last kept
+// token in four passes of 8 bits; the 256-bin histograms of the CTAs are added up through
+// distributed shared memory.  Counts of greater and equal keys per warp then give every kept
+// token its place without a sort.  Selection is latency bound (a row is read once from memory),
+// so a call with few rows spreads each over up to 8 SMs.
+// gather_kernel moves the kept K/V, 16 bytes per thread and step: memory bound, and nearly all
+// of the operator's bytes.
+#include "tc_common.cuh"
+
+namespace {
+
+constexpr int SEL_THREADS = 512, SEL_WARPS = SEL_THREADS / 32;
+constexpr int SEL_MAX_C = 8;                       // portable cluster size
+constexpr int SEL_MAX_SEG = 50 * 1024;             // keys of a CTA's shared memory (200 KB)
+
+// Order of the masses as unsigned integers: greater mass, greater key; -0 equals +0, NaN is the
+// smallest of all, so that a broken mass is the first to go.
+__device__ __forceinline__ uint32_t mass_key(float m) {
+  if (m != m) return 0u;
+  const uint32_t u = __float_as_uint(m + 0.f);     // -0 + 0 = +0
+  return (u >> 31) ? ~u : (u | 0x80000000u);
+}
+__device__ __forceinline__ uint32_t ld_cluster(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+template <bool CACHED>
+__global__ void __launch_bounds__(SEL_THREADS)
+select_kernel(const float* __restrict__ mass, int T, int n_sink, int n_recent, int budget, int seg,
+              int32_t* __restrict__ idx, float* __restrict__ mass_out) {
+  extern __shared__ uint32_t keys[];               // [seg] when CACHED
+  __shared__ uint32_t hist[2][256];
+  __shared__ uint32_t warp_part[SEL_WARPS];
+  __shared__ uint32_t found[2];                    // bin, keys still wanted from it
+  __shared__ uint32_t cnt[2];                      // this CTA's kept-for-sure and tied tokens
+  __shared__ uint32_t w_sure[SEL_WARPS], w_tied[SEL_WARPS];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int C = gridDim.x;
+  const uint32_t rank = tc::cluster_ctarank();
+  const int row = blockIdx.y;
+  const int t0 = min((int64_t)rank * seg, (int64_t)T), t1 = min((int64_t)t0 + seg, (int64_t)T);
+  const int n = t1 - t0;
+  pdl_trigger();
+  pdl_wait();
+  const float* m = mass + (int64_t)row * T + t0;
+  if (CACHED) {
+    for (int i = tid; i < n; i += SEL_THREADS) keys[i] = mass_key(m[i]);
+  }
+  auto key = [&](int i) { return CACHED ? keys[i] : mass_key(__ldg(m + i)); };
+  auto forced = [&](int i) { const int t = t0 + i; return t < n_sink || t >= T - n_recent; };
+  const int from = max(n_sink - t0, 0), to = min(T - n_recent - t0, n);    // candidates of this CTA
+
+  uint32_t want = (uint32_t)(budget - n_sink - n_recent);
+  uint32_t prefix = 0, mask = 0;
+  for (int i = tid; i < 512; i += SEL_THREADS) (&hist[0][0])[i] = 0;
+  __syncthreads();
+  if (want > 0) {                                  // the same in all CTAs of the cluster
+    for (int pass = 0; pass < 4; ++pass) {
+      const int shift = 24 - 8 * pass;
+      uint32_t* hb = hist[pass & 1];
+      // lanes of equal bins add together: masses share exponents, and untouched keys are all zero
+      for (int i = from + tid - lane; i < to; i += SEL_THREADS) {
+        const int j = i + lane;
+        const uint32_t kx = j < to ? key(j) : 0u;
+        const bool in = j < to && (kx & mask) == prefix;
+        const uint32_t bin = in ? ((kx >> shift) & 255u) : 256u;
+        const uint32_t peers = __match_any_sync(0xFFFFFFFFu, bin);
+        if (in && (peers & ((1u << lane) - 1u)) == 0) atomicAdd(&hb[bin], (uint32_t)__popc(peers));
+      }
+      tc::cluster_sync_all();
+      // total of each bin, greatest bin first: thread i holds bin 255 - i
+      uint32_t total = 0;
+      if (tid < 256) {
+        const uint32_t a = tc::smem_u32(&hb[255 - tid]);
+        for (int c = 0; c < C; ++c) total += ld_cluster(tc::map_to_rank(a, c));
+      }
+      uint32_t incl = total;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        if (lane >= o) incl += up;
+      }
+      if (lane == 31) warp_part[warp] = incl;
+      if (pass < 3 && tid >= 256) hist[(pass + 1) & 1][tid - 256] = 0;   // last read before the sync above
+      __syncthreads();
+      if (tid < 256) {
+        for (int w = 0; w < warp; ++w) incl += warp_part[w];
+        if (incl >= want && incl - total < want) {
+          found[0] = 255 - tid;
+          found[1] = want - (incl - total);
+        }
+      }
+      __syncthreads();
+      prefix |= found[0] << shift;
+      mask |= 255u << shift;
+      want = found[1];
+    }
+  }
+  const uint32_t cut = budget > n_sink + n_recent ? prefix : 0xFFFFFFFFu;   // no key is all ones
+  const uint32_t ties = budget > n_sink + n_recent ? want : 0u;
+
+  // every warp owns a run of consecutive tokens: count, exchange, then place
+  const int per = (seg + SEL_THREADS - 1) / SEL_THREADS * 32;
+  const int a = min(warp * per, n), b = min(a + per, n);
+  uint32_t sure = 0, tied = 0;
+  for (int i = a; i < b; i += 32) {
+    const int j = i + lane;
+    const bool f = j < b && forced(j);
+    const uint32_t kx = j < b ? key(j) : 0u;
+    sure += __popc(__ballot_sync(0xFFFFFFFFu, f || (j < b && kx > cut)));
+    tied += __popc(__ballot_sync(0xFFFFFFFFu, j < b && !f && kx == cut));
+  }
+  if (lane == 0) { w_sure[warp] = sure; w_tied[warp] = tied; }
+  __syncthreads();
+  if (tid == 0) {
+    uint32_t s = 0, t = 0;
+    for (int w = 0; w < SEL_WARPS; ++w) { s += w_sure[w]; t += w_tied[w]; }
+    cnt[0] = s;
+    cnt[1] = t;
+  }
+  tc::cluster_sync_all();
+  uint32_t before_s = 0, before_t = 0;
+  for (uint32_t c = 0; c < rank; ++c) {
+    before_s += ld_cluster(tc::map_to_rank(tc::smem_u32(&cnt[0]), c));
+    before_t += ld_cluster(tc::map_to_rank(tc::smem_u32(&cnt[1]), c));
+  }
+  for (int w = 0; w < warp; ++w) { before_s += w_sure[w]; before_t += w_tied[w]; }
+  int32_t* out = idx + (int64_t)row * budget;
+  float* mo = mass_out + (int64_t)row * budget;
+  for (int i = a; i < b; i += 32) {
+    const int j = i + lane;
+    const bool f = j < b && forced(j);
+    const uint32_t kx = j < b ? key(j) : 0u;
+    const bool is_sure = f || (j < b && kx > cut), is_tied = j < b && !f && kx == cut;
+    const uint32_t bs = __ballot_sync(0xFFFFFFFFu, is_sure), bt = __ballot_sync(0xFFFFFFFFu, is_tied);
+    const uint32_t below = (1u << lane) - 1u;
+    const uint32_t my_s = before_s + __popc(bs & below), my_t = before_t + __popc(bt & below);
+    if (is_sure || (is_tied && my_t < ties)) {
+      const uint32_t at = my_s + min(my_t, ties);
+      out[at] = t0 + j;
+      mo[at] = m[j];
+    }
+    before_s += __popc(bs);
+    before_t += __popc(bt);
+  }
+  tc::cluster_sync_all();                          // nobody leaves while its counts may be read
+}
+
+constexpr int GATHER_THREADS = 256, GATHER_UN = 4;
+
+// One thread moves GATHER_UN 16-byte chunks of K and the same chunks of V.
+__global__ void __launch_bounds__(GATHER_THREADS)
+gather_kernel(const uint4* __restrict__ k, const uint4* __restrict__ v, const int32_t* __restrict__ idx, int budget,
+              int n_kv, int log_cph, int64_t layer_ld, int64_t tok_ld, uint4* __restrict__ k_out,
+              uint4* __restrict__ v_out) {
+  pdl_trigger();
+  pdl_wait();
+  const int l = blockIdx.y;
+  const int64_t total = ((int64_t)budget * n_kv) << log_cph;
+  const int64_t base = (int64_t)blockIdx.x * (GATHER_THREADS * GATHER_UN) + threadIdx.x;
+  const int32_t* ix = idx + (int64_t)l * n_kv * budget;
+  uint4 a[GATHER_UN], b[GATHER_UN];
+#pragma unroll
+  for (int u = 0; u < GATHER_UN; ++u) {
+    const int64_t i = base + u * GATHER_THREADS;
+    if (i < total) {
+      const int64_t s = i >> log_cph;
+      const int c = (int)(i & ((1 << log_cph) - 1));
+      const int64_t o = s / n_kv;
+      const int h = (int)(s - o * n_kv);
+      const int64_t at = l * layer_ld + (int64_t)__ldg(ix + (int64_t)h * budget + o) * tok_ld + ((int64_t)h << log_cph) + c;
+      a[u] = __ldcs(k + at);
+      b[u] = __ldcs(v + at);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < GATHER_UN; ++u) {
+    const int64_t i = base + u * GATHER_THREADS;
+    if (i < total) {
+      __stcs(k_out + l * total + i, a[u]);
+      __stcs(v_out + l * total + i, b[u]);
+    }
+  }
+}
+
+}  // namespace
+
+extern "C" int32_t akvs_op_evict(int32_t dtype, const float* mass, const void* k, const void* v, int64_t layer_ld,
+                                 int64_t tok_ld, int32_t n_layers, int32_t T, int32_t n_kv_heads, int32_t head_dim,
+                                 int32_t budget, int32_t n_sink, int32_t n_recent, int32_t* idx, void* k_out,
+                                 void* v_out, float* mass_out, void* stream) {
+  if (dtype != AKVS_F32 && dtype != AKVS_BF16 && dtype != AKVS_F16) return AKVS_ERR_UNSUPPORTED;
+  if (n_layers < 0 || T < 0 || n_kv_heads <= 0 || budget < 0 || n_sink < 0 || n_recent < 0) return AKVS_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return AKVS_ERR_UNSUPPORTED;
+  if (budget > T || (int64_t)n_sink + n_recent > budget) return AKVS_ERR_SHAPE;
+  if (n_layers == 0 || budget == 0) return AKVS_OK;
+  if (!mass || !k || !v || !idx || !k_out || !v_out || !mass_out) return AKVS_ERR_INVALID_ARG;
+  const int64_t es = (int64_t)dtype_size(dtype), row = (int64_t)n_kv_heads * head_dim;
+  if (tok_ld < row || layer_ld < 0 || (n_layers > 1 && layer_ld < (T - 1) * tok_ld + row)) return AKVS_ERR_SHAPE;
+  if (!aligned16(k) || !aligned16(v) || !aligned16(k_out) || !aligned16(v_out) || tok_ld * es % 16 || layer_ld * es % 16)
+    return AKVS_ERR_INVALID_ARG;
+  const int64_t rows = (int64_t)n_layers * n_kv_heads;
+  if (rows > 65535 || n_layers > 65535) return AKVS_ERR_TOO_LARGE;
+  const int64_t in_bytes = ((n_layers - 1) * layer_ld + (int64_t)(T - 1) * tok_ld + row) * es;
+  const void* ins[3] = {mass, k, v};
+  const int64_t in_n[3] = {rows * T * 4, in_bytes, in_bytes};
+  const void* outs[4] = {idx, k_out, v_out, mass_out};
+  const int64_t out_n[4] = {rows * budget * 4, n_layers * budget * row * es, n_layers * budget * row * es, rows * budget * 4};
+  for (int o = 0; o < 4; ++o) {
+    for (int i = 0; i < 3; ++i)
+      if (bytes_overlap(ins[i], in_n[i], outs[o], out_n[o])) return AKVS_ERR_INVALID_ARG;
+    for (int i = 0; i < o; ++i)
+      if (bytes_overlap(outs[i], out_n[i], outs[o], out_n[o])) return AKVS_ERR_INVALID_ARG;
+  }
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  static bool attr_set = false;
+  if (!attr_set) {
+    AKVS_CUDA(cudaFuncSetAttribute(select_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SEL_MAX_SEG * 4));
+    attr_set = true;
+  }
+  // Rows are spread over clusters while SMs would idle and a CTA's share is still worth a pass
+  // (2048 keys), and as far as the keys need the room; beyond that they are re-read from memory.
+  int C = 1;
+  while (C < SEL_MAX_C && ((rows * C * 2 <= 148 && T / C > 2048) || akvs_cdiv(T, C) > SEL_MAX_SEG)) C *= 2;
+  const int seg = akvs_cdiv(T, C);
+  const bool cached = seg <= SEL_MAX_SEG;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(C, (unsigned)rows);
+  cfg.blockDim = dim3(SEL_THREADS);
+  cfg.dynamicSmemBytes = cached ? (size_t)seg * 4 : 0;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = C;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  AKVS_CUDA(cudaLaunchKernelEx(&cfg, cached ? select_kernel<true> : select_kernel<false>, mass, (int)T, (int)n_sink,
+                               (int)n_recent, (int)budget, seg, idx, mass_out));
+  AKVS_LAUNCHED();
+  const int64_t cph = head_dim * es / 16;              // 8, 16 or 32 chunks of a head
+  const int log_cph = cph == 8 ? 3 : cph == 16 ? 4 : 5;
+  const int64_t blocks = (((int64_t)budget * n_kv_heads << log_cph) + GATHER_THREADS * GATHER_UN - 1) / (GATHER_THREADS * GATHER_UN);
+  if (blocks > 0x7fffffff) return AKVS_ERR_TOO_LARGE;
+  AKVS_CUDA(launch_pdl(gather_kernel, dim3((unsigned)blocks, (unsigned)n_layers), dim3(GATHER_THREADS), 0, st,
+                       (const uint4*)k, (const uint4*)v, (const int32_t*)idx, (int)budget, (int)n_kv_heads, log_cph,
+                       layer_ld * es / 16, tok_ld * es / 16, (uint4*)k_out, (uint4*)v_out));
+  AKVS_LAUNCHED();
+  return AKVS_OK;
+}
