@@ -474,75 +474,65 @@ def op_quantize(x, bits):
 
 
 # ------------------------------------------------------------------ answering from a context cache
+#
+# A decoding step is a handful of these calls, each of a few microseconds on the device, so the
+# checks below read every tensor's shape, strides and device once and build no objects.
 
 _CODE = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+_device = torch._C._cuda_getDevice                     # the current device, without the lookup of its properties
+_raw_stream = torch._C._cuda_getCurrentRawStream       # the current stream's handle, without a Stream object
 
 
 def _refuse(where, code=-1):
     raise AkvsError(code, where)
 
 
-def _on_device(where, *tensors):
-    """All tensors on the current CUDA device: the stream the call runs on is that device's."""
-    dev = None
-    for t in tensors:
-        if not t.is_cuda:
-            _refuse(where)
-        if dev is None:
-            dev = torch.cuda.current_device()
-        if t.get_device() != dev:
-            _refuse(where)
+def _current(where, dev):
+    """The call runs on the current stream of the current device: tensors of another one are refused."""
+    if dev < 0 or dev != _device():
+        _refuse(where)
+    return dev
 
 
-def _heads_packed(where, *tensors):
-    """The last two dimensions (head, value) of each lie back to back."""
-    for t in tensors:
-        hd = t.shape[-1]
-        if (t.shape[-1] > 1 and t.stride(-1) != 1) or (t.shape[-2] > 1 and t.stride(-2) != hd):
-            _refuse(where, -2)
-
-
-def _ld(t, dim=0):
-    """Stride between rows; a dimension of one row has none of its own."""
-    return t.stride(dim) if t.shape[dim] > 1 else t.shape[-1] * t.shape[-2]
-
-
-def _dense(where, dtype, *tensors):
-    for t in tensors:
-        if t.dtype != dtype:
-            _refuse(where, -4)
-        if not t.is_contiguous():
-            _refuse(where, -2)
+def _ld(where, shape, stride):
+    """Elements between rows of [rows][heads][hd], whose heads must lie back to back; a single row
+    has no stride of its own."""
+    n, heads, hd = shape
+    if stride[2] != 1 or (heads > 1 and stride[1] != hd):
+        _refuse(where, -2)
+    return stride[0] if n > 1 else heads * hd
 
 
 def op_qk_norm_rope(q, k, q_gain, k_gain, pos, eps, base, q_out=None, k_out=None):
     """RMSNorm of every head of q [n][n_q][hd] and k [n][n_kv][hd] (gains float [hd]), then RoPE at
     pos [n]; rows may be strided (column ranges of one projection).  q_out / k_out may be q / k."""
     w = "akvs_op_qk_norm_rope"
-    _on_device(w, q, k, q_gain, k_gain, pos)
-    n, nq, hd = q.shape
-    if k.dtype != q.dtype or q.dtype not in _CODE:
+    dev, dt, qs, ks = _current(w, q.get_device()), q.dtype, q.shape, k.shape
+    q_out = q.new_empty(qs) if q_out is None else q_out
+    k_out = q.new_empty(ks) if k_out is None else k_out
+    if not (dev == k.get_device() == q_gain.get_device() == k_gain.get_device() == pos.get_device() == q_out.get_device()
+            == k_out.get_device()):
+        _refuse(w)
+    if not (dt in _CODE and dt == k.dtype == q_out.dtype == k_out.dtype and pos.dtype == torch.int32
+            and q_gain.dtype == k_gain.dtype == torch.float32):
         _refuse(w, -4)
-    if k.shape[0] != n or k.shape[2] != hd or pos.shape != (n,) or q_gain.shape != (hd,) or k_gain.shape != (hd,):
+    n, nq, hd = qs
+    if not (len(ks) == 3 and ks[0] == n and ks[2] == hd and q_out.shape == qs and k_out.shape == ks and pos.shape == (n,)
+            and q_gain.shape == k_gain.shape == (hd,) and q_gain.is_contiguous() and k_gain.is_contiguous()
+            and pos.is_contiguous()):
         _refuse(w, -2)
-    _dense(w, torch.float32, q_gain, k_gain)
-    _dense(w, torch.int32, pos)
-    q_out = torch.empty((n, nq, hd), dtype=q.dtype, device=q.device) if q_out is None else q_out
-    k_out = torch.empty(k.shape, dtype=q.dtype, device=q.device) if k_out is None else k_out
-    if q_out.shape != q.shape or k_out.shape != k.shape:
-        _refuse(w, -2)
-    if q_out.dtype != q.dtype or k_out.dtype != q.dtype:
-        _refuse(w, -4)
-    _on_device(w, q_out, k_out)
-    _heads_packed(w, q, k, q_out, k_out)
-    _chk(lib.akvs_op_qk_norm_rope(_CODE[q.dtype], q.data_ptr(), _ld(q), k.data_ptr(), _ld(k), q_gain.data_ptr(),
-                                  k_gain.data_ptr(), pos.data_ptr(), n, nq, k.shape[1], hd, eps, base,
-                                  q_out.data_ptr(), _ld(q_out), k_out.data_ptr(), _ld(k_out), _stream()), w)
+    _chk(lib.akvs_op_qk_norm_rope(_CODE[dt], q.data_ptr(), _ld(w, qs, q.stride()), k.data_ptr(), _ld(w, ks, k.stride()),
+                                  q_gain.data_ptr(), k_gain.data_ptr(), pos.data_ptr(), n, nq, ks[1], hd, eps, base,
+                                  q_out.data_ptr(), _ld(w, qs, q_out.stride()), k_out.data_ptr(),
+                                  _ld(w, ks, k_out.stride()), _raw_stream(dev)), w)
     return q_out, k_out
 
 
 def op_attention_shared_scratch(R, P, n_q, n_kv, hd, device="cuda"):
-    return alloc_workspace(lib.akvs_op_attention_shared_scratch_bytes(R, P, n_q, n_kv, hd), device)
+    nbytes = lib.akvs_op_attention_shared_scratch_bytes(R, P, n_q, n_kv, hd)
+    if nbytes < 0:
+        _refuse("akvs_op_attention_shared_scratch_bytes")
+    return alloc_workspace(nbytes, device)
 
 
 def op_attention_shared(q, ctx_k, ctx_v, own_k, own_v, own_len, q_off=None, out=None, lse=None, scratch=None):
@@ -551,38 +541,42 @@ def op_attention_shared(q, ctx_k, ctx_v, own_k, own_v, own_len, q_off=None, out=
     sequence (None: one row each).  Returns (out, lse); rows of no sequence keep what `out` and
     `lse` held (zeros where this call allocates them)."""
     w = "akvs_op_attention_shared"
-    _on_device(w, q, ctx_k, ctx_v, own_k, own_v, own_len)
-    (R, nq, hd), (P, nkv, _), (S, cap, _, _) = q.shape, ctx_k.shape, own_k.shape
-    dt = q.dtype
-    if dt not in _CODE or ctx_k.dtype != dt or ctx_v.dtype != dt or own_k.dtype != dt or own_v.dtype != dt:
+    dev, dt, qs, cs, os_ = _current(w, q.get_device()), q.dtype, q.shape, ctx_k.shape, own_k.shape
+    (R, nq, hd), (P, nkv, _), (S, cap, _, _) = qs, cs, os_
+    if out is None or lse is None:
+        fresh = torch.empty if q_off is None and R == S else torch.zeros
+        out = fresh(qs, dtype=dt, device=q.device) if out is None else out
+        lse = fresh((R, nq), dtype=torch.float32, device=q.device) if lse is None else lse
+    if not (dev == ctx_k.get_device() == ctx_v.get_device() == own_k.get_device() == own_v.get_device()
+            == own_len.get_device() == out.get_device() == lse.get_device()):
+        _refuse(w)
+    if not (dt in _CODE and dt == ctx_k.dtype == ctx_v.dtype == own_k.dtype == own_v.dtype == out.dtype
+            and lse.dtype == torch.float32 and own_len.dtype == torch.int32):
         _refuse(w, -4)
-    if (ctx_k.shape[2] != hd or ctx_v.shape != ctx_k.shape or own_k.shape[2:] != (nkv, hd) or own_v.shape != own_k.shape
-            or own_len.shape != (S,) or ctx_k.stride() != ctx_v.stride() or own_k.stride() != own_v.stride()):
+    cst, ost = ctx_k.stride(), own_k.stride()
+    if not (cs[2] == hd and ctx_v.shape == cs and os_[2:] == (nkv, hd) and own_v.shape == os_ and own_len.shape == (S,)
+            and ctx_v.stride() == cst and own_v.stride() == ost and out.shape == qs and lse.shape == (R, nq)
+            and out.is_contiguous() and lse.is_contiguous() and own_len.is_contiguous()):
         _refuse(w, -2)
-    _dense(w, torch.int32, own_len)
+    off = None
     if q_off is not None:
-        _on_device(w, q_off)
-        _dense(w, torch.int32, q_off)
-        if q_off.shape != (S + 1,):
+        if q_off.get_device() != dev:
+            _refuse(w)
+        if q_off.dtype != torch.int32:
+            _refuse(w, -4)
+        if q_off.shape != (S + 1,) or not q_off.is_contiguous():
             _refuse(w, -2)
-    fresh = torch.empty if q_off is None and R == S else torch.zeros
-    out = fresh((R, nq, hd), dtype=dt, device=q.device) if out is None else out
-    lse = fresh((R, nq), dtype=torch.float32, device=q.device) if lse is None else lse
-    _on_device(w, out, lse)
-    if out.shape != q.shape or lse.shape != (R, nq):
-        _refuse(w, -2)
-    _dense(w, dt, out)
-    _dense(w, torch.float32, lse)
-    _heads_packed(w, q, ctx_k, own_k)
+        off = q_off.data_ptr()
     if scratch is None:
         need = lib.akvs_op_attention_shared_scratch_bytes(R, P, nq, nkv, hd)
         scratch = torch.empty(max(need, 0), dtype=torch.uint8, device=q.device)
-    else:
-        _on_device(w, scratch)
-    _chk(lib.akvs_op_attention_shared(_CODE[dt], q.data_ptr(), _ld(q), R, ctx_k.data_ptr(), ctx_v.data_ptr(), _ld(ctx_k),
-                                      P, own_k.data_ptr(), own_v.data_ptr(), _ld(own_k, 1), own_k.stride(0), S, cap,
-                                      own_len.data_ptr(), q_off.data_ptr() if q_off is not None else None, nq, nkv, hd,
-                                      out.data_ptr(), lse.data_ptr(), scratch.data_ptr(), scratch.numel(), _stream()), w)
+    elif scratch.get_device() != dev or not scratch.is_contiguous():
+        _refuse(w)
+    _chk(lib.akvs_op_attention_shared(_CODE[dt], q.data_ptr(), _ld(w, qs, q.stride()), R, ctx_k.data_ptr(),
+                                      ctx_v.data_ptr(), _ld(w, cs, cst), P, own_k.data_ptr(), own_v.data_ptr(),
+                                      _ld(w, os_[1:], ost[1:]), ost[0], S, cap, own_len.data_ptr(), off, nq, nkv, hd,
+                                      out.data_ptr(), lse.data_ptr(), scratch.data_ptr(), scratch.nbytes,
+                                      _raw_stream(dev)), w)
     return out, lse
 
 
@@ -591,25 +585,29 @@ def op_attention_mass(q, k, lse, k_lo, k_hi, mass=None, out=None):
     log-sum-exp lse [R][n_q] put on the keys k [T][n_kv][hd] in k_lo[r] .. k_hi[r].  `out` may be
     `mass`."""
     w = "akvs_op_attention_mass"
-    _on_device(w, q, k, lse, k_lo, k_hi)
-    (R, nq, hd), (T, nkv, _) = q.shape, k.shape
-    if q.dtype not in _CODE or k.dtype != q.dtype:
+    dev, dt, qs, ks = _current(w, q.get_device()), q.dtype, q.shape, k.shape
+    (R, nq, hd), (T, nkv, _) = qs, ks
+    out = lse.new_empty((nkv, T)) if out is None else out
+    if not (dev == k.get_device() == lse.get_device() == k_lo.get_device() == k_hi.get_device() == out.get_device()):
+        _refuse(w)
+    if not (dt in _CODE and dt == k.dtype and lse.dtype == out.dtype == torch.float32
+            and k_lo.dtype == k_hi.dtype == torch.int32):
         _refuse(w, -4)
-    if k.shape[2] != hd or lse.shape != (R, nq) or k_lo.shape != (R,) or k_hi.shape != (R,):
+    if not (ks[2] == hd and lse.shape == (R, nq) and k_lo.shape == k_hi.shape == (R,) and out.shape == (nkv, T)
+            and lse.is_contiguous() and k_lo.is_contiguous() and k_hi.is_contiguous() and out.is_contiguous()):
         _refuse(w, -2)
-    out = torch.empty((nkv, T), dtype=torch.float32, device=q.device) if out is None else out
-    for t in (mass, out):
-        if t is not None:
-            _on_device(w, t)
-            _dense(w, torch.float32, t)
-            if t.shape != (nkv, T):
-                _refuse(w, -2)
-    _dense(w, torch.float32, lse)
-    _dense(w, torch.int32, k_lo, k_hi)
-    _heads_packed(w, q, k)
-    _chk(lib.akvs_op_attention_mass(_CODE[q.dtype], q.data_ptr(), _ld(q), k.data_ptr(), _ld(k), lse.data_ptr(),
-                                    k_lo.data_ptr(), k_hi.data_ptr(), R, T, nq, nkv, hd,
-                                    mass.data_ptr() if mass is not None else None, out.data_ptr(), _stream()), w)
+    old = None
+    if mass is not None:
+        if mass.get_device() != dev:
+            _refuse(w)
+        if mass.dtype != torch.float32:
+            _refuse(w, -4)
+        if mass.shape != (nkv, T) or not mass.is_contiguous():
+            _refuse(w, -2)
+        old = mass.data_ptr()
+    _chk(lib.akvs_op_attention_mass(_CODE[dt], q.data_ptr(), _ld(w, qs, q.stride()), k.data_ptr(), _ld(w, ks, k.stride()),
+                                    lse.data_ptr(), k_lo.data_ptr(), k_hi.data_ptr(), R, T, nq, nkv, hd, old,
+                                    out.data_ptr(), _raw_stream(dev)), w)
     return out
 
 
@@ -618,22 +616,22 @@ def op_evict(mass, k, v, budget, n_sink=0, n_recent=0):
     first n_sink, the last n_recent and the heaviest others.  Returns (idx [L][n_kv][budget],
     k_out, v_out [L][budget][n_kv][hd], mass_out [L][n_kv][budget]), tokens ascending."""
     w = "akvs_op_evict"
-    _on_device(w, mass, k, v)
-    (L, nkv, T), hd = mass.shape, k.shape[-1]
-    if k.dtype not in _CODE or v.dtype != k.dtype:
+    dev, dt, ks, kst = _current(w, k.get_device()), k.dtype, k.shape, k.stride()
+    L, T, nkv, hd = ks
+    if not (dev == v.get_device() == mass.get_device()):
+        _refuse(w)
+    if not (dt in _CODE and dt == v.dtype and mass.dtype == torch.float32):
         _refuse(w, -4)
-    if k.shape != (L, T, nkv, hd) or v.shape != k.shape or v.stride() != k.stride():
+    if not (v.shape == ks and v.stride() == kst and mass.shape == (L, nkv, T) and mass.is_contiguous() and budget <= T):
         _refuse(w, -2)
-    if not 0 <= budget <= T or n_sink < 0 or n_recent < 0:
-        _refuse(w, -2 if budget > T else -1)
-    _dense(w, torch.float32, mass)
-    _heads_packed(w, k)
-    idx = torch.empty((L, nkv, budget), dtype=torch.int32, device=k.device)
-    k_out = torch.empty((L, budget, nkv, hd), dtype=k.dtype, device=k.device)
-    v_out, m_out = torch.empty_like(k_out), torch.empty((L, nkv, budget), dtype=torch.float32, device=k.device)
-    tok_ld = _ld(k, 1)
-    layer_ld = k.stride(0) if L > 1 else T * tok_ld
-    _chk(lib.akvs_op_evict(_CODE[k.dtype], mass.data_ptr(), k.data_ptr(), v.data_ptr(), layer_ld, tok_ld, L, T, nkv, hd,
-                           budget, n_sink, n_recent, idx.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
-                           m_out.data_ptr(), _stream()), w)
-    return idx, k_out, v_out, m_out
+    if budget < 0:
+        _refuse(w)
+    mass_out = mass.new_empty((L, nkv, budget))
+    idx = torch.empty_like(mass_out, dtype=torch.int32)
+    k_out = k.new_empty((L, budget, nkv, hd))
+    v_out = torch.empty_like(k_out)
+    tok_ld = _ld(w, ks[1:], kst[1:])
+    _chk(lib.akvs_op_evict(_CODE[dt], mass.data_ptr(), k.data_ptr(), v.data_ptr(), kst[0] if L > 1 else T * tok_ld,
+                           tok_ld, L, T, nkv, hd, budget, n_sink, n_recent, idx.data_ptr(), k_out.data_ptr(),
+                           v_out.data_ptr(), mass_out.data_ptr(), _raw_stream(dev)), w)
+    return idx, k_out, v_out, mass_out
