@@ -740,17 +740,11 @@ std::unordered_map<TmapKey, CUtensorMap, TmapKeyHash> g_tmap_cache;
 constexpr size_t kTmapCacheMax = 16384;
 }  // namespace
 
-int32_t encode_tmap_2d_16bit(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t ld,
-                            uint32_t box_rows) {
+int32_t make_tmap_2d_16bit(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t ld,
+                           uint32_t box_rows) {
   EncodeFn enc = get_encoder();
   if (!enc) return AKVS_ERR_CUDA;
   if ((reinterpret_cast<uintptr_t>(base) & 15) || (ld * 2) % 16 != 0) return AKVS_ERR_SHAPE;
-  const TmapKey key{base, rows, cols, ld, box_rows};
-  auto it = g_tmap_cache.find(key);
-  if (it != g_tmap_cache.end()) {
-    *map = it->second;
-    return AKVS_OK;
-  }
   const cuuint64_t dims[2] = {cols, rows};
   const cuuint64_t strides[1] = {ld * 2};
   const cuuint32_t box[2] = {64, box_rows};
@@ -758,7 +752,18 @@ int32_t encode_tmap_2d_16bit(CUtensorMap* map, const void* base, uint64_t rows, 
   const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void*>(base), dims, strides, box, estr,
                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) return AKVS_ERR_CUDA;
+  return r == CUDA_SUCCESS ? AKVS_OK : AKVS_ERR_CUDA;
+}
+
+int32_t encode_tmap_2d_16bit(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t ld,
+                            uint32_t box_rows) {
+  const TmapKey key{base, rows, cols, ld, box_rows};
+  auto it = g_tmap_cache.find(key);
+  if (it != g_tmap_cache.end()) {
+    *map = it->second;
+    return AKVS_OK;
+  }
+  AKVS_TRY(make_tmap_2d_16bit(map, base, rows, cols, ld, box_rows));
   if (g_tmap_cache.size() >= kTmapCacheMax) g_tmap_cache.clear();
   g_tmap_cache.emplace(key, *map);
   return AKVS_OK;

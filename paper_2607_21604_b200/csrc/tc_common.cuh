@@ -241,6 +241,9 @@ __device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uin
 // if the driver entry point is missing or refuses the arguments.
 int32_t encode_tmap_2d_16bit(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t ld,
                             uint32_t box_rows);
+// The same without the process-wide table of maps: for tensors that belong to one call.
+int32_t make_tmap_2d_16bit(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t ld,
+                           uint32_t box_rows);
 // 3D: [d2][d1][d0 contiguous] with strides in elements; box [b2][b1][64].
 int32_t encode_tmap_3d_16bit(CUtensorMap* map, const void* base, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t ld1,
                             uint64_t ld2, uint32_t b1, uint32_t b2);
