@@ -14,7 +14,9 @@
 //     context's parts and writes the rows.  The launch overlaps the first (it waits for it only
 //     before it reads the parts).
 //
-// Both are memory bound for few rows: K and V go from global memory straight into the operand
+// Context, 16-bit types and more than one tile of 16 stacked rows: the tcgen05 attention kernel
+// (attn_tc.cu) on 128 stacked rows per CTA, so that K and V are read once for up to 128 of them.
+// The rest, and all own tokens, are memory bound with few rows: K and V go from global memory straight into the operand
 // registers of mma.sync m16n8k16, whose contraction index may be permuted at will (for Q K^T a
 // lane's 16-byte chunk of K and of Q supplies four of its k positions; for P V a lane's chunk
 // of V supplies one column of eight tiles), so no shared-memory staging stands between a load
@@ -518,30 +520,48 @@ own_join_kernel(const __grid_constant__ SharedParams p, int C) {
   pdl_wait();                                       // a CTA without rows, too: the next kernel relies on it
 }
 
-struct Plan { int splits, split_len; };
+struct Plan { bool tc; int splits, split_len; };
 
-// How the context is cut.  A CTA runs 64 keys at a time; two CTAs fit an SM.
-Plan plan_context(int R, int P, int g, int n_kv) {
-  if (P == 0 || R == 0) return {0, 0};
+// How the context is cut.
+Plan plan_context(bool is16, int R, int P, int g, int n_kv, int hd) {
+  if (P == 0 || R == 0) return {false, 0, 0};
+  if (is16 && (int64_t)R * g > MT) {
+    // One CTA per SM.  In units of a key tile: rounds of CTAs times (a CTA's tiles + 6 for its start
+    // and end), plus writing and reading the parts at memory speed (a tile takes about 0.7 us).
+    const int64_t base = (int64_t)akvs_cdiv(R, 128 / g) * n_kv;
+    const int tiles = akvs_cdiv(P, 128);
+    const double part = 2.0 * R * g * n_kv * (hd + 2) * 4 / 6.4e6 / 0.7;
+    int best = 1;
+    double best_cost = 1e300;
+    for (int s = 1; s <= tiles && s <= 148; ++s) {
+      const double cost = (double)((base * s + 147) / 148) * (akvs_cdiv(tiles, s) + 6) + part * s;
+      if (cost < best_cost) { best_cost = cost; best = s; }
+    }
+    const int len = akvs_cdiv(tiles, best) * 128;
+    return {true, akvs_cdiv(P, len), len};
+  }
+  // A CTA runs 64 keys at a time; two CTAs fit an SM.
   const int64_t base = (int64_t)n_kv * akvs_cdiv((int64_t)R * g, MT);
   int splits = (int)(base >= 296 ? 1 : akvs_cdiv(296, base));
   const int most = akvs_cdiv(P, 128);
   if (splits > most) splits = most;
   const int len = akvs_cdiv(akvs_cdiv(P, splits), 64) * 64;
-  return {akvs_cdiv(P, len), len};
+  return {false, akvs_cdiv(P, len), len};
 }
 
-int64_t scratch_bytes(int R, int P, int n_q, int n_kv, int hd) {
-  const Plan pl = plan_context(R, P, n_q / n_kv, n_kv);
-  const int64_t rows = (int64_t)pl.splits * R * n_q;
+int64_t parts_bytes(int splits, int R, int n_q, int hd) {
+  const int64_t rows = (int64_t)splits * R * n_q;
   return akvs_align_up(rows * hd * 4, 256) + akvs_align_up(rows * 8, 256) + 256;
 }
 
 template <typename T, int HD>
-int32_t run(SharedParams& p, cudaStream_t st) {
+int32_t run(SharedParams& p, int dtype, bool tc, cudaStream_t st) {
   constexpr int smem = direct_smem<T, HD>();
   static_assert(smem <= 48 * 1024, "the direct kernels stay below the size that needs an attribute");
-  if (p.splits > 0) {
+  if (p.splits > 0 && tc) {
+    AKVS_TRY(launch_attention_parts_tc(dtype, HD, p.q, p.q_ld, p.pk, p.pv, p.p_ld, p.R, p.P, p.n_q, p.n_kv, p.split_len,
+                                       p.part_o, p.part_ml, st));
+  } else if (p.splits > 0) {
     const int64_t tiles = akvs_cdiv((int64_t)p.R * p.g, MT);
     if (tiles > 65535) return AKVS_ERR_TOO_LARGE;
     AKVS_CUDA(launch_pdl(context_direct_kernel<T, HD>, dim3(p.splits, p.n_kv, (unsigned)tiles), dim3(DIR_THREADS), smem, st, p));
@@ -581,7 +601,9 @@ bool heads_ok(int32_t n_q, int32_t n_kv) { return n_kv > 0 && n_q > 0 && n_q % n
 extern "C" int64_t akvs_op_attention_shared_scratch_bytes(int32_t R, int32_t P, int32_t n_q_heads, int32_t n_kv_heads,
                                                           int32_t head_dim) {
   if (R < 0 || P < 0 || !heads_ok(n_q_heads, n_kv_heads) || (head_dim != 64 && head_dim != 128)) return -1;
-  return scratch_bytes(R, P, n_q_heads, n_kv_heads, head_dim);
+  const int g = n_q_heads / n_kv_heads;       // the larger of the two ways the types take
+  const int a = plan_context(true, R, P, g, n_kv_heads, head_dim).splits, b = plan_context(false, R, P, g, n_kv_heads, head_dim).splits;
+  return parts_bytes(a > b ? a : b, R, n_q_heads, head_dim);
 }
 
 extern "C" int32_t akvs_op_attention_shared(int32_t dtype, const void* q, int64_t q_ld, int32_t R, const void* ctx_k,
@@ -604,8 +626,8 @@ extern "C" int32_t akvs_op_attention_shared(int32_t dtype, const void* q, int64_
       (cap > 0 && (!aligned16(own_k) || !aligned16(own_v) || own_ld * es % 16 || own_seq_ld * es % 16)))
     return AKVS_ERR_INVALID_ARG;
   if ((int64_t)R * n_q_heads > 0x7fffffff || (int64_t)S * MAX_C > 0x7fffffff) return AKVS_ERR_TOO_LARGE;
-  const Plan pl = plan_context(R, P, n_q_heads / n_kv_heads, n_kv_heads);
-  const int64_t need = scratch_bytes(R, P, n_q_heads, n_kv_heads, head_dim);
+  const Plan pl = plan_context(dtype != AKVS_F32, R, P, n_q_heads / n_kv_heads, n_kv_heads, head_dim);
+  const int64_t need = parts_bytes(pl.splits, R, n_q_heads, head_dim);
   if (pl.splits > 0 && (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255) || scratch_size < need)) return AKVS_ERR_WORKSPACE;
   const int64_t ctx_n = P > 0 ? ((P - 1) * ctx_ld + row) * es : 0;
   const int64_t own_n = cap > 0 ? ((S - 1) * own_seq_ld + (cap - 1) * own_ld + row) * es : 0;
@@ -632,6 +654,6 @@ extern "C" int32_t akvs_op_attention_shared(int32_t dtype, const void* q, int64_
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   return dispatch_dtype(dtype, [&](auto tag) -> int32_t {
     using T = decltype(tag);
-    return head_dim == 64 ? run<T, 64>(p, st) : run<T, 128>(p, st);
+    return head_dim == 64 ? run<T, 64>(p, dtype, pl.tc, st) : run<T, 128>(p, dtype, pl.tc, st);
   });
 }

@@ -36,28 +36,30 @@
 // adjacent to it, its own query tokens) a row also sees k_lo2[r] <= j <= k_hi2[r]; the key
 // tiles of a CTA then walk the hull of its rows' first ranges and after it the hull of the
 // second ranges, each tile masked with the range of its segment.
+// PART: all rows see all keys (a context that many sequences share).  The key range is cut into
+// splits so that few row blocks still fill the device, and a CTA leaves its rows' unnormalised
+// output, reference maximum and row sum in float for a later join; head_dim may also be 64.
 #include "tc_common.cuh"
 
 namespace {
 
-constexpr int HD = 128;              // head dimension
 constexpr int BN = 128;              // keys per tile
 constexpr int SLAB = 128 * 64 * 2;   // one 64-wide slab of a 128-row tile: 16 KB
-constexpr int TILE = 2 * SLAB;       // 32 KB
+template <int HD> constexpr int TILE_OF = HD / 64 * SLAB;      // 32 KB for head_dim 128
 constexpr int ATT_THREADS = 384;     // warp group 0: TMA / MMA, warp groups 1 and 2: softmax
 constexpr int K_STAGES = 3, V_STAGES = 4;
 constexpr float RESCALE_STEP = 8.f;  // the reference maximum may lag a tile's maximum by this much
 // shared memory: K[3] | V[4] | barriers | reference maxima and row sums
-constexpr int OFF_K = 0, OFF_V = K_STAGES * TILE, OFF_BAR = (K_STAGES + V_STAGES) * TILE;
-constexpr int OFF_ROW = OFF_BAR + 512;       // float m_ref[128], l_part[2][128], m_part[2][128]
-constexpr int ATT_SMEM = OFF_ROW + 5 * 128 * 4;    // 232448 bytes is all a CTA may own: no slack for
-                                                   // re-aligning, the buffer itself is declared 1024-byte aligned
+// (float m_ref[128], l_part[2][128], m_part[2][128])
+// 232448 bytes is all a CTA may own: no slack for re-aligning, the buffer itself is declared 1024-byte aligned
+template <int HD> constexpr int ATT_SMEM = (K_STAGES + V_STAGES) * TILE_OF<HD> + 512 + 5 * 128 * 4;
 // tensor-memory columns
 constexpr uint32_t COL_O = 0, COL_Q = 128, COL_P = 192, COL_S = 256;
 
 struct AttnParams {
   int R, T, n_q, n_kv, g, BR, row_blocks;
   const void* q;
+  int64_t q_ld;                // elements between rows of q
   const int32_t* k_lo;
   const int32_t* k_hi;
   const int32_t* k_lo2;        // second visible range per row, or null
@@ -66,6 +68,9 @@ struct AttnParams {
   float scale_log2;            // log2(e) / sqrt(head_dim)
   uint32_t idesc_qk, idesc_pv;
   int32_t* status;
+  int split_len;               // PART: keys of a split (a multiple of BN)
+  float* part_o;               // PART: [splits][R * n_q][HD]
+  float2* part_ml;             // PART: [splits][R * n_q] (reference maximum in log2 units, row sum)
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -94,12 +99,14 @@ enum { B_QFULL = 0,     // Q sits in tensor memory (4 warps)
        B_FIN = B_DEC + 8,               // [4] both warps of this quad have published their row sums
        B_COUNT = B_FIN + 4 };
 static_assert(B_COUNT * 8 + 16 <= 512, "barriers, the tensor-memory slot and the abort flag share 512 bytes");
-static_assert((K_STAGES + V_STAGES) * TILE + 512 + 5 * 128 * 4 <= 232448, "shared memory of one CTA");
+static_assert(ATT_SMEM<128> <= 232448, "shared memory of one CTA");
 
-template <typename T>
+template <typename T, int HD, bool PART>
 __global__ void __launch_bounds__(ATT_THREADS, 1)
 attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                     const AttnParams p) {
+  constexpr int TILE = TILE_OF<HD>;
+  constexpr int OFF_K = 0, OFF_V = K_STAGES * TILE, OFF_BAR = (K_STAGES + V_STAGES) * TILE, OFF_ROW = OFF_BAR + 512;
   extern __shared__ __align__(1024) uint8_t smem[];
   if (tc::smem_u32(smem) & 1023u) {               // swizzled tiles need 1024-byte alignment
     if (threadIdx.x == 0) set_status(p.status, AKVS_ERR_UNSUPPORTED);
@@ -113,7 +120,7 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   float* m_part = m_ref + 3 * 128;                                // [2][128]
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  pdl_trigger();
+  if constexpr (!PART) pdl_trigger();
   if (threadIdx.x == 0) {
     for (int i = 0; i < B_COUNT; ++i) {
       int count = 1;
@@ -131,15 +138,18 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
     tc::tmem_relinquish();
   }
   pdl_wait();                       // the key ranges below are the first global memory this kernel reads
+  if constexpr (PART) pdl_trigger();    // after the wait: the join reads what is older than this kernel without waiting
   // 1-D grid, kv head fastest: CTAs are handed out longest row block first across ALL heads
   // (the last rows see the most keys), so the tail of the launch is made of short CTAs
-  const int hk = blockIdx.x % p.n_kv;
-  const int r0 = (p.row_blocks - 1 - blockIdx.x / p.n_kv) * p.BR;
+  // PART: the row blocks of one kv head and split are neighbours, so that they share K/V in L2
+  const int hk = PART ? (blockIdx.x / p.row_blocks) % p.n_kv : blockIdx.x % p.n_kv;
+  const int r0 = PART ? (blockIdx.x % p.row_blocks) * p.BR : (p.row_blocks - 1 - blockIdx.x / p.n_kv) * p.BR;
+  const int split = PART ? blockIdx.x / (p.row_blocks * p.n_kv) : 0;
   const int n_rows = min(p.BR, p.R - r0);
-  int key_lo = p.k_lo[r0];
-  int key_hi = p.k_hi[r0 + n_rows - 1];
+  int key_lo = PART ? split * p.split_len : p.k_lo[r0];
+  int key_hi = PART ? min(key_lo + p.split_len, p.T) - 1 : p.k_hi[r0 + n_rows - 1];
   int key_lo2 = 1, key_hi2 = 0;
-  if (p.k_lo2) {
+  if (!PART && p.k_lo2) {
     // two ranges per row: neither is monotone across the rows of a block, take the hulls
     int a = 0x7fffffff, b = -1, c = 0x7fffffff, d = -1;
     for (int i = lane; i < n_rows; i += 32) {
@@ -178,8 +188,9 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
           const int y = tile_key(j);
           if (!tc::mbar_wait(&bar[B_KEMPTY + s], ph, abort_flag)) { ok = false; break; }
           tc::mbar_expect_tx(&bar[B_KFULL + s], TILE);
-          tc::tma_load_2d(smem + OFF_K + s * TILE, &tmK, hk * HD, y, &bar[B_KFULL + s]);
-          tc::tma_load_2d(smem + OFF_K + s * TILE + SLAB, &tmK, hk * HD + 64, y, &bar[B_KFULL + s]);
+#pragma unroll
+          for (int c = 0; c < HD / 64; ++c)
+            tc::tma_load_2d(smem + OFF_K + s * TILE + c * SLAB, &tmK, hk * HD + c * 64, y, &bar[B_KFULL + s]);
         }
         if (!ok) { *abort_flag = 1; set_status(p.status, AKVS_ERR_TIMEOUT); }
       }
@@ -194,8 +205,9 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
           const int y = tile_key(j);
           if (!tc::mbar_wait(&bar[B_VEMPTY + s], ph, abort_flag)) { ok = false; break; }
           tc::mbar_expect_tx(&bar[B_VFULL + s], TILE);
-          tc::tma_load_2d(smem + OFF_V + s * TILE, &tmV, hk * HD, y, &bar[B_VFULL + s]);
-          tc::tma_load_2d(smem + OFF_V + s * TILE + SLAB, &tmV, hk * HD + 64, y, &bar[B_VFULL + s]);
+#pragma unroll
+          for (int c = 0; c < HD / 64; ++c)
+            tc::tma_load_2d(smem + OFF_V + s * TILE + c * SLAB, &tmV, hk * HD + c * 64, y, &bar[B_VFULL + s]);
         }
         if (!ok) { *abort_flag = 1; set_status(p.status, AKVS_ERR_TIMEOUT); }
       }
@@ -259,10 +271,10 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
     // Rows of the M tile that belong to no query row (g does not divide 128, or the last row
     // block is short) have Q = 0 and are never written: they take every key as visible, so that
     // their warp does not run the masking pass on every tile for their sake.
-    const int hi1 = valid ? p.k_hi[r] : 0x3fffffff;
-    const int lo1 = !valid ? -0x40000000 : (p.k_lo[r] <= hi1 ? p.k_lo[r] : 0x40000000);   // nothing visible: no key reaches lo
-    const int hi2 = !valid ? 0x3fffffff : (p.k_lo2 ? p.k_hi2[r] : -1);
-    const int lo2 = !valid ? -0x40000000 : (p.k_lo2 && p.k_lo2[r] <= hi2 ? p.k_lo2[r] : 0x40000000);
+    const int hi1 = !valid ? 0x3fffffff : (PART ? key_hi : p.k_hi[r]);
+    const int lo1 = !valid ? -0x40000000 : PART ? key_lo : (p.k_lo[r] <= hi1 ? p.k_lo[r] : 0x40000000);   // nothing visible: no key reaches lo
+    const int hi2 = !valid ? 0x3fffffff : (!PART && p.k_lo2 ? p.k_hi2[r] : -1);
+    const int lo2 = !valid ? -0x40000000 : (!PART && p.k_lo2 && p.k_lo2[r] <= hi2 ? p.k_lo2[r] : 0x40000000);
     // key visible  <=>  lo <= key <= hi  <=>  (unsigned)(key - lo) <= hi - lo: one compare and a
     // select per element (a per-element && / || compiles to divergent branches, measured 2x slower)
     const unsigned span1 = hi1 >= lo1 ? (unsigned)(hi1 - lo1) : 0u;
@@ -270,10 +282,10 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
     const uint32_t lane_addr = tmem_base + ((uint32_t)(quad * 32) << 16);
     if (grp == 0 && n_tiles > 0) {
       // Q row of this thread: global -> registers -> tensor memory, 16-bit pairs as they lie in memory
-      const uint4* qp = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.q) +
-                                                       ((size_t)r * p.n_q + (size_t)hk * p.g + head) * HD);
+      const uint4* qp = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.q) + (size_t)r * p.q_ld +
+                                                       ((size_t)hk * p.g + head) * HD);
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
+      for (int c = 0; c < HD / 64; ++c) {
         uint32_t w[32];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -391,19 +403,28 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
       const float m_fin = fmaxf(ma, mb);            // the maximum only grows: the later tile's is final
       const float l = l_part[m] * ex2(ma - m_fin) + l_part[128 + m] * ex2(mb - m_fin);
       const float inv = l > 0.f ? 1.f / l : 0.f;
-      float o[64];
+      constexpr int HALF = HD / 2;
+      float o[HALF];
       if (n_tiles > 0) {
-        tc::tmem_ld32(lane_addr + COL_O + grp * 64, *reinterpret_cast<float(*)[32]>(&o[0]));
-        tc::tmem_ld32(lane_addr + COL_O + grp * 64 + 32, *reinterpret_cast<float(*)[32]>(&o[32]));
+#pragma unroll
+        for (int c = 0; c < HALF / 32; ++c)
+          tc::tmem_ld32(lane_addr + COL_O + grp * HALF + c * 32, *reinterpret_cast<float(*)[32]>(&o[c * 32]));
         tc::tmem_ld_wait();
       } else {
 #pragma unroll
-        for (int i = 0; i < 64; ++i) o[i] = 0.f;
+        for (int i = 0; i < HALF; ++i) o[i] = 0.f;
       }
-      if (valid) {
-        T* op = reinterpret_cast<T*>(p.out) + ((size_t)r * p.n_q + (size_t)hk * p.g + head) * HD + grp * 64;
+      const size_t at = (size_t)r * p.n_q + (size_t)hk * p.g + head;
+      if (PART && valid) {
+        const size_t row = (size_t)split * p.R * p.n_q + at;
+        float* op = p.part_o + row * HD + grp * HALF;
 #pragma unroll
-        for (int v = 0; v < 8; ++v) {
+        for (int v = 0; v < HALF; v += 4) *reinterpret_cast<float4*>(op + v) = make_float4(o[v], o[v + 1], o[v + 2], o[v + 3]);
+        if (grp == 0) p.part_ml[row] = make_float2(m_fin, l);
+      } else if (valid) {
+        T* op = reinterpret_cast<T*>(p.out) + at * HD + grp * HALF;
+#pragma unroll
+        for (int v = 0; v < HALF / 8; ++v) {
           float w[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) w[i] = o[v * 8 + i] * inv;
@@ -423,6 +444,28 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
   }
 }
 
+template <typename T, int HD, bool PART>
+int32_t launch(AttnParams& p, const void* k, const void* v, int64_t kv_ld, int n_cta, cudaStream_t st) {
+  static bool attr_set = false;
+  if (!attr_set) {
+    AKVS_CUDA(cudaFuncSetAttribute(attention_tc_kernel<T, HD, PART>, cudaFuncAttributeMaxDynamicSharedMemorySize, ATT_SMEM<HD>));
+    attr_set = true;
+  }
+  p.scale_log2 = 1.4426950408889634f / sqrtf((float)HD);
+  const uint32_t fmt = std::is_same<T, f16>::value ? tc::kF16 : tc::kBF16;
+  p.idesc_qk = tc::idesc_f16(fmt, 128, BN, 0);
+  p.idesc_pv = tc::idesc_f16(fmt, 128, HD, 1);
+  CUtensorMap tmK, tmV;
+  auto encode = PART ? make_tmap_2d_16bit : encode_tmap_2d_16bit;
+  AKVS_TRY(encode(&tmK, k, p.T, (uint64_t)p.n_kv * HD, (uint64_t)kv_ld, BN));
+  AKVS_TRY(encode(&tmV, v, p.T, (uint64_t)p.n_kv * HD, (uint64_t)kv_ld, BN));
+  double flops = 0;   // filled by the caller's accounting when profiling attention
+  ProfScope prof(3, 0, flops, st);
+  AKVS_CUDA(launch_pdl(attention_tc_kernel<T, HD, PART>, dim3((unsigned)n_cta), dim3(ATT_THREADS), ATT_SMEM<HD>, st, tmK, tmV, p));
+  AKVS_LAUNCHED();
+  return AKVS_OK;
+}
+
 }  // namespace
 
 // q [R][n_q][128], k/v [T][n_kv][128], out [R][n_q][128], all of the 16-bit type `dtype`.
@@ -432,30 +475,31 @@ int32_t launch_attention_tc(int dtype, const void* q, const void* k, const void*
   if (R == 0) return AKVS_OK;
   if (dtype != AKVS_BF16 && dtype != AKVS_F16) return AKVS_ERR_UNSUPPORTED;
   if (n_kv <= 0 || n_q % n_kv != 0 || n_q / n_kv > 128 || T <= 0) return AKVS_ERR_SHAPE;
-  static bool attr_set = false;
-  if (!attr_set) {
-    AKVS_CUDA(cudaFuncSetAttribute(attention_tc_kernel<bf16>, cudaFuncAttributeMaxDynamicSharedMemorySize, ATT_SMEM));
-    AKVS_CUDA(cudaFuncSetAttribute(attention_tc_kernel<f16>, cudaFuncAttributeMaxDynamicSharedMemorySize, ATT_SMEM));
-    attr_set = true;
-  }
-  AttnParams p;
+  AttnParams p = {};
   p.R = R; p.T = T; p.n_q = n_q; p.n_kv = n_kv;
   p.g = n_q / n_kv;
   p.BR = 128 / p.g;
-  p.q = q; p.k_lo = k_lo; p.k_hi = k_hi; p.k_lo2 = k_lo2; p.k_hi2 = k_lo2 ? k_hi2 : nullptr; p.out = out; p.status = status;
-  p.scale_log2 = 1.4426950408889634f / sqrtf((float)HD);
-  const uint32_t fmt = dtype == AKVS_F16 ? tc::kF16 : tc::kBF16;
-  p.idesc_qk = tc::idesc_f16(fmt, 128, BN, 0);
-  p.idesc_pv = tc::idesc_f16(fmt, 128, HD, 1);
-  CUtensorMap tmK, tmV;
-  AKVS_TRY(encode_tmap_2d_16bit(&tmK, k, T, (uint64_t)n_kv * HD, (uint64_t)n_kv * HD, BN));
-  AKVS_TRY(encode_tmap_2d_16bit(&tmV, v, T, (uint64_t)n_kv * HD, (uint64_t)n_kv * HD, BN));
+  p.q = q; p.q_ld = (int64_t)n_q * 128;
+  p.k_lo = k_lo; p.k_hi = k_hi; p.k_lo2 = k_lo2; p.k_hi2 = k_lo2 ? k_hi2 : nullptr; p.out = out; p.status = status;
   p.row_blocks = akvs_cdiv(R, p.BR);
-  const dim3 grid((unsigned)p.row_blocks * n_kv);
-  double flops = 0;   // filled by the caller's accounting when profiling attention
-  ProfScope prof(3, 0, flops, st);
-  if (dtype == AKVS_BF16) AKVS_CUDA(launch_pdl(attention_tc_kernel<bf16>, grid, dim3(ATT_THREADS), ATT_SMEM, st, tmK, tmV, p));
-  else AKVS_CUDA(launch_pdl(attention_tc_kernel<f16>, grid, dim3(ATT_THREADS), ATT_SMEM, st, tmK, tmV, p));
-  AKVS_LAUNCHED();
-  return AKVS_OK;
+  const int64_t kv_ld = (int64_t)n_kv * 128;
+  return dtype == AKVS_BF16 ? launch<bf16, 128, false>(p, k, v, kv_ld, p.row_blocks * n_kv, st)
+                            : launch<f16, 128, false>(p, k, v, kv_ld, p.row_blocks * n_kv, st);
+}
+
+int32_t launch_attention_parts_tc(int dtype, int hd, const void* q, int64_t q_ld, const void* k, const void* v, int64_t kv_ld,
+                                  int R, int T, int n_q, int n_kv, int split_len, float* part_o, float2* part_ml,
+                                  cudaStream_t st) {
+  AttnParams p = {};
+  p.R = R; p.T = T; p.n_q = n_q; p.n_kv = n_kv;
+  p.g = n_q / n_kv;
+  p.BR = 128 / p.g;
+  p.q = q; p.q_ld = q_ld;
+  p.row_blocks = akvs_cdiv(R, p.BR);
+  p.split_len = split_len; p.part_o = part_o; p.part_ml = part_ml;
+  const int64_t n_cta = (int64_t)p.row_blocks * n_kv * akvs_cdiv(T, split_len);
+  if (n_cta > 0x7fffffff) return AKVS_ERR_TOO_LARGE;
+  if (dtype == AKVS_BF16)
+    return hd == 64 ? launch<bf16, 64, true>(p, k, v, kv_ld, (int)n_cta, st) : launch<bf16, 128, true>(p, k, v, kv_ld, (int)n_cta, st);
+  return hd == 64 ? launch<f16, 64, true>(p, k, v, kv_ld, (int)n_cta, st) : launch<f16, 128, true>(p, k, v, kv_ld, (int)n_cta, st);
 }

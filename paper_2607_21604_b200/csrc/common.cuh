@@ -267,6 +267,11 @@ int32_t launch_linear_tc(int dtype, int epi, const void* x, int M, int K, int n_
 int32_t launch_attention_tc(int dtype, const void* q, const void* k, const void* v, void* out, const int32_t* k_lo,
                             const int32_t* k_hi, const int32_t* k_lo2, const int32_t* k_hi2, int R, int T, int n_q,
                             int n_kv, int32_t* status, cudaStream_t st);
+// The same kernel over a context that all rows see, keys cut into splits of split_len (a multiple of
+// 128): float (m, l, O) of every row and split, unnormalised.  head_dim 64 or 128.
+int32_t launch_attention_parts_tc(int dtype, int hd, const void* q, int64_t q_ld, const void* k, const void* v, int64_t kv_ld,
+                                  int R, int T, int n_q, int n_kv, int split_len, float* part_o, float2* part_ml,
+                                  cudaStream_t st);
 int32_t launch_attention_simt(int dtype, const void* q, const void* k, const void* v, void* out,
                               const int32_t* k_lo, const int32_t* k_hi, const int32_t* k_lo2, const int32_t* k_hi2,
                               int R, int n_q, int n_kv, int hd, cudaStream_t st);
