@@ -36,44 +36,56 @@ constexpr float LOG2E = 1.4426950408889634f;
 
 // ---- tensor cores
 constexpr int BK = 128;              // keys of a tile, two tiles per item
-constexpr int BQ = 128;              // stacked rows of a tile at most
-constexpr int MK_STAGES = 2, MQ_STAGES = 2, M_THREADS = 384;
+constexpr int M_THREADS = 384;       // warp group 0: TMA and MMA, warp groups 1 and 2: sums
 constexpr int M_SLAB = 128 * 128;    // 128 rows of 64 values
-template <int HD> constexpr int M_TILE = HD / 64 * M_SLAB;
-// shared memory: K[2][2 tiles] | Q[2] | barriers (256 B) | per group: what a column sees, [2][128] | partial sums | flags
-constexpr int M_COL_BYTES = 2 * 128 * 4 + 2 * 128 * 8;
-template <int HD> constexpr int M_SMEM = (2 * MK_STAGES + MQ_STAGES) * M_TILE<HD> + 256 + 2 * M_COL_BYTES + 2 * 128 * 4 + 64;
-enum { MB_KFULL = 0, MB_KEMPTY = MB_KFULL + MK_STAGES, MB_QFULL = MB_KEMPTY + MK_STAGES, MB_QEMPTY = MB_QFULL + MQ_STAGES,
-       MB_SFULL = MB_QEMPTY + MQ_STAGES,      // [2 groups][2 buffers] S^T of a tile is complete
-       MB_SEMPTY = MB_SFULL + 4,              // [2][2] the group has taken it into registers (4 warps)
-       MB_COUNT = MB_SEMPTY + 4 };
+// FEW: all stacked rows fit 128 columns.  One Q tile stays as long as the head does, K streams
+// through two stages and S^T has two buffers, so that items overlap.  Otherwise row tiles of 256
+// columns stream past one K item: an MMA of 256 columns reads its A operand from shared memory half
+// as often per column (with 128 columns the tensor pipe took 2.4x its rate's time and bounded the
+// kernel: 241 us for 512 rows x 40 heads x 32768 keys), and the loads of the next K hide
+// behind the sums of the last tile.
+template <bool FEW> struct MassCfg {
+  static constexpr int BQ = FEW ? 128 : 256, NB = FEW ? 2 : 1, KST = FEW ? 2 : 1, QST = FEW ? 1 : 2;
+};
+template <int HD> constexpr int M_TILE = HD / 64 * M_SLAB;               // 128 rows
+// shared memory: K[KST][2 tiles] | Q[QST] | barriers (256 B) | what a column sees, twice | partial sums | flags
+template <bool FEW> constexpr int M_COLS = 2 * MassCfg<FEW>::BQ * (4 + 8);
+template <int HD, bool FEW> constexpr int M_SMEM = (2 * MassCfg<FEW>::KST + MassCfg<FEW>::QST * MassCfg<FEW>::BQ / 128) * M_TILE<HD> +
+                                                   256 + M_COLS<FEW> + 2 * 128 * 4 + 64;
+enum { MB_KFULL = 0, MB_KEMPTY = 2, MB_QFULL = 4, MB_QEMPTY = 6,
+       MB_SFULL = 8,                          // [2 groups][2 buffers] S^T of a tile is complete
+       MB_SEMPTY = 12,                        // [2][2] the group has taken it into registers (4 warps)
+       MB_CFULL = 16, MB_CEMPTY = 18,         // [2] what the columns of a tile see has been written / read (2 warps, 8 warps)
+       MB_COUNT = 20 };
 static_assert(MB_COUNT * 8 + 8 <= 256, "barriers, the tensor-memory slot and the abort flag share 256 bytes");
-static_assert(M_SMEM<128> <= 232448, "shared memory of one CTA");
+static_assert(M_SMEM<128, true> <= 232448 && M_SMEM<128, false> <= 232448, "shared memory of one CTA");
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ void group_sync(int grp) { asm volatile("bar.sync %0, 128;" ::"r"(grp + 1) : "memory"); }
-
-template <typename T, int HD>
+template <typename T, int HD, bool FEW>
 __global__ void __launch_bounds__(M_THREADS, 1)
 mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmQ, const MassParams p,
-               int C, int key_items, int n_items, int BR, uint32_t fmt) {
-  constexpr int TILE = M_TILE<HD>;
-  constexpr int OFF_Q = 2 * MK_STAGES * TILE, OFF_BAR = OFF_Q + MQ_STAGES * TILE, OFF_COL = OFF_BAR + 256;
-  constexpr int OFF_PART = OFF_COL + 2 * M_COL_BYTES, OFF_FLAG = OFF_PART + 2 * 128 * 4;
+               int C, int key_items, int n_items, int BR, int q_boxes, uint32_t fmt) {
+  using Cfg = MassCfg<FEW>;
+  constexpr int TILE = M_TILE<HD>, BQ = Cfg::BQ, NB = Cfg::NB, KST = Cfg::KST, QST = Cfg::QST, Q_BYTES = BQ / 128 * TILE;
+  constexpr int OFF_Q = 2 * KST * TILE, OFF_BAR = OFF_Q + QST * Q_BYTES, OFF_COL = OFF_BAR + 256;
+  constexpr int OFF_PART = OFF_COL + M_COLS<FEW>, OFF_FLAG = OFF_PART + 2 * 128 * 4, Q_SLAB = BQ * 128;
   extern __shared__ __align__(1024) uint8_t smem[];
   if (tc::smem_u32(smem) & 1023u) return;           // swizzled tiles need 1024-byte alignment (the same in every CTA)
   uint64_t* bar = reinterpret_cast<uint64_t*>(smem + OFF_BAR);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + MB_COUNT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   float* part = reinterpret_cast<float*>(smem + OFF_PART);          // [2][128]
+  float* col_z = reinterpret_cast<float*>(smem + OFF_COL);          // [2][BQ] -lse of a column in log2 units
+  int2* col_rng = reinterpret_cast<int2*>(col_z + 2 * BQ);          // [2][BQ] its first visible key, and how many follow
+  volatile int* flag = reinterpret_cast<volatile int*>(smem + OFF_FLAG);    // [2][2 groups][2 halves] a column needs a mask
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_trigger();
   if (threadIdx.x == 0) {
-    for (int i = 0; i < MB_COUNT; ++i) tc::mbar_init(&bar[i], i >= MB_SEMPTY ? 4 : 1);
+    for (int i = 0; i < MB_COUNT; ++i) tc::mbar_init(&bar[i], i >= MB_CEMPTY ? 8 : i >= MB_CFULL ? 2 : i >= MB_SEMPTY ? 4 : 1);
     *abort_flag = 0;
     tc::fence_barrier_init();
   }
@@ -81,8 +93,8 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     tc::tmem_alloc(tmem_slot, 512);
     tc::tmem_relinquish();
   }
-  // Q tiles hold BR * g rows; where g does not divide 128 the last ones are never loaded and stay zero
-  for (int i = threadIdx.x; i < MQ_STAGES * TILE / 16; i += M_THREADS)
+  // Q tiles hold BR * g rows; what the loads leave out behind them stays zero
+  for (int i = threadIdx.x; i < QST * Q_BYTES / 16; i += M_THREADS)
     *reinterpret_cast<uint4*>(smem + OFF_Q + i * 16) = make_uint4(0u, 0u, 0u, 0u);
   tc::fence_proxy_async();
   pdl_wait();
@@ -90,8 +102,13 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
   __syncthreads();
   tc::fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
-  const int rank = blockIdx.x % C, first = blockIdx.x / C, stride = gridDim.x / C;
+  // FEW: consecutive items (of one head, mostly) for each cluster.  Otherwise every n_cl-th, so that
+  // masked items (the end of a causal window) spread.
+  const int rank = blockIdx.x % C, n_cl = gridDim.x / C, cl = blockIdx.x / C;
+  const int item0 = FEW ? (int)((int64_t)n_items * cl / n_cl) : cl, step = FEW ? 1 : n_cl;
+  const int item1 = FEW ? (int)((int64_t)n_items * (cl + 1) / n_cl) : n_items;
   const int row_tiles = (p.R + BR - 1) / BR;
+  auto head_ends = [&](int item) { return item + 1 == item1 || (item + 1) / key_items != item / key_items; };
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
@@ -100,25 +117,29 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       if (lane == 0) {
         tc::prefetch_tmap(&tmK);
         tc::prefetch_tmap(&tmQ);
-        const uint32_t q_bytes = (uint32_t)(BR * p.g) * 128u * (HD / 64);
+        // boxes of at most 128 stacked rows, back to back
+        const int box_rows = BR / q_boxes, box_bytes = box_rows * p.g * 128;
         bool ok = true;
         int it = 0, n = 0;
-        for (int item = first; item < n_items && ok; item += stride, ++it) {
-          const int h = item / key_items, j0 = (item % key_items) * (2 * BK), ks = it % MK_STAGES;
-          if (!tc::mbar_wait(&bar[MB_KEMPTY + ks], ((it / MK_STAGES) & 1) ^ 1, abort_flag)) { ok = false; break; }
+        for (int item = item0; item < item1 && ok; item += step, ++it) {
+          const int h = item / key_items, j0 = (item % key_items) * (2 * BK), ks = it % KST;
+          if (!tc::mbar_wait(&bar[MB_KEMPTY + ks], ((it / KST) & 1) ^ 1, abort_flag)) { ok = false; break; }
           tc::mbar_expect_tx(&bar[MB_KFULL + ks], 2 * TILE);
 #pragma unroll
           for (int w = 0; w < 2; ++w)
 #pragma unroll
             for (int c = 0; c < HD / 64; ++c)
               tc::tma_load_2d(smem + (2 * ks + w) * TILE + c * M_SLAB, &tmK, h * HD + c * 64, j0 + w * BK, &bar[MB_KFULL + ks]);
+          if (FEW && it > 0 && (item - 1) / key_items == h) continue;    // the head's rows are there
           for (int rt = rank; rt < row_tiles; rt += C, ++n) {
-            const int qs = n % MQ_STAGES;
-            if (!tc::mbar_wait(&bar[MB_QEMPTY + qs], ((n / MQ_STAGES) & 1) ^ 1, abort_flag)) { ok = false; break; }
-            tc::mbar_expect_tx(&bar[MB_QFULL + qs], q_bytes);
+            const int qs = n % QST;
+            if (!tc::mbar_wait(&bar[MB_QEMPTY + qs], ((n / QST) & 1) ^ 1, abort_flag)) { ok = false; break; }
+            tc::mbar_expect_tx(&bar[MB_QFULL + qs], (uint32_t)(q_boxes * box_bytes * (HD / 64)));
+            for (int x = 0; x < q_boxes; ++x)
 #pragma unroll
-            for (int c = 0; c < HD / 64; ++c)
-              tc::tma_load_3d(smem + OFF_Q + qs * TILE + c * M_SLAB, &tmQ, c * 64, h * p.g, rt * BR, &bar[MB_QFULL + qs]);
+              for (int c = 0; c < HD / 64; ++c)
+                tc::tma_load_3d(smem + OFF_Q + qs * Q_BYTES + c * Q_SLAB + x * box_bytes, &tmQ, c * 64, h * p.g,
+                                rt * BR + x * box_rows, &bar[MB_QFULL + qs]);
           }
         }
         if (!ok) *abort_flag = 1;
@@ -127,101 +148,165 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       // ------------------------------------------------------------------ MMA issuer
       if (lane == 0) {
         bool ok = true;
-        int it = 0, n = 0;
-        for (int item = first; item < n_items && ok; item += stride, ++it) {
-          const int ks = it % MK_STAGES;
-          if (!tc::mbar_wait(&bar[MB_KFULL + ks], (it / MK_STAGES) & 1, abort_flag)) { ok = false; break; }
+        int it = 0, n = 0, nq = 0;                    // items, tiles, Q tiles so far
+        for (int item = item0; item < item1 && ok; item += step, ++it) {
+          const int ks = it % KST;
+          if (!tc::mbar_wait(&bar[MB_KFULL + ks], (it / KST) & 1, abort_flag)) { ok = false; break; }
           for (int rt = rank; rt < row_tiles && ok; rt += C, ++n) {
-            const int qs = n % MQ_STAGES, b = n & 1;
-            if (!tc::mbar_wait(&bar[MB_QFULL + qs], (n / MQ_STAGES) & 1, abort_flag)) { ok = false; break; }
+            const int qs = nq % QST, b = n % NB;
+            if (!tc::mbar_wait(&bar[MB_QFULL + qs], (nq / QST) & 1, abort_flag)) { ok = false; break; }
             const int cols = min(BR, p.R - rt * BR) * p.g;
-            const uint32_t idesc = tc::idesc_f16(fmt, BK, (cols + 15) / 16 * 16, 0);
-            const uint32_t q_addr = tc::smem_u32(smem + OFF_Q + qs * TILE);
+            const uint32_t idesc = tc::idesc_f16(fmt, BK, (cols + 63) / 64 * 64, 0);      // whole chunks: rows of zeros behind the last
+            const uint32_t q_addr = tc::smem_u32(smem + OFF_Q + qs * Q_BYTES);
             for (int w = 0; w < 2; ++w) {
-              if (!tc::mbar_wait(&bar[MB_SEMPTY + 2 * w + b], ((n >> 1) & 1) ^ 1, abort_flag)) { ok = false; break; }
+              if (!tc::mbar_wait(&bar[MB_SEMPTY + 2 * w + b], ((n / NB) & 1) ^ 1, abort_flag)) { ok = false; break; }
               tc::fence_after_sync();
               const uint32_t k_addr = tc::smem_u32(smem + (2 * ks + w) * TILE);
 #pragma unroll
-              for (int k = 0; k < HD / 16; ++k) {
-                const uint32_t off = (k >> 2) * M_SLAB + (k & 3) * 32;
-                tc::mma_f16(tmem_base + (2 * w + b) * BQ, tc::smem_desc_k_sw128(k_addr + off),
-                            tc::smem_desc_k_sw128(q_addr + off), idesc, k != 0);
-              }
+              for (int k = 0; k < HD / 16; ++k)
+                tc::mma_f16(tmem_base + w * 256 + b * BQ, tc::smem_desc_k_sw128(k_addr + (k >> 2) * M_SLAB + (k & 3) * 32),
+                            tc::smem_desc_k_sw128(q_addr + (k >> 2) * Q_SLAB + (k & 3) * 32), idesc, k != 0);
               tc::mma_commit(&bar[MB_SFULL + 2 * w + b]);
             }
-            if (ok) tc::mma_commit(&bar[MB_QEMPTY + qs]);
+            if (ok && (!FEW || head_ends(item))) { tc::mma_commit(&bar[MB_QEMPTY + qs]); ++nq; }
           }
           if (ok) tc::mma_commit(&bar[MB_KEMPTY + ks]);
         }
         if (!ok) *abort_flag = 1;
       }
     }
+    else {
+      // ------------------------------------------------------------------ what the columns see
+      // In two warps of their own, half of the columns each, all loads in flight together: in the
+      // summing warps, or one column after the other, the latency of these loads bounded the kernel.
+      constexpr int CPL = BQ / 64;
+      const int half = warp - 2;
+      int r_in[CPL], head_in[CPL];
+#pragma unroll
+      for (int x = 0; x < CPL; ++x) {
+        const int i = x * 64 + half * 32 + lane;
+        r_in[x] = i < BR * p.g ? i / p.g : 0x3fffffff;
+        head_in[x] = i % p.g;
+      }
+      bool ok = true;
+      int n = 0;
+      for (int item = item0; item < item1 && ok; item += step) {
+        const int h = item / key_items, k0 = (item % key_items) * (2 * BK);
+        for (int rt = rank; rt < row_tiles; rt += C, ++n) {
+          const int cb = n & 1;
+          float z[CPL];
+          int lo[CPL], hi[CPL];
+#pragma unroll
+          for (int x = 0; x < CPL; ++x) {
+            const int r = min(rt * BR + min(r_in[x], BR), p.R - 1);
+            z[x] = __ldg(p.lse + (int64_t)r * p.n_q + h * p.g + head_in[x]);
+            lo[x] = __ldg(p.k_lo + r);
+            hi[x] = __ldg(p.k_hi + r);
+          }
+          if (!tc::mbar_wait(&bar[MB_CEMPTY + cb], ((n >> 1) & 1) ^ 1, abort_flag)) { ok = false; break; }
+          bool masked[2] = {false, false};
+#pragma unroll
+          for (int x = 0; x < CPL; ++x) {
+            const int i = x * 64 + half * 32 + lane;
+            const bool real = r_in[x] < BR && rt * BR + r_in[x] < p.R;
+            lo[x] = max(lo[x], 0);
+            hi[x] = min(hi[x], p.T - 1);
+            const bool blind = !real || z[x] == -INFINITY || lo[x] > hi[x];     // such a row adds nothing
+            // a column of zeros behind the last row needs no mask: exp2(0 - inf) = 0
+#pragma unroll
+            for (int w = 0; w < 2; ++w)
+              masked[w] |= real && (blind || lo[x] > k0 + w * BK || hi[x] < min(k0 + (w + 1) * BK, p.T) - 1);
+            col_z[cb * BQ + i] = blind ? -INFINITY : -z[x] * LOG2E;
+            // seen <=> (unsigned)(key - first) <= length: never for a blind row (keys are not negative)
+            col_rng[cb * BQ + i] = blind ? make_int2(0x7fffffff, 0) : make_int2(lo[x], hi[x] - lo[x]);
+          }
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            const bool any = __any_sync(0xFFFFFFFFu, masked[w]);
+            if (lane == 0) flag[(cb * 2 + w) * 2 + half] = any;
+          }
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(&bar[MB_CFULL + cb]);
+        }
+      }
+      if (!ok && lane == 0) *abort_flag = 1;
+    }
   } else {
     // ---------------------------------------------------------------------- a key per thread
     asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
     const int w = (warp >> 2) - 1, m = threadIdx.x & 127, quad = warp & 3;
-    float* col_z = reinterpret_cast<float*>(smem + OFF_COL + w * M_COL_BYTES);        // [2][128] -lse in log2 units
-    int2* col_rng = reinterpret_cast<int2*>(col_z + 2 * 128);                         // [2][128] visible keys
-    volatile int* flag = reinterpret_cast<volatile int*>(smem + OFF_FLAG) + w * 8;    // [2][4] a column of the quad needs a mask
     const uint32_t lane_addr = tmem_base + ((uint32_t)(quad * 32) << 16);
     const float scale2 = p.scale * LOG2E;
     bool ok = true;
     int n = 0;
-    for (int item = first; item < n_items && ok; item += stride) {
-      const int h = item / key_items, k0 = (item % key_items) * (2 * BK) + w * BK, key = k0 + m;
-      const int k_last = min(k0 + BK, p.T) - 1;
-      float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int item = item0; item < item1 && ok; item += step) {
+      const int h = item / key_items, key = (item % key_items) * (2 * BK) + w * BK + m;
+      float2 acc[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
       for (int rt = rank; rt < row_tiles; rt += C, ++n) {
-        const int b = n & 1;
-        {
-          // this thread describes column m of the tile
-          const int r = rt * BR + m / p.g;
-          const bool real = m < BR * p.g && r < p.R;
-          float z = INFINITY;
-          int lo = 0x7fffffff, hi = -1;
-          if (real) {
-            z = __ldg(p.lse + (int64_t)r * p.n_q + h * p.g + m % p.g);
-            lo = __ldg(p.k_lo + r);
-            hi = __ldg(p.k_hi + r);
-            if (z == -INFINITY) { z = INFINITY; lo = 0x7fffffff; hi = -1; }    // a row that sees nothing adds nothing
-          }
-          // a column of zeros behind the last row needs no mask: exp2(0 - inf) = 0
-          const bool masked = real && !(lo <= k0 && hi >= k_last);
-          col_z[b * 128 + m] = -z * LOG2E;
-          col_rng[b * 128 + m] = make_int2(lo, hi);
-          const bool any = __any_sync(0xFFFFFFFFu, masked);
-          if (lane == 0) flag[b * 4 + quad] = any;
-        }
-        group_sync(w);
-        const bool mask = flag[b * 4] || flag[b * 4 + 1] || flag[b * 4 + 2] || flag[b * 4 + 3];
-        const int cols = min(BR, p.R - rt * BR) * p.g;
-        if (!tc::mbar_wait(&bar[MB_SFULL + 2 * w + b], (n >> 1) & 1, abort_flag)) { ok = false; break; }
+        const int b = n % NB, cb = n & 1;
+        const int all_cols = min(BR, p.R - rt * BR) * p.g;
+        if (!tc::mbar_wait(&bar[MB_CFULL + cb], (n >> 1) & 1, abort_flag)) { ok = false; break; }
+        const bool mask = (flag[(cb * 2 + w) * 2] | flag[(cb * 2 + w) * 2 + 1]) != 0;
+        if (!tc::mbar_wait(&bar[MB_SFULL + 2 * w + b], (n / NB) & 1, abort_flag)) { ok = false; break; }
         tc::fence_after_sync();
-        float t[BQ];
-        const uint32_t s_addr = lane_addr + (2 * w + b) * BQ;
+        // 64 columns at a time, the next ones on their way from tensor memory meanwhile
+        const uint32_t s_addr = lane_addr + w * 256 + b * BQ;
+        const int chunks = (all_cols + 63) / 64;
+        float ta[64], tb[64];
+        auto fetch = [&](float(&t)[64], int c) {
+          tc::tmem_ld32(s_addr + c * 64, *reinterpret_cast<float(*)[32]>(&t[0]));
+          tc::tmem_ld32(s_addr + c * 64 + 32, *reinterpret_cast<float(*)[32]>(&t[32]));
+        };
+        auto arrived = [&](int c) {
+          tc::tmem_ld_wait();
+          if (c + 1 == chunks) {                          // all of the tile is in registers: its buffer is free
+            tc::fence_before_sync();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(&bar[MB_SEMPTY + 2 * w + b]);
+          }
+        };
+        auto add = [&](const float(&t)[64], int c) {
+          const float* z = col_z + cb * BQ + c * 64;
+          const float2 sc = make_float2(scale2, scale2);
+          // no branch inside: the loads, exponentials and sums of different columns overlap
+          if (!mask) {
 #pragma unroll
-        for (int c = 0; c < BQ / 32; ++c) tc::tmem_ld32(s_addr + c * 32, *reinterpret_cast<float(*)[32]>(&t[c * 32]));
-        tc::tmem_ld_wait();
-        tc::fence_before_sync();
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&bar[MB_SEMPTY + 2 * w + b]);
+            for (int i = 0; i < 64; i += 4) {
+              const float4 zz = *reinterpret_cast<const float4*>(z + i);
+              const float2 x = __ffma2_rn(make_float2(t[i], t[i + 1]), sc, make_float2(zz.x, zz.y));
+              const float2 y = __ffma2_rn(make_float2(t[i + 2], t[i + 3]), sc, make_float2(zz.z, zz.w));
+              acc[(i >> 1) & 3] = __fadd2_rn(acc[(i >> 1) & 3], make_float2(ex2(x.x), ex2(x.y)));
+              acc[((i >> 1) + 1) & 3] = __fadd2_rn(acc[((i >> 1) + 1) & 3], make_float2(ex2(y.x), ex2(y.y)));
+            }
+          } else {
+            const int2* ranges = col_rng + cb * BQ + c * 64;
 #pragma unroll
-        for (int c = 0; c < BQ; c += 16) {
-          if (c < cols) {                                 // S^T behind the last 16 columns was not written
-#pragma unroll
-            for (int i = c; i < c + 16; ++i) {
-              float e = ex2(fmaf(t[i], scale2, col_z[b * 128 + i]));
-              if (mask) {
-                const int2 rng = col_rng[b * 128 + i];
-                e = rng.x <= key && key <= rng.y ? e : 0.f;
-              }
-              acc[i & 3] += e;
+            for (int i = 0; i < 64; i += 2) {
+              const float2 zz = *reinterpret_cast<const float2*>(z + i);
+              const int4 rng = *reinterpret_cast<const int4*>(ranges + i);
+              const float2 x = __ffma2_rn(make_float2(t[i], t[i + 1]), sc, zz);
+              const float e0 = ex2(x.x), e1 = ex2(x.y);
+              acc[(i >> 1) & 3] = __fadd2_rn(acc[(i >> 1) & 3], make_float2((unsigned)(key - rng.x) <= (unsigned)rng.y ? e0 : 0.f,
+                                                                          (unsigned)(key - rng.z) <= (unsigned)rng.w ? e1 : 0.f));
             }
           }
+        };
+        fetch(ta, 0);
+        for (int c = 0; c < chunks; c += 2) {
+          arrived(c);
+          if (c + 1 < chunks) fetch(tb, c + 1);
+          add(ta, c);
+          if (c + 1 >= chunks) break;
+          arrived(c + 1);
+          if (c + 2 < chunks) fetch(ta, c + 2);
+          add(tb, c + 1);
         }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&bar[MB_CEMPTY + cb]);
       }
       if (!ok) break;
-      const float sum = (acc[0] + acc[1]) + (acc[2] + acc[3]);
+      const float2 s01 = __fadd2_rn(acc[0], acc[1]), s23 = __fadd2_rn(acc[2], acc[3]);
+      const float sum = (s01.x + s01.y) + (s23.x + s23.y);
       const int64_t at = (int64_t)h * p.T + key;
       if (C == 1) {
         if (key < p.T) p.mass_out[at] = (p.mass_in ? p.mass_in[at] : 0.f) + sum;
@@ -238,7 +323,7 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     // a cluster has one item: its first CTA adds the parts in rank order
     tc::cluster_sync_all();
     if (rank == 0 && warp >= 4) {
-      const int w = (warp >> 2) - 1, m = threadIdx.x & 127, h = first / key_items, key = (first % key_items) * (2 * BK) + w * BK + m;
+      const int w = (warp >> 2) - 1, m = threadIdx.x & 127, h = item0 / key_items, key = (item0 % key_items) * (2 * BK) + w * BK + m;
       float sum = 0.f;
       for (int c = 0; c < C; ++c) {
         float x;
@@ -257,14 +342,20 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
   }
 }
 
-template <typename T, int HD>
+template <typename T, int HD, bool FEW>
 int32_t run_tc(const MassParams& p, cudaStream_t st) {
   static bool attr_set = false;
   if (!attr_set) {
-    AKVS_CUDA(cudaFuncSetAttribute(mass_tc_kernel<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, M_SMEM<HD>));
+    AKVS_CUDA(cudaFuncSetAttribute(mass_tc_kernel<T, HD, FEW>, cudaFuncAttributeMaxDynamicSharedMemorySize, M_SMEM<HD, FEW>));
     attr_set = true;
   }
-  const int BR = BQ / p.g;
+  // rows of a tile: 1 or 2 boxes whose rows fill whole groups of 8 (a swizzle atom), so that boxes lie back to back
+  int box_rows = 128 / p.g, q_boxes = FEW ? 1 : 2;
+  if (!FEW) {
+    while (box_rows > 1 && box_rows * p.g % 8) --box_rows;
+    if (box_rows * p.g % 8) { box_rows = 128 / p.g; q_boxes = 1; }
+  }
+  const int BR = box_rows * q_boxes;
   const int row_tiles = akvs_cdiv(p.R, BR), key_items = akvs_cdiv(p.T, 2 * BK);
   const int64_t n_items = (int64_t)key_items * p.n_kv;
   if (n_items > 0x7fffffff) return AKVS_ERR_TOO_LARGE;
@@ -272,14 +363,14 @@ int32_t run_tc(const MassParams& p, cudaStream_t st) {
   AKVS_TRY(make_tmap_2d_16bit(&tmK, p.k, p.T, (uint64_t)p.n_kv * HD, (uint64_t)p.k_ld, BK));
   // without rows there is no tile to load either; the map only has to be well formed
   AKVS_TRY(encode_tmap_3d_16bit(&tmQ, p.R > 0 ? p.q : p.k, HD, p.R > 0 ? p.n_q : p.n_kv, p.R > 0 ? p.R : p.T, HD,
-                                p.R > 0 ? p.q_ld : p.k_ld, p.g, BR));
+                                p.R > 0 ? p.q_ld : p.k_ld, p.g, box_rows));
   int C = 1;
   while (C < 8 && n_items * C * 2 <= 148 && row_tiles >= C * 4) C *= 2;
   const int64_t grid = C > 1 ? n_items * C : (n_items < 148 ? n_items : 148);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3(M_THREADS);
-  cfg.dynamicSmemBytes = M_SMEM<HD>;
+  cfg.dynamicSmemBytes = M_SMEM<HD, FEW>;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -290,10 +381,16 @@ int32_t run_tc(const MassParams& p, cudaStream_t st) {
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  AKVS_CUDA(cudaLaunchKernelEx(&cfg, mass_tc_kernel<T, HD>, tmK, tmQ, p, C, key_items, (int)n_items, BR,
+  AKVS_CUDA(cudaLaunchKernelEx(&cfg, mass_tc_kernel<T, HD, FEW>, tmK, tmQ, p, C, key_items, (int)n_items, BR, q_boxes,
                                std::is_same<T, f16>::value ? tc::kF16 : tc::kBF16));
   AKVS_LAUNCHED();
   return AKVS_OK;
+}
+
+template <typename T, int HD>
+int32_t run_tc(const MassParams& p, cudaStream_t st) {
+  // up to 128 stacked rows: one tile of whole rows
+  return (int64_t)akvs_cdiv(p.R, 128 / p.g) <= 1 ? run_tc<T, HD, true>(p, st) : run_tc<T, HD, false>(p, st);
 }
 
 // ---- CUDA cores: 64 keys per CTA, the stacked rows 64 at a time, 4 x 4 scores per thread.
