@@ -7,12 +7,15 @@
 //
 // 16-bit types run on the tensor cores with the keys along M, so that a thread owns one key and its
 // sum over the rows needs no shuffle; the score matrix never leaves tensor memory:
-//     S^T = K Q^T     tcgen05.mma, two tiles of 128 keys against one tile of up to 128 stacked rows
-//     sum            two warp groups, one per key tile: exp2 of a row of S^T, added up in registers
+//     S^T = K Q^T     tcgen05.mma, two tiles of 128 keys against one tile of up to 256 stacked rows
+//     sum             two warp groups, one per key tile: exp2 of a row of S^T, added up in registers
 // A CTA keeps 256 keys in shared memory while the rows' Q tiles stream past them (each is used
-// twice), then goes on to its next 256 keys.  The exponentials bound it: 16 per clock and SM, 2048
-// clocks for a tile of 256 keys x 128 rows, against 1050 of the MMAs.  With few rows it is bound by
-// reading K once.  Few keys and many rows: a cluster shares the row tiles of its keys and adds the
+// twice), then goes on to its next 256 keys.  Two warps work out what each column sees; a tile whose
+// columns all see its keys runs without a mask.  The exponentials bound it from below (16 per clock
+// and SM: 4096 clocks for 256 keys x 256 rows, 160 us of the 229 us that 512 rows x 40 heads x 32768
+// keys take); the rest is the MMA of a group's next tile, which waits for its only buffer.  With few
+// rows it is bound by reading K once (16 rows x 32 heads over 12416 keys: 8.9 us, 3.0 TB/s).
+// Few keys and many rows: a cluster shares the row tiles of its keys and adds the
 // partial sums through distributed shared memory.
 #include "tc_common.cuh"
 #include <math.h>
@@ -41,9 +44,8 @@ constexpr int M_SLAB = 128 * 128;    // 128 rows of 64 values
 // FEW: all stacked rows fit 128 columns.  One Q tile stays as long as the head does, K streams
 // through two stages and S^T has two buffers, so that items overlap.  Otherwise row tiles of 256
 // columns stream past one K item: an MMA of 256 columns reads its A operand from shared memory half
-// as often per column (with 128 columns the tensor pipe took 2.4x its rate's time and bounded the
-// kernel: 241 us for 512 rows x 40 heads x 32768 keys), and the loads of the next K hide
-// behind the sums of the last tile.
+// as often per column, and the load of the next K hides behind the sums of the last tile (512 rows
+// x 40 heads x 32768 keys: 229 us, against 238 us with two buffers of 128 columns).
 template <bool FEW> struct MassCfg {
   static constexpr int BQ = FEW ? 128 : 256, NB = FEW ? 2 : 1, KST = FEW ? 2 : 1, QST = FEW ? 1 : 2;
 };
