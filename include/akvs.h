@@ -356,9 +356,9 @@ int32_t akvs_op_qk_norm_rope(int32_t dtype, const void* q, int64_t q_ld, const v
  * backwards is empty; ranges must not overlap.  P = 0 or cap = 0 (then own_k, own_v and own_len
  * may be NULL) are allowed.  head_dim 64 or 128.
  * scratch: device, 256-byte aligned, akvs_op_attention_shared_scratch_bytes(...) bytes (else
- * AKVS_ERR_WORKSPACE; may be NULL when P = 0); two calls that may overlap on the GPU need two. */
-int64_t akvs_op_attention_shared_scratch_bytes(int32_t R, int32_t P, int32_t n_q_heads, int32_t n_kv_heads,
-                                               int32_t head_dim);
+ * AKVS_ERR_WORKSPACE); two calls that may overlap on the GPU need two. */
+int64_t akvs_op_attention_shared_scratch_bytes(int32_t dtype, int32_t R, int32_t P, int32_t S, int32_t cap,
+                                               int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim);
 int32_t akvs_op_attention_shared(int32_t dtype, const void* q, int64_t q_ld, int32_t R, const void* ctx_k,
                                  const void* ctx_v, int64_t ctx_ld, int32_t P, const void* own_k, const void* own_v,
                                  int64_t own_ld, int64_t own_seq_ld, int32_t S, int32_t cap, const int32_t* own_len,

@@ -79,7 +79,7 @@ def _load():
     P, I, L, F = C.c_void_p, C.c_int32, C.c_int64, C.c_float
     lib.akvs_op_qk_norm_rope.argtypes = [I, P, L, P, L, P, P, P, I, I, I, I, F, F, P, L, P, L, P]
     lib.akvs_op_attention_shared_scratch_bytes.restype = L
-    lib.akvs_op_attention_shared_scratch_bytes.argtypes = [I] * 5
+    lib.akvs_op_attention_shared_scratch_bytes.argtypes = [I] * 8
     lib.akvs_op_attention_shared.argtypes = [I, P, L, I, P, P, L, I, P, P, L, L, I, I, P, P, I, I, I, P, P, P, L, P]
     lib.akvs_op_attention_mass.argtypes = [I, P, L, P, L, P, P, P, I, I, I, I, I, P, P, P]
     lib.akvs_op_evict.argtypes = [I, P, P, P, L, L, I, I, I, I, I, I, I, P, P, P, P, P]
@@ -528,8 +528,8 @@ def op_qk_norm_rope(q, k, q_gain, k_gain, pos, eps, base, q_out=None, k_out=None
     return q_out, k_out
 
 
-def op_attention_shared_scratch(R, P, n_q, n_kv, hd, device="cuda"):
-    nbytes = lib.akvs_op_attention_shared_scratch_bytes(R, P, n_q, n_kv, hd)
+def op_attention_shared_scratch(dtype, R, P, S, cap, n_q, n_kv, hd, device="cuda"):
+    nbytes = lib.akvs_op_attention_shared_scratch_bytes(_CODE[dtype], R, P, S, cap, n_q, n_kv, hd)
     if nbytes < 0:
         _refuse("akvs_op_attention_shared_scratch_bytes")
     return alloc_workspace(nbytes, device)
@@ -568,7 +568,7 @@ def op_attention_shared(q, ctx_k, ctx_v, own_k, own_v, own_len, q_off=None, out=
             _refuse(w, -2)
         off = q_off.data_ptr()
     if scratch is None:
-        need = lib.akvs_op_attention_shared_scratch_bytes(R, P, nq, nkv, hd)
+        need = lib.akvs_op_attention_shared_scratch_bytes(_CODE[dt], R, P, S, cap, nq, nkv, hd)
         scratch = torch.empty(max(need, 0), dtype=torch.uint8, device=q.device)
     elif scratch.get_device() != dev or not scratch.is_contiguous():
         _refuse(w)

@@ -10,19 +10,20 @@
 //  1. The context is read once for all rows: the g = n_q / n_kv query heads of all R rows that
 //     share a kv head are stacked (row-major: r * g + i), and the key range is split over CTAs;
 //     each leaves (m, l, O) of its rows in scratch, in float.
-//  2. One cluster per (sequence, kv head) runs the sequence's own tokens, joins them with the
-//     context's parts and writes the rows.  The launch overlaps the first (it waits for it only
-//     before it reads the parts).
+//  2. A sequence's own tokens give further parts of the same form.  This launch needs nothing of
+//     the first and runs beside it, on SMs that it leaves idle.
+//  3. The parts of a row are joined and the row is written.
 //
 // Context, 16-bit types and more than one tile of 16 stacked rows: the tcgen05 attention kernel
 // (attn_tc.cu) on 128 stacked rows per CTA, so that K and V are read once for up to 128 of them.
-// The rest, and all own tokens, are memory bound with few rows: K and V go from global memory straight into the operand
-// registers of mma.sync m16n8k16, whose contraction index may be permuted at will (for Q K^T a
-// lane's 16-byte chunk of K and of Q supplies four of its k positions; for P V a lane's chunk
-// of V supplies one column of eight tiles), so no shared-memory staging stands between a load
-// and its use.  Probabilities enter P V as a 16-bit value and the 16-bit rounding of what it
-// lost: with one 16-bit value alone the rounding of P would cost the output as much accuracy
-// as its own final rounding.  Scores, maxima, sums and O are float.
+// The rest, and all own tokens, are memory bound with few rows, on mma.sync m16n8k16: a warp keeps a
+// tile of 16 stacked rows and streams keys through a cp.async ring of its own (16 keys a stage, two
+// stages in flight: 128 KB per SM).  The contraction index of an mma may be permuted at will, so a
+// lane's 16-byte chunk of K and of Q supplies four of its k positions in Q K^T, and in P V a lane's
+// chunk of V supplies one column of eight tiles: fragments are plain 16-byte loads.  Probabilities
+// enter P V as a 16-bit value and the 16-bit rounding of what it lost: with one 16-bit value alone
+// the rounding of P would cost the output as much accuracy as its own final rounding.  Scores,
+// maxima, sums and O are float.
 #include "tc_common.cuh"
 #include <math.h>
 
@@ -30,7 +31,8 @@ namespace {
 
 constexpr int DIR_WARPS = 4, DIR_THREADS = DIR_WARPS * 32;
 constexpr int MT = 16;                        // stacked rows of a tile (the M of one mma)
-constexpr int MAX_C = 8;                      // portable cluster size
+constexpr int ST = 3;                         // stages of a warp's ring
+constexpr int MAX_OWN_SPLITS = 64;
 constexpr float NO_MAX = -1.0e30f;            // running maximum before any key: exp2(x - NO_MAX) is never formed for x = -inf rows
 constexpr float LN2 = 0.69314718f, LOG2E = 1.4426950408889634f;
 
@@ -50,9 +52,10 @@ struct SharedParams {
   const int32_t* q_off;                       // null: row s belongs to sequence s
   void* out;
   float* lse;
-  float* part_o;                              // [splits][R * n_q][hd]
-  float2* part_ml;                            // [splits][R * n_q] (m in log2 units, l)
-  int splits, split_len;
+  float* part_o;                              // [splits + own_splits][R * n_q][hd]
+  float2* part_ml;                            // [splits + own_splits][R * n_q] (m in log2 units, l)
+  int splits, split_len;                      // of the context
+  int own_splits;                             // of every sequence's own tokens
   float scale_log2;                           // log2(e) / sqrt(hd)
 };
 
@@ -79,26 +82,55 @@ template <> __device__ __forceinline__ float2 unpack2<f16>(uint32_t w) {
   return __half22float2(*reinterpret_cast<const __half2*>(&w));
 }
 
-// Which stacked rows a tile holds and how many keys each of them sees.
+// Which stacked rows a tile holds.
 struct Tile {
-  int r0, j0, count;                          // first row, first stacked index, stacked rows in all
-  int h;                                      // kv head
-  int len, n;                                 // own tokens and rows of the sequence (own tokens only)
+  int r0, j0, count, h;                       // first row, first stacked index, stacked rows in all, kv head
   __device__ __forceinline__ bool valid(int m) const { return j0 + m < count; }
   __device__ __forceinline__ int row(int m, int g) const { return r0 + (j0 + m) / g; }
   __device__ __forceinline__ int head(int m, int g) const { return h * g + (j0 + m) % g; }
 };
 
-// floats between rows of a joined O: 16-byte rows that start in different banks
-template <int HD> constexpr int o_ld = HD + 4;
+// ---- 16-bit core of one warp: keys start, start + step, ... (16 at a time) below `end` of k/v (rows
+// `ld` apart); row m sees the keys below lim(m), all rows those below all_see.
+template <int HD> constexpr int STAGE = 16 * HD * 4;       // bytes: 16 rows of K, 16 rows of V
+template <int HD> struct WarpAcc {
+  float o[HD / 64][8][4];                     // rows gr and gr + 8; columns 64 c + 16 t + 8 e + i at [c][i][2 s + e]
+  float mx[2], sum[2];
+};
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool ok) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ uint4 lds16(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
 
-// ---- 16-bit core: keys [start, end) of k/v (rows `ld` apart); row m sees keys below lim(m).
-// Leaves O (unnormalised) in raw[16][HD + 4] and (m, l) in cm / cl.
 template <typename T, int HD, typename Lim>
-__device__ __forceinline__ void core(const SharedParams& p, const Tile& tl, const T* k, const T* v, int64_t ld, int start,
-                                     int end, int all_see, const Lim& lim, float* raw, float* cm, float* cl) {
-  constexpr int KC = HD / 32, VC = HD / 64;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gr = lane >> 2, t = lane & 3;
+__device__ __forceinline__ void warp_core(const SharedParams& p, const Tile& tl, const T* k, const T* v, int64_t ld, int start,
+                                          int end, int step, int all_see, const Lim& lim, uint32_t ring, WarpAcc<HD>& acc) {
+  constexpr int KC = HD / 32, VC = HD / 64, CH = HD / 8;    // 16-byte chunks of a row: CH
+  const int lane = threadIdx.x & 31, gr = lane >> 2, t = lane & 3;
+  // Places in a stage are exchanged so that the eight lanes of a shared-memory phase hit different
+  // banks: a K read takes 4 chunks of two neighbouring rows, a V read 2 chunks of four even rows.
+  auto issue = [&](int n) {
+    const int key0 = start + n * step;
+    if (key0 < end) {
+      const uint32_t base = ring + (n % ST) * STAGE<HD>;
+#pragma unroll
+      for (int i = 0; i < 16 * CH / 32; ++i) {
+        const int row = (i * 32 + lane) / CH, c = (i * 32 + lane) % CH;
+        const bool ok = key0 + row < end;
+        // rows behind the end may hold anything, NaN included, and 0 * NaN is not 0: they arrive as zeros
+        const int64_t at = (int64_t)(ok ? key0 + row : end - 1) * ld + c * 8;
+        cp16(base + (row * CH + (c ^ ((row & 1) << 2))) * 16, k + at, ok);
+        cp16(base + STAGE<HD> / 2 + (row * CH + (c ^ (row & 6))) * 16, v + at, ok);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int n = 0; n < ST - 1; ++n) issue(n);
   uint32_t qa[2][KC][4];
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
@@ -112,40 +144,34 @@ __device__ __forceinline__ void core(const SharedParams& p, const Tile& tl, cons
     }
   }
   const int limit[2] = {min(lim(gr), end), min(lim(gr + 8), end)};
-  float o[VC][8][4];
+  auto& o = acc.o;
+  auto& mx = acc.mx;
+  auto& sum = acc.sum;
 #pragma unroll
   for (int a = 0; a < VC; ++a)
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[a][i][e] = 0.f;
-  float mx[2] = {NO_MAX, NO_MAX}, sum[2] = {0.f, 0.f};
+  mx[0] = mx[1] = NO_MAX;
+  sum[0] = sum[1] = 0.f;
 
-  for (int key0 = start + warp * 16; key0 < end; key0 += DIR_WARPS * 16) {
-    uint4 kr[2][KC], vr[4][VC];
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      const T* kp = k + (int64_t)min(key0 + hf * 8 + gr, end - 1) * ld + 8 * t;
-#pragma unroll
-      for (int c = 0; c < KC; ++c) kr[hf][c] = __ldcg(reinterpret_cast<const uint4*>(kp + 32 * c));
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int key = key0 + 2 * t + (i & 1) + (i >> 1) * 8;
-      const T* vp = v + (int64_t)min(key, end - 1) * ld + 8 * gr;
-      // rows behind the end may hold anything, NaN included, and 0 * NaN is not 0
-#pragma unroll
-      for (int c = 0; c < VC; ++c)
-        vr[i][c] = key < end ? __ldcg(reinterpret_cast<const uint4*>(vp + 64 * c)) : make_uint4(0u, 0u, 0u, 0u);
-    }
+  int n = 0;
+  for (int key0 = start; key0 < end; key0 += step, ++n) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(ST - 2) : "memory");
+    __syncwarp();                                   // every lane's copies are there, and the stage before is read
+    issue(n + ST - 1);
+    const uint32_t ks = ring + (n % ST) * STAGE<HD>, vs = ks + STAGE<HD> / 2;
     float sc[2][4];
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
       sc[hf][0] = sc[hf][1] = sc[hf][2] = sc[hf][3] = 0.f;
+      const int row = hf * 8 + gr;
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
-        mma16816<T>(sc[hf], qa[0][c][0], qa[1][c][0], qa[0][c][1], qa[1][c][1], kr[hf][c].x, kr[hf][c].y);
-        mma16816<T>(sc[hf], qa[0][c][2], qa[1][c][2], qa[0][c][3], qa[1][c][3], kr[hf][c].z, kr[hf][c].w);
+        const uint4 x = lds16(ks + (row * CH + ((4 * c + t) ^ ((row & 1) << 2))) * 16);
+        mma16816<T>(sc[hf], qa[0][c][0], qa[1][c][0], qa[0][c][1], qa[1][c][1], x.x, x.y);
+        mma16816<T>(sc[hf], qa[0][c][2], qa[1][c][2], qa[0][c][3], qa[1][c][3], x.z, x.w);
       }
     }
     const bool every = key0 + 16 <= all_see;        // all rows see all 16 keys
@@ -192,10 +218,13 @@ __device__ __forceinline__ void core(const SharedParams& p, const Tile& tl, cons
       }
 #pragma unroll
       for (int c = 0; c < VC; ++c) {
-        const uint32_t w[4][4] = {{vr[0][c].x, vr[0][c].y, vr[0][c].z, vr[0][c].w},
-                                  {vr[1][c].x, vr[1][c].y, vr[1][c].z, vr[1][c].w},
-                                  {vr[2][c].x, vr[2][c].y, vr[2][c].z, vr[2][c].w},
-                                  {vr[3][c].x, vr[3][c].y, vr[3][c].z, vr[3][c].w}};
+        uint32_t w[4][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int row = 2 * t + (i & 1) + (i >> 1) * 8;
+          const uint4 x = lds16(vs + (row * CH + ((8 * c + gr) ^ (row & 6))) * 16);
+          w[i][0] = x.x; w[i][1] = x.y; w[i][2] = x.z; w[i][3] = x.w;
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const uint32_t sel = (i & 1) ? 0x7632u : 0x5410u;
@@ -217,13 +246,12 @@ __device__ __forceinline__ void core(const SharedParams& p, const Tile& tl, cons
         float pb = e == 0 ? pr[1][0] : e == 1 ? pr[1][1] : e == 2 ? pr[1][2] : pr[1][3];
         pa = __shfl_sync(0xFFFFFFFFu, pa, src);
         pb = __shfl_sync(0xFFFFFFFFu, pb, src);
-        const T* vp = v + (int64_t)key * ld + 16 * t;
 #pragma unroll
         for (int c = 0; c < VC; ++c) {
           float x[2][8];
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
-            const uint4 w = __ldcg(reinterpret_cast<const uint4*>(vp + 64 * c + 8 * b));
+            const uint4 w = lds16(vs + (kk * CH + ((8 * c + 2 * t + b) ^ (kk & 6))) * 16);
             const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -243,61 +271,86 @@ __device__ __forceinline__ void core(const SharedParams& p, const Tile& tl, cons
       }
     }
   }
-  // join the warps
-  __shared__ float wm[DIR_WARPS][MT], wl[DIR_WARPS][MT];
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     sum[s] += __shfl_xor_sync(0xFFFFFFFFu, sum[s], 1);
     sum[s] += __shfl_xor_sync(0xFFFFFFFFu, sum[s], 2);
-    if (t == 0) { wm[warp][gr + 8 * s] = mx[s]; wl[warp][gr + 8 * s] = sum[s]; }
   }
-  __syncthreads();
+}
+
+// Row m's part into scratch, from a row of O in shared memory.
+template <int HD>
+__device__ __forceinline__ void store_part(const SharedParams& p, const Tile& tl, int part, int m, int c4, float4 o) {
+  const int64_t row = (int64_t)part * p.R * p.n_q + (int64_t)tl.row(m, p.g) * p.n_q + tl.head(m, p.g);
+  *reinterpret_cast<float4*>(p.part_o + row * HD + c4) = o;
+}
+__device__ __forceinline__ void store_ml(const SharedParams& p, const Tile& tl, int part, int m, float mx, float l) {
+  p.part_ml[(int64_t)part * p.R * p.n_q + (int64_t)tl.row(m, p.g) * p.n_q + tl.head(m, p.g)] = make_float2(mx, l);
+}
+
+// One tile, the CTA's warps taking turns over its keys; joins them and leaves the part in scratch.
+template <typename T, int HD, typename Lim>
+__device__ __forceinline__ void cta_part(const SharedParams& p, const Tile& tl, const T* k, const T* v, int64_t ld, int start,
+                                         int end, int all_see, const Lim& lim, uint8_t* smem, int part) {
+  __shared__ float wm[DIR_WARPS][MT], wl[DIR_WARPS][MT];
+  constexpr int LD = HD + 4;                  // 16-byte rows that start in different banks
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gr = lane >> 2, t = lane & 3;
+  float* raw = reinterpret_cast<float*>(smem);
+  WarpAcc<HD> acc;
+  warp_core<T, HD>(p, tl, k, v, ld, start + warp * 16, end, DIR_WARPS * 16, all_see, lim,
+                   tc::smem_u32(smem) + warp * ST * STAGE<HD>, acc);
+  if (t == 0)
+#pragma unroll
+    for (int s = 0; s < 2; ++s) { wm[warp][gr + 8 * s] = acc.mx[s]; wl[warp][gr + 8 * s] = acc.sum[s]; }
+  __syncthreads();                            // the rings become the warps' rows of O
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     const int m = gr + 8 * s;
     float top = wm[0][m];
 #pragma unroll
     for (int w = 1; w < DIR_WARPS; ++w) top = fmaxf(top, wm[w][m]);
-    const float f = ex2(mx[s] - top);
-    float* dst = raw + (warp * MT + m) * o_ld<HD> + 16 * t;
+    const float f = ex2(acc.mx[s] - top);
+    float* dst = raw + (warp * MT + m) * LD + 16 * t;
 #pragma unroll
-    for (int c = 0; c < VC; ++c)
+    for (int c = 0; c < HD / 64; ++c)
 #pragma unroll
       for (int i = 0; i < 8; i += 4)
 #pragma unroll
         for (int e = 0; e < 2; ++e)
           *reinterpret_cast<float4*>(dst + 64 * c + 8 * e + i) =
-              make_float4(o[c][i][2 * s + e] * f, o[c][i + 1][2 * s + e] * f, o[c][i + 2][2 * s + e] * f, o[c][i + 3][2 * s + e] * f);
+              make_float4(acc.o[c][i][2 * s + e] * f, acc.o[c][i + 1][2 * s + e] * f, acc.o[c][i + 2][2 * s + e] * f,
+                          acc.o[c][i + 3][2 * s + e] * f);
   }
   __syncthreads();
   for (int i = threadIdx.x; i < MT * HD / 4; i += DIR_THREADS) {
-    float4* at = reinterpret_cast<float4*>(raw + (i / (HD / 4)) * o_ld<HD> + i % (HD / 4) * 4);
-    float4 a = *at;
+    const int m = i / (HD / 4), c4 = i % (HD / 4) * 4;
+    if (!tl.valid(m)) continue;
+    float4 a = *reinterpret_cast<const float4*>(raw + m * LD + c4);
 #pragma unroll
     for (int w = 1; w < DIR_WARPS; ++w) {
-      const float4 b = *reinterpret_cast<float4*>(reinterpret_cast<float*>(at) + w * MT * o_ld<HD>);
+      const float4 b = *reinterpret_cast<const float4*>(raw + (w * MT + m) * LD + c4);
       a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
     }
-    *at = a;
+    store_part<HD>(p, tl, part, m, c4, a);
   }
-  if (threadIdx.x < MT) {
+  if (threadIdx.x < MT && tl.valid(threadIdx.x)) {
     const int m = threadIdx.x;
     float top = wm[0][m], l = 0.f;
     for (int w = 1; w < DIR_WARPS; ++w) top = fmaxf(top, wm[w][m]);
     for (int w = 0; w < DIR_WARPS; ++w) l += wl[w][m] * ex2(wm[w][m] - top);
-    cm[m] = top;
-    cl[m] = l;
+    store_ml(p, tl, part, m, top, l);
   }
-  __syncthreads();
+  __syncthreads();                            // before another tile reuses the shared memory
 }
 
 // ---- float core: the same on the CUDA cores, 32 keys at a time through shared memory.
 constexpr int FK = 32;
 template <int HD, typename Lim>
-__device__ __forceinline__ void core_f32(const SharedParams& p, const Tile& tl, const float* k, const float* v, int64_t ld,
-                                         int start, int end, const Lim& lim, float* raw, float* cm, float* cl) {
+__device__ __forceinline__ void cta_part_f32(const SharedParams& p, const Tile& tl, const float* k, const float* v, int64_t ld,
+                                             int start, int end, const Lim& lim, uint8_t* smem, int part) {
   constexpr int LD = HD + 4, OC = HD / 32;
-  float* kt = raw;                            // [FK][LD]
+  float* kt = reinterpret_cast<float*>(smem); // [FK][LD]
   float* vt = kt + FK * LD;                   // [FK][LD]
   float* qt = vt + FK * LD;                   // [MT][LD]
   float* pt = qt + MT * LD;                   // [MT][FK + 1]
@@ -374,158 +427,201 @@ __device__ __forceinline__ void core_f32(const SharedParams& p, const Tile& tl, 
   }
 #pragma unroll
   for (int s = 4; s > 0; s >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, s);
-  __syncthreads();                            // the key tile becomes the output tile
+  if (tl.valid(m)) {
 #pragma unroll
-  for (int c = 0; c < OC; ++c) *reinterpret_cast<float4*>(raw + m * LD + 32 * c + 4 * e) = o[c];
-  if (e == 0) { cm[m] = mx; cl[m] = sum; }
-  __syncthreads();
+    for (int c = 0; c < OC; ++c) store_part<HD>(p, tl, part, m, 32 * c + 4 * e, o[c]);
+    if (e == 0) store_ml(p, tl, part, m, mx, sum);
+  }
+  __syncthreads();                            // before another tile reuses the shared memory
 }
 
 template <typename T, int HD> constexpr int direct_smem() {
-  return std::is_same<T, float>::value ? (2 * FK * (HD + 4) + MT * (HD + 4) + MT * (FK + 1)) * 4
-                                       : DIR_WARPS * MT * (HD + 4) * 4;
+  return std::is_same<T, float>::value ? (2 * FK * (HD + 4) + MT * (HD + 4) + MT * (FK + 1)) * 4 : DIR_WARPS * ST * STAGE<HD>;
 }
 
 template <typename T, int HD, typename Lim>
-__device__ __forceinline__ void run_core(const SharedParams& p, const Tile& tl, const void* k, const void* v, int64_t ld,
-                                         int start, int end, int all_see, const Lim& lim, float* raw, float* cm, float* cl) {
+__device__ __forceinline__ void tile_part(const SharedParams& p, const Tile& tl, const T* k, const T* v, int64_t ld, int start,
+                                          int end, int all_see, const Lim& lim, uint8_t* smem, int part) {
   if constexpr (std::is_same<T, float>::value)
-    core_f32<HD>(p, tl, (const float*)k, (const float*)v, ld, start, end, lim, raw, cm, cl);
+    cta_part_f32<HD>(p, tl, k, v, ld, start, end, lim, smem, part);
   else
-    core<T, HD>(p, tl, (const T*)k, (const T*)v, ld, start, end, all_see, lim, raw, cm, cl);
+    cta_part<T, HD>(p, tl, k, v, ld, start, end, all_see, lim, smem, part);
 }
 
 // ---- 1. context: grid (split, kv head, tile of 16 stacked rows)
 template <typename T, int HD>
 __global__ void __launch_bounds__(DIR_THREADS)
 context_direct_kernel(const __grid_constant__ SharedParams p) {
-  extern __shared__ __align__(16) float raw[];
-  __shared__ float cm[MT], cl[MT];
+  extern __shared__ __align__(16) uint8_t smem[];
   pdl_wait();
-  pdl_trigger();                              // after the wait: see own_join_kernel
+  pdl_trigger();                              // after the wait: see own_kernel
   const int split = blockIdx.x, h = blockIdx.y;
-  const Tile tl{0, (int)blockIdx.z * MT, p.R * p.g, h, 0, 0};
+  const Tile tl{0, (int)blockIdx.z * MT, p.R * p.g, h};
   const int start = split * p.split_len, end = min(start + p.split_len, p.P);
-  run_core<T, HD>(p, tl, (const T*)p.pk + (int64_t)h * HD, (const T*)p.pv + (int64_t)h * HD, p.p_ld, start, end, end,
-                  [&](int) { return end; }, raw, cm, cl);
-  const int64_t rows = (int64_t)p.R * p.n_q;
-  for (int i = threadIdx.x; i < MT * HD / 4; i += DIR_THREADS) {
-    const int m = i / (HD / 4), c = i % (HD / 4) * 4;
-    if (tl.valid(m))
-      *reinterpret_cast<float4*>(p.part_o + ((int64_t)split * rows + (int64_t)tl.row(m, p.g) * p.n_q + tl.head(m, p.g)) * HD + c) =
-          *reinterpret_cast<const float4*>(raw + m * o_ld<HD> + c);
+  tile_part<T, HD>(p, tl, (const T*)p.pk + (int64_t)h * HD, (const T*)p.pv + (int64_t)h * HD, p.p_ld, start, end, end,
+                   [&](int) { return end; }, smem, split);
+}
+
+// The rows of sequence s and how many of its tokens are filled.
+struct Seq { int r0, n, len; };
+__device__ __forceinline__ Seq sequence(const SharedParams& p, int s) {
+  Seq q;
+  int r1 = s + 1;
+  q.r0 = s;
+  if (p.q_off) {
+    q.r0 = min(max(__ldcg(p.q_off + s), 0), p.R);
+    r1 = min(max(__ldcg(p.q_off + s + 1), q.r0), p.R);
   }
-  if (threadIdx.x < MT && tl.valid(threadIdx.x))
-    p.part_ml[(int64_t)split * rows + (int64_t)tl.row(threadIdx.x, p.g) * p.n_q + tl.head(threadIdx.x, p.g)] =
-        make_float2(cm[threadIdx.x], cl[threadIdx.x]);
+  q.n = r1 - q.r0;
+  q.len = p.cap > 0 ? min(max(__ldcg(p.s_len + s), 0), p.cap) : 0;
+  return q;
 }
 
-__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-  return v;
-}
-__device__ __forceinline__ float ld_cluster1(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-  return v;
-}
-__device__ __forceinline__ void add_scaled(float4& a, const float4& b, float f) {
-  a.x = fmaf(b.x, f, a.x); a.y = fmaf(b.y, f, a.y); a.z = fmaf(b.z, f, a.z); a.w = fmaf(b.w, f, a.w);
-}
-
-// ---- 2. own tokens and the join: cluster of C CTAs per (sequence, kv head), the own tokens split
-// over the cluster; CTA c joins the rows m = c mod C of each tile.  grid (S * C, n_kv, tiles in flight)
-template <typename T, int HD>
+// ---- 2. own tokens: grid (sequence * own split, kv head, tiles in flight).
+// WIDE (sequences of many rows, one split): every warp has a tile of its own and runs all its keys.
+template <typename T, int HD, bool WIDE>
 __global__ void __launch_bounds__(DIR_THREADS)
-own_join_kernel(const __grid_constant__ SharedParams p, int C) {
-  extern __shared__ __align__(16) float raw[];
-  __shared__ __align__(16) float cm[MT], cl[MT];
-  pdl_trigger();
-  const int s = blockIdx.x / C, rank = blockIdx.x % C, h = blockIdx.y;
+own_kernel(const __grid_constant__ SharedParams p) {
+  extern __shared__ __align__(16) uint8_t smem[];
   // A CTA of this kernel starts once every CTA of the context's kernel has passed its own wait, so
   // q, the own tokens, lengths and offsets (older than that kernel) are complete in L2 and are read
-  // there; only the parts, which that kernel writes, need a wait of this one.  Without a context
-  // the kernel before is a stranger: wait for it first.
+  // there.  Without a context the kernel before is a stranger: wait for it first.
   if (p.splits == 0) pdl_wait();
-  int r0 = s, r1 = s + 1;
-  if (p.q_off) {
-    r0 = min(max(__ldcg(p.q_off + s), 0), p.R);
-    r1 = min(max(__ldcg(p.q_off + s + 1), r0), p.R);
-  }
-  const int n = r1 - r0;
-  const int len = p.cap > 0 ? min(max(__ldcg(p.s_len + s), 0), p.cap) : 0;
-  const int64_t rows = (int64_t)p.R * p.n_q;
+  pdl_trigger();
+  const int s = blockIdx.x / p.own_splits, split = blockIdx.x % p.own_splits, h = blockIdx.y;
+  const Seq sq = sequence(p, s);
   const T* k = (const T*)p.sk + (int64_t)s * p.s_seq + (int64_t)h * HD;
   const T* v = (const T*)p.sv + (int64_t)s * p.s_seq + (int64_t)h * HD;
+  const int count = sq.n * p.g;
+  constexpr int TILES = WIDE ? DIR_WARPS : 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr int LPR = HD / 4, RPW = 32 / LPR;       // lanes of a row, rows a warp joins at a time
-  for (int j0 = blockIdx.z * MT; j0 < n * p.g; j0 += gridDim.z * MT) {
-    const Tile tl{r0, j0, n * p.g, h, len, n};
+  for (int j0 = (blockIdx.z * TILES + (WIDE ? warp : 0)) * MT; j0 < count; j0 += gridDim.z * TILES * MT) {
+    const Tile tl{sq.r0, j0, count, h};
     // row i of the sequence sees len - (n - 1 - i) own tokens: the tile's first row the fewest
-    auto lim = [&](int m) { return tl.valid(m) ? len - (n - 1 - (j0 + m) / p.g) : len; };
-    const int most = max(0, lim(min(MT, n * p.g - j0) - 1)), fewest = max(0, lim(0));
-    const int chunk = (((most + C - 1) / C + 63) / 64) * 64;
-    const int start = min(rank * chunk, most), end = min(start + chunk, most);
-    run_core<T, HD>(p, tl, k, v, p.s_ld, start, end, min(fewest, end), lim, raw, cm, cl);
-    pdl_wait();
-    if (C > 1) tc::cluster_sync_all();
-    for (int m0 = rank + warp * RPW * C; m0 < MT; m0 += DIR_WARPS * RPW * C) {
-      const int m = m0 + (lane / LPR) * C;
-      const bool ok = m < MT && tl.valid(m);
-      const int c4 = (lane % LPR) * 4;
-      const int64_t at = ok ? (int64_t)tl.row(m, p.g) * p.n_q + tl.head(m, p.g) : 0;
-      const int mm = ok ? m : 0;
-      float top = NO_MAX;
-      for (int c = 0; c < C; ++c) top = fmaxf(top, C > 1 ? ld_cluster1(tc::map_to_rank(tc::smem_u32(&cm[mm]), c)) : cm[mm]);
-      if (ok)
-        for (int i = 0; i < p.splits; ++i) top = fmaxf(top, __ldcg(p.part_ml + i * rows + at).x);
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-      float l = 0.f;
-      for (int c = 0; c < C; ++c) {
-        if (C > 1) {
-          const float f = ex2(ld_cluster1(tc::map_to_rank(tc::smem_u32(&cm[mm]), c)) - top);
-          l += f * ld_cluster1(tc::map_to_rank(tc::smem_u32(&cl[mm]), c));
-          add_scaled(o, ld_cluster4(tc::map_to_rank(tc::smem_u32(raw + mm * o_ld<HD> + c4), c)), f);
-        } else {
-          const float f = ex2(cm[mm] - top);
-          l += f * cl[mm];
-          add_scaled(o, *reinterpret_cast<const float4*>(raw + mm * o_ld<HD> + c4), f);
-        }
+    auto lim = [&](int m) { return tl.valid(m) ? sq.len - (sq.n - 1 - (j0 + m) / p.g) : sq.len; };
+    const int most = max(0, lim(min(MT, count - j0) - 1)), fewest = max(0, lim(0));
+    if constexpr (WIDE) {
+      WarpAcc<HD> acc;
+      warp_core<T, HD>(p, tl, k, v, p.s_ld, 0, most, 16, min(fewest, most), lim, tc::smem_u32(smem) + warp * ST * STAGE<HD>, acc);
+      const int gr = lane >> 2, t = lane & 3;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int m = gr + 8 * x;
+        if (!tl.valid(m)) continue;
+#pragma unroll
+        for (int c = 0; c < HD / 64; ++c)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int i = 0; i < 8; i += 4)
+              store_part<HD>(p, tl, p.splits, m, 64 * c + 16 * t + 8 * e + i,
+                             make_float4(acc.o[c][i][2 * x + e], acc.o[c][i + 1][2 * x + e], acc.o[c][i + 2][2 * x + e],
+                                         acc.o[c][i + 3][2 * x + e]));
+        if (t == 0) store_ml(p, tl, p.splits, m, acc.mx[x], acc.sum[x]);
       }
-      if (ok) {
-#pragma unroll 4
-        for (int i = 0; i < p.splits; ++i) {
-          const float2 ml = __ldcg(p.part_ml + i * rows + at);
-          const float f = ex2(ml.x - top);
-          l = fmaf(f, ml.y, l);
-          add_scaled(o, __ldcg(reinterpret_cast<const float4*>(p.part_o + (i * rows + at) * HD + c4)), f);
-        }
-        const float inv = l == 0.f ? 0.f : 1.f / l;          // nothing visible: zeros, lse = -inf
-        T* dst = reinterpret_cast<T*>(p.out) + at * HD + c4;
-        if constexpr (sizeof(T) == 4) {
-          *reinterpret_cast<float4*>(dst) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-        } else {
-          uint2 w;
-          w.x = pack2<T>(o.x * inv, o.y * inv);
-          w.y = pack2<T>(o.z * inv, o.w * inv);
-          *reinterpret_cast<uint2*>(dst) = w;
-        }
-        if (c4 == 0) p.lse[at] = l == 0.f ? -INFINITY : (top + log2f(l)) * LN2;
-      }
+      __syncwarp();
+    } else {
+      const int chunk = ((most + p.own_splits - 1) / p.own_splits + 63) / 64 * 64;
+      const int start = min(split * chunk, most), end = min(start + chunk, most);
+      tile_part<T, HD>(p, tl, k, v, p.s_ld, start, end, min(fewest, end), lim, smem, p.splits + split);
     }
-    if (C > 1) tc::cluster_sync_all();              // the tile's parts stay until the cluster has read them
-    else __syncthreads();
   }
-  pdl_wait();                                       // a CTA without rows, too: the next kernel relies on it
+  // The join waits for this grid alone: its last CTA ends after the context's kernel.
+  if (blockIdx.x == gridDim.x - 1 && blockIdx.y == gridDim.y - 1 && blockIdx.z == gridDim.z - 1) pdl_wait();
 }
 
-struct Plan { bool tc; int splits, split_len; };
+// ---- 3. join: WPR warps per row, which share its parts.  grid (sequence, kv head, rows in flight)
+template <typename T, int HD, int WPR>
+__global__ void __launch_bounds__(DIR_THREADS)
+join_kernel(const __grid_constant__ SharedParams p) {
+  constexpr int V = HD / 32, RPC = DIR_WARPS / WPR, UN = 8;    // values of a lane, rows of a CTA, parts in flight
+  __shared__ float jo[DIR_WARPS][HD], jm[DIR_WARPS], jl[DIR_WARPS];
+  pdl_trigger();
+  const int s = blockIdx.x, h = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % WPR;
+  const Seq sq = sequence(p, s);              // older than the kernels before, which have started: no wait
+  pdl_wait();
+  const int parts = p.splits + p.own_splits, mine = parts > sub ? (parts - sub + WPR - 1) / WPR : 0;
+  const int64_t rows = (int64_t)p.R * p.n_q;
+  const int count = sq.n * p.g;
+  for (int j0 = blockIdx.z * RPC; j0 < count; j0 += gridDim.z * RPC) {
+    const int j = j0 + warp / WPR;
+    const bool ok = j < count;
+    const int64_t at = (int64_t)(sq.r0 + (ok ? j : 0) / p.g) * p.n_q + h * p.g + (ok ? j : 0) % p.g;
+    float mx = NO_MAX, l = 0.f, o[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = 0.f;
+    for (int b = 0; b < mine; b += 32) {
+      const bool have = b + lane < mine;
+      const float2 ml = have ? __ldcg(p.part_ml + (int64_t)(sub + (b + lane) * WPR) * rows + at) : make_float2(NO_MAX, 0.f);
+      const float top = fmaxf(mx, warp_max(ml.x));
+      const float w = have ? ex2(ml.x - top) : 0.f, f = ex2(mx - top);
+      l = l * f + warp_sum(w * ml.y);
+#pragma unroll
+      for (int i = 0; i < V; ++i) o[i] *= f;
+      mx = top;
+      const int n = min(32, mine - b);
+      for (int c = 0; c < n; c += UN) {
+        float x[UN][V];
+#pragma unroll
+        for (int u = 0; u < UN; ++u) {
+          // a part without a key (weight times zeros) is read like the others; beyond the last one nothing is
+          const float* src = p.part_o + ((int64_t)(sub + (b + min(c + u, n - 1)) * WPR) * rows + at) * HD + lane * V;
+          if constexpr (V == 4) {
+            const float4 y = __ldcg(reinterpret_cast<const float4*>(src));
+            x[u][0] = y.x; x[u][1] = y.y; x[u][2] = y.z; x[u][3] = y.w;
+          } else {
+            const float2 y = __ldcg(reinterpret_cast<const float2*>(src));
+            x[u][0] = y.x; x[u][1] = y.y;
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < UN; ++u) {
+          const float wu = __shfl_sync(0xFFFFFFFFu, w, min(c + u, 31));
+          if (c + u < n)
+#pragma unroll
+            for (int i = 0; i < V; ++i) o[i] = fmaf(wu, x[u][i], o[i]);
+        }
+      }
+    }
+    if constexpr (WPR > 1) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) jo[warp][lane * V + i] = o[i];
+      if (lane == 0) { jm[warp] = mx; jl[warp] = l; }
+      __syncthreads();
+      if (sub == 0) {
+#pragma unroll
+        for (int w = 1; w < WPR; ++w) {
+          const float top = fmaxf(mx, jm[warp + w]), f = ex2(mx - top), e = ex2(jm[warp + w] - top);
+          l = l * f + jl[warp + w] * e;
+#pragma unroll
+          for (int i = 0; i < V; ++i) o[i] = o[i] * f + jo[warp + w][lane * V + i] * e;
+          mx = top;
+        }
+      }
+      __syncthreads();
+    }
+    if (ok && sub == 0) {
+      const float inv = l == 0.f ? 0.f : 1.f / l;              // nothing visible: zeros, lse = -inf
+      T* dst = reinterpret_cast<T*>(p.out) + at * HD + lane * V;
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) dst[i] = o[i] * inv;
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = pack2<T>(o[i] * inv, o[i + 1] * inv);
+      }
+      if (lane == 0) p.lse[at] = l == 0.f ? -INFINITY : (mx + log2f(l)) * LN2;
+    }
+  }
+}
 
-// How the context is cut.
-Plan plan_context(bool is16, int R, int P, int g, int n_kv, int hd) {
-  if (P == 0 || R == 0) return {false, 0, 0};
-  if (is16 && (int64_t)R * g > MT) {
+struct Plan { bool tc; int splits, split_len, own_splits; bool wide; int z; };
+
+// How the context and the own tokens are cut.
+Plan make_plan(bool is16, int R, int P, int S, int cap, int g, int n_kv, int hd, bool ragged) {
+  Plan pl = {false, 0, 0, 0, false, 1};
+  if (R == 0 || S == 0) return pl;
+  if (P > 0 && is16 && (int64_t)R * g > MT) {
     // One CTA per SM.  In units of a key tile: rounds of CTAs times (a CTA's tiles + 6 for its start
     // and end), plus writing and reading the parts at memory speed (a tile takes about 0.7 us).
     const int64_t base = (int64_t)akvs_cdiv(R, 128 / g) * n_kv;
@@ -537,28 +633,50 @@ Plan plan_context(bool is16, int R, int P, int g, int n_kv, int hd) {
       const double cost = (double)((base * s + 147) / 148) * (akvs_cdiv(tiles, s) + 6) + part * s;
       if (cost < best_cost) { best_cost = cost; best = s; }
     }
-    const int len = akvs_cdiv(tiles, best) * 128;
-    return {true, akvs_cdiv(P, len), len};
+    pl.tc = true;
+    pl.split_len = akvs_cdiv(tiles, best) * 128;
+  } else if (P > 0) {
+    // Two CTAs fit an SM; one runs 64 keys at a time (32 of the float kernel).
+    const int unit = is16 ? 64 : 32;
+    const int64_t base = (int64_t)n_kv * akvs_cdiv((int64_t)R * g, MT);
+    const int units = akvs_cdiv(P, unit);
+    const int splits = (int)(base >= 296 ? 1 : akvs_cdiv(296, base));
+    pl.split_len = akvs_cdiv(units, splits < units ? splits : units) * unit;
   }
-  // A CTA runs 64 keys at a time; two CTAs fit an SM.
-  const int64_t base = (int64_t)n_kv * akvs_cdiv((int64_t)R * g, MT);
-  int splits = (int)(base >= 296 ? 1 : akvs_cdiv(296, base));
-  const int most = akvs_cdiv(P, 128);
-  if (splits > most) splits = most;
-  const int len = akvs_cdiv(akvs_cdiv(P, splits), 64) * 64;
-  return {false, akvs_cdiv(P, len), len};
+  if (P > 0) pl.splits = akvs_cdiv(P, pl.split_len);
+  // Stacked rows of a sequence: g, or the mean of a ragged batch.  Ragged batches get room for twice
+  // the mean at once, and a CTA walks what is left.
+  const int64_t stacked = ragged ? (int64_t)akvs_cdiv(R, S) * g * 2 : g;
+  pl.wide = is16 && ragged && (int64_t)akvs_cdiv(R, S) * g > MT;
+  const int64_t tiles = (stacked + MT - 1) / MT, z = pl.wide ? (tiles + DIR_WARPS - 1) / DIR_WARPS : tiles;
+  pl.z = (int)(z < 64 ? z : 64);
+  if (cap > 0) {
+    pl.own_splits = 1;
+    // Few sequences: their tokens are split while CTAs are missing and a split keeps 128 keys.
+    while (!pl.wide && pl.own_splits < MAX_OWN_SPLITS && (int64_t)S * n_kv * pl.z * pl.own_splits * 2 <= 296 &&
+           cap / (pl.own_splits * 2) >= 128)
+      pl.own_splits *= 2;
+  }
+  return pl;
 }
 
-int64_t parts_bytes(int splits, int R, int n_q, int hd) {
-  const int64_t rows = (int64_t)splits * R * n_q;
+int64_t parts_bytes(const Plan& pl, int R, int n_q, int hd) {
+  const int64_t rows = (int64_t)(pl.splits + pl.own_splits) * R * n_q;
   return akvs_align_up(rows * hd * 4, 256) + akvs_align_up(rows * 8, 256) + 256;
 }
 
 template <typename T, int HD>
-int32_t run(SharedParams& p, int dtype, bool tc, cudaStream_t st) {
+int32_t run(SharedParams& p, int dtype, const Plan& pl, cudaStream_t st) {
   constexpr int smem = direct_smem<T, HD>();
-  static_assert(smem <= 48 * 1024, "the direct kernels stay below the size that needs an attribute");
-  if (p.splits > 0 && tc) {
+  static bool attr_set = false;
+  if (!attr_set) {
+    AKVS_CUDA(cudaFuncSetAttribute(context_direct_kernel<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    AKVS_CUDA(cudaFuncSetAttribute(own_kernel<T, HD, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    if constexpr (sizeof(T) == 2)
+      AKVS_CUDA(cudaFuncSetAttribute(own_kernel<T, HD, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    attr_set = true;
+  }
+  if (p.splits > 0 && pl.tc) {
     AKVS_TRY(launch_attention_parts_tc(dtype, HD, p.q, p.q_ld, p.pk, p.pv, p.p_ld, p.R, p.P, p.n_q, p.n_kv, p.split_len,
                                        p.part_o, p.part_ml, st));
   } else if (p.splits > 0) {
@@ -567,29 +685,23 @@ int32_t run(SharedParams& p, int dtype, bool tc, cudaStream_t st) {
     AKVS_CUDA(launch_pdl(context_direct_kernel<T, HD>, dim3(p.splits, p.n_kv, (unsigned)tiles), dim3(DIR_THREADS), smem, st, p));
     AKVS_LAUNCHED();
   }
-  if (p.S == 0) return AKVS_OK;
-  // Tiles in flight per sequence: one is all there is for a row per sequence and up to 16 heads per
-  // kv head; ragged batches get room for twice the mean, and a CTA walks what is left.
-  const int z = p.q_off ? (int)min((int64_t)64, ((int64_t)akvs_cdiv(p.R, p.S) * p.g * 2 + MT - 1) / MT) : akvs_cdiv(p.g, MT);
-  // Few sequences with long slots: a cluster shares the own tokens of one (256 keys or more each).
-  int C = 1;
-  while (C < MAX_C && (int64_t)p.S * p.n_kv * z * C * 2 <= 296 && p.cap / (C * 2) >= 256) C *= 2;
-  if (C == 1 && (int64_t)p.S * p.n_kv * z * 4 <= 148 && p.splits > 8) C = 4;   // the join alone is worth four SMs
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(p.S * C), p.n_kv, z < 1 ? 1 : z);
-  cfg.blockDim = dim3(DIR_THREADS);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = C;
-  attr[1].val.clusterDim.y = 1;
-  attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  AKVS_CUDA(cudaLaunchKernelEx(&cfg, own_join_kernel<T, HD>, p, C));
+  if (p.own_splits > 0) {
+    const dim3 grid((unsigned)(p.S * p.own_splits), p.n_kv, pl.z);
+    auto kernel = own_kernel<T, HD, false>;
+    if constexpr (sizeof(T) == 2)
+      if (pl.wide) kernel = own_kernel<T, HD, true>;
+    AKVS_CUDA(launch_pdl(kernel, grid, dim3(DIR_THREADS), smem, st, p));
+    AKVS_LAUNCHED();
+  }
+  // Few rows with many parts: four warps share a row's parts.
+  const int64_t rows_z = p.q_off ? (int64_t)akvs_cdiv(p.R, p.S) * p.g * 2 : p.g;
+  if ((int64_t)p.R * p.n_q <= 2048 && p.splits + p.own_splits > 8) {
+    const int z = (int)(rows_z < 256 ? rows_z : 256);
+    AKVS_CUDA(launch_pdl(join_kernel<T, HD, 4>, dim3(p.S, p.n_kv, z), dim3(DIR_THREADS), 0, st, p));
+  } else {
+    const int64_t z4 = (rows_z + DIR_WARPS - 1) / DIR_WARPS;
+    AKVS_CUDA(launch_pdl(join_kernel<T, HD, 1>, dim3(p.S, p.n_kv, (unsigned)(z4 < 256 ? z4 : 256)), dim3(DIR_THREADS), 0, st, p));
+  }
   AKVS_LAUNCHED();
   return AKVS_OK;
 }
@@ -598,12 +710,15 @@ bool heads_ok(int32_t n_q, int32_t n_kv) { return n_kv > 0 && n_q > 0 && n_q % n
 
 }  // namespace
 
-extern "C" int64_t akvs_op_attention_shared_scratch_bytes(int32_t R, int32_t P, int32_t n_q_heads, int32_t n_kv_heads,
-                                                          int32_t head_dim) {
-  if (R < 0 || P < 0 || !heads_ok(n_q_heads, n_kv_heads) || (head_dim != 64 && head_dim != 128)) return -1;
-  const int g = n_q_heads / n_kv_heads;       // the larger of the two ways the types take
-  const int a = plan_context(true, R, P, g, n_kv_heads, head_dim).splits, b = plan_context(false, R, P, g, n_kv_heads, head_dim).splits;
-  return parts_bytes(a > b ? a : b, R, n_q_heads, head_dim);
+extern "C" int64_t akvs_op_attention_shared_scratch_bytes(int32_t dtype, int32_t R, int32_t P, int32_t S, int32_t cap,
+                                                          int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim) {
+  if (dtype != AKVS_F32 && dtype != AKVS_BF16 && dtype != AKVS_F16) return -1;
+  if (R < 0 || P < 0 || S < 0 || cap < 0 || !heads_ok(n_q_heads, n_kv_heads) || (head_dim != 64 && head_dim != 128)) return -1;
+  // one row per sequence and ragged rows are cut differently: room for either
+  const int g = n_q_heads / n_kv_heads;
+  const int64_t a = parts_bytes(make_plan(dtype != AKVS_F32, R, P, S, cap, g, n_kv_heads, head_dim, false), R, n_q_heads, head_dim);
+  const int64_t b = parts_bytes(make_plan(dtype != AKVS_F32, R, P, S, cap, g, n_kv_heads, head_dim, true), R, n_q_heads, head_dim);
+  return a > b ? a : b;
 }
 
 extern "C" int32_t akvs_op_attention_shared(int32_t dtype, const void* q, int64_t q_ld, int32_t R, const void* ctx_k,
@@ -625,16 +740,16 @@ extern "C" int32_t akvs_op_attention_shared(int32_t dtype, const void* q, int64_
   if (!aligned16(q) || !aligned16(out) || q_ld * es % 16 || (P > 0 && (!aligned16(ctx_k) || !aligned16(ctx_v) || ctx_ld * es % 16)) ||
       (cap > 0 && (!aligned16(own_k) || !aligned16(own_v) || own_ld * es % 16 || own_seq_ld * es % 16)))
     return AKVS_ERR_INVALID_ARG;
-  if ((int64_t)R * n_q_heads > 0x7fffffff || (int64_t)S * MAX_C > 0x7fffffff) return AKVS_ERR_TOO_LARGE;
-  const Plan pl = plan_context(dtype != AKVS_F32, R, P, n_q_heads / n_kv_heads, n_kv_heads, head_dim);
-  const int64_t need = parts_bytes(pl.splits, R, n_q_heads, head_dim);
-  if (pl.splits > 0 && (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255) || scratch_size < need)) return AKVS_ERR_WORKSPACE;
+  if ((int64_t)R * n_q_heads > 0x7fffffff || (int64_t)S * MAX_OWN_SPLITS > 0x7fffffff) return AKVS_ERR_TOO_LARGE;
+  const Plan pl = make_plan(dtype != AKVS_F32, R, P, S, cap, n_q_heads / n_kv_heads, n_kv_heads, head_dim, q_off != nullptr);
+  const int64_t need = parts_bytes(pl, R, n_q_heads, head_dim);
+  if (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255) || scratch_size < need) return AKVS_ERR_WORKSPACE;
   const int64_t ctx_n = P > 0 ? ((P - 1) * ctx_ld + row) * es : 0;
   const int64_t own_n = cap > 0 ? ((S - 1) * own_seq_ld + (cap - 1) * own_ld + row) * es : 0;
   const void* ins[7] = {q, ctx_k, ctx_v, own_k, own_v, own_len, q_off};
   const int64_t in_n[7] = {((R - 1) * q_ld + q_row) * es, ctx_n, ctx_n, own_n, own_n, cap > 0 ? S * 4ll : 0, q_off ? (S + 1) * 4ll : 0};
   const void* outs[3] = {out, lse, scratch};
-  const int64_t out_n[3] = {R * q_row * es, (int64_t)R * n_q_heads * 4, pl.splits > 0 ? need : 0};
+  const int64_t out_n[3] = {R * q_row * es, (int64_t)R * n_q_heads * 4, need};
   for (int o = 0; o < 3; ++o) {
     for (int i = 0; i < 7; ++i)
       if (bytes_overlap(ins[i], in_n[i], outs[o], out_n[o])) return AKVS_ERR_INVALID_ARG;
@@ -646,14 +761,14 @@ extern "C" int32_t akvs_op_attention_shared(int32_t dtype, const void* q, int64_
   p.pk = ctx_k; p.pv = ctx_v; p.P = P; p.p_ld = ctx_ld;
   p.sk = own_k; p.sv = own_v; p.S = S; p.cap = cap; p.s_ld = own_ld; p.s_seq = own_seq_ld; p.s_len = own_len; p.q_off = q_off;
   p.out = out; p.lse = lse;
-  p.splits = pl.splits; p.split_len = pl.split_len;
-  const int64_t rows = (int64_t)pl.splits * R * n_q_heads;
+  p.splits = pl.splits; p.split_len = pl.split_len; p.own_splits = pl.own_splits;
+  const int64_t rows = (int64_t)(pl.splits + pl.own_splits) * R * n_q_heads;
   p.part_o = reinterpret_cast<float*>(scratch);
   p.part_ml = reinterpret_cast<float2*>(reinterpret_cast<char*>(scratch) + akvs_align_up(rows * head_dim * 4, 256));
   p.scale_log2 = LOG2E / sqrtf((float)head_dim);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   return dispatch_dtype(dtype, [&](auto tag) -> int32_t {
     using T = decltype(tag);
-    return head_dim == 64 ? run<T, 64>(p, dtype, pl.tc, st) : run<T, 128>(p, dtype, pl.tc, st);
+    return head_dim == 64 ? run<T, 64>(p, dtype, pl, st) : run<T, 128>(p, dtype, pl, st);
   });
 }

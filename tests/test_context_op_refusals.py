@@ -73,8 +73,10 @@ def test_shared_attention_refuses(b, change, code):
 
 def test_shared_attention_sizes(b):
     f = b.lib.akvs_op_attention_shared_scratch_bytes
-    assert f(3, 100, 4, 2, 128) >= 3 * 4 * (128 + 2) * 4
-    assert f(-1, 100, 4, 2, 128) == -1 and f(3, 100, 5, 2, 128) == -1 and f(3, 100, 4, 2, 96) == -1
+    assert f(1, 3, 100, 3, 20, 4, 2, 128) >= 2 * 3 * 4 * (128 + 2) * 4
+    for bad in ((3, 3, 100, 3, 20, 4, 2, 128), (1, -1, 100, 3, 20, 4, 2, 128), (1, 3, 100, 3, 20, 5, 2, 128), (1, 3, 100, 3, -1, 4, 2, 128),
+                (1, 3, 100, 3, 20, 4, 2, 96)):
+        assert f(*bad) == -1
     assert b.lib.akvs_op_attention_shared(*{**SHARED, "R": 0, "S": 0, "q": None}.values()) == 0
 
 

@@ -286,7 +286,7 @@ def test_shared_replayed_graph_follows_lengths(akvs):
     q, ck, cv, sk, sv, _, off = c
     sk, sv = torch.nan_to_num(sk, 0.5, 0.5), torch.nan_to_num(sv, 0.5, 0.5)
     dl = ints(lens)
-    scratch = akvs.op_attention_shared_scratch(4, 400, 8, 2, 128)
+    scratch = akvs.op_attention_shared_scratch(F16, 4, 400, 4, 40, 8, 2, 128)
     outs = [(torch.zeros_like(q), torch.zeros(4, 8, device="cuda")) for _ in range(2)]
     akvs.op_attention_shared(q, ck, cv, sk, sv, dl, None, *outs[0], scratch)
     graphs = []
