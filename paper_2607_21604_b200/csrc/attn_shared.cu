@@ -31,7 +31,7 @@ namespace {
 
 constexpr int DIR_WARPS = 4, DIR_THREADS = DIR_WARPS * 32;
 constexpr int MT = 16;                        // stacked rows of a tile (the M of one mma)
-constexpr int ST = 3;                         // stages of a warp's ring
+constexpr int ST = 3;                         // stages of a warp's ring, 16 keys each
 constexpr int MAX_OWN_SPLITS = 64;
 constexpr float NO_MAX = -1.0e30f;            // running maximum before any key: exp2(x - NO_MAX) is never formed for x = -inf rows
 constexpr float LN2 = 0.69314718f, LOG2E = 1.4426950408889634f;
@@ -90,78 +90,68 @@ struct Tile {
   __device__ __forceinline__ int head(int m, int g) const { return h * g + (j0 + m) % g; }
 };
 
-// ---- 16-bit core of one warp: keys start, start + step, ... (16 at a time) below `end` of k/v (rows
-// `ld` apart); row m sees the keys below lim(m), all rows those below all_see.
+// ---- 16-bit types: what a warp keeps of its tile while keys pass by.
 template <int HD> constexpr int STAGE = 16 * HD * 4;       // bytes: 16 rows of K, 16 rows of V
-template <int HD> struct WarpAcc {
-  float o[HD / 64][8][4];                     // rows gr and gr + 8; columns 64 c + 16 t + 8 e + i at [c][i][2 s + e]
-  float mx[2], sum[2];
-};
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool ok) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ uint4 lds16(uint32_t a) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
   return v;
 }
+// Copies chunk c of row `row` (of 16) of K and V into a stage.  Places are exchanged so that the eight
+// lanes of a shared-memory phase hit different banks: a K read takes 4 chunks of two neighbouring
+// rows, a V read 2 chunks of four even rows.  Rows behind the end may hold anything, NaN included,
+// and 0 * NaN is not 0: they arrive as zeros.
+template <typename T, int HD>
+__device__ __forceinline__ void copy_chunk(uint32_t stage, const T* k, const T* v, int64_t ld, int key, int end, int row, int c) {
+  constexpr int CH = HD / 8;
+  const bool ok = key < end;
+  const int64_t at = (int64_t)(ok ? key : end - 1) * ld + c * 8;
+  cp16(stage + (row * CH + (c ^ ((row & 1) << 2))) * 16, k + at, ok);
+  cp16(stage + STAGE<HD> / 2 + (row * CH + (c ^ (row & 6))) * 16, v + at, ok);
+}
 
-template <typename T, int HD, typename Lim>
-__device__ __forceinline__ void warp_core(const SharedParams& p, const Tile& tl, const T* k, const T* v, int64_t ld, int start,
-                                          int end, int step, int all_see, const Lim& lim, uint32_t ring, WarpAcc<HD>& acc) {
-  constexpr int KC = HD / 32, VC = HD / 64, CH = HD / 8;    // 16-byte chunks of a row: CH
-  const int lane = threadIdx.x & 31, gr = lane >> 2, t = lane & 3;
-  // Places in a stage are exchanged so that the eight lanes of a shared-memory phase hit different
-  // banks: a K read takes 4 chunks of two neighbouring rows, a V read 2 chunks of four even rows.
-  auto issue = [&](int n) {
-    const int key0 = start + n * step;
-    if (key0 < end) {
-      const uint32_t base = ring + (n % ST) * STAGE<HD>;
-#pragma unroll
-      for (int i = 0; i < 16 * CH / 32; ++i) {
-        const int row = (i * 32 + lane) / CH, c = (i * 32 + lane) % CH;
-        const bool ok = key0 + row < end;
-        // rows behind the end may hold anything, NaN included, and 0 * NaN is not 0: they arrive as zeros
-        const int64_t at = (int64_t)(ok ? key0 + row : end - 1) * ld + c * 8;
-        cp16(base + (row * CH + (c ^ ((row & 1) << 2))) * 16, k + at, ok);
-        cp16(base + STAGE<HD> / 2 + (row * CH + (c ^ (row & 6))) * 16, v + at, ok);
-      }
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-#pragma unroll
-  for (int n = 0; n < ST - 1; ++n) issue(n);
+template <typename T, int HD>
+struct WarpTile {
+  static constexpr int KC = HD / 32, VC = HD / 64, CH = HD / 8;
   uint32_t qa[2][KC][4];
-#pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    const int m = gr + 8 * s;
-    const bool ok = tl.valid(m);
-    const T* q = reinterpret_cast<const T*>(p.q) + (ok ? (int64_t)tl.row(m, p.g) * p.q_ld + (int64_t)tl.head(m, p.g) * HD : 0);
-#pragma unroll
-    for (int c = 0; c < KC; ++c) {
-      const uint4 x = ok ? __ldcg(reinterpret_cast<const uint4*>(q + 32 * c + 8 * t)) : make_uint4(0u, 0u, 0u, 0u);
-      qa[s][c][0] = x.x; qa[s][c][1] = x.y; qa[s][c][2] = x.z; qa[s][c][3] = x.w;
-    }
-  }
-  const int limit[2] = {min(lim(gr), end), min(lim(gr + 8), end)};
-  auto& o = acc.o;
-  auto& mx = acc.mx;
-  auto& sum = acc.sum;
-#pragma unroll
-  for (int a = 0; a < VC; ++a)
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[a][i][e] = 0.f;
-  mx[0] = mx[1] = NO_MAX;
-  sum[0] = sum[1] = 0.f;
+  int limit[2];                               // rows gr and gr + 8 see the keys below these
+  float o[VC][8][4];                          // columns 64 c + 16 t + 8 e + i of row gr + 8 s at [c][i][2 s + e]
+  float mx[2], sum[2];
 
-  int n = 0;
-  for (int key0 = start; key0 < end; key0 += step, ++n) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(ST - 2) : "memory");
-    __syncwarp();                                   // every lane's copies are there, and the stage before is read
-    issue(n + ST - 1);
-    const uint32_t ks = ring + (n % ST) * STAGE<HD>, vs = ks + STAGE<HD> / 2;
+  template <typename Lim>
+  __device__ __forceinline__ void begin(const SharedParams& p, const Tile& tl, int end, const Lim& lim) {
+    const int lane = threadIdx.x & 31, gr = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int m = gr + 8 * s;
+      const bool ok = tl.valid(m);
+      const T* q = reinterpret_cast<const T*>(p.q) + (ok ? (int64_t)tl.row(m, p.g) * p.q_ld + (int64_t)tl.head(m, p.g) * HD : 0);
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        const uint4 x = ok ? __ldcg(reinterpret_cast<const uint4*>(q + 32 * c + 8 * t)) : make_uint4(0u, 0u, 0u, 0u);
+        qa[s][c][0] = x.x; qa[s][c][1] = x.y; qa[s][c][2] = x.z; qa[s][c][3] = x.w;
+      }
+      limit[s] = min(lim(m), end);
+      mx[s] = NO_MAX;
+      sum[s] = 0.f;
+    }
+#pragma unroll
+    for (int a = 0; a < VC; ++a)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[a][i][e] = 0.f;
+  }
+
+  // 16 keys from key0, staged at `ks`; no key from `end` on exists, all rows see those below all_see.
+  __device__ __forceinline__ void step(uint32_t ks, int key0, int end, int all_see, float scale_log2) {
+    const int lane = threadIdx.x & 31, gr = lane >> 2, t = lane & 3;
+    const uint32_t vs = ks + STAGE<HD> / 2;
     float sc[2][4];
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
@@ -182,7 +172,7 @@ __device__ __forceinline__ void warp_core(const SharedParams& p, const Tile& tl,
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int key = key0 + (e >> 1) * 8 + 2 * t + (e & 1);
-        const float y = sc[e >> 1][2 * s + (e & 1)] * p.scale_log2;
+        const float y = sc[e >> 1][2 * s + (e & 1)] * scale_log2;
         x[e] = every || key < limit[s] ? y : -INFINITY;
       }
       float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
@@ -271,12 +261,50 @@ __device__ __forceinline__ void warp_core(const SharedParams& p, const Tile& tl,
       }
     }
   }
-  asm volatile("cp.async.wait_group 0;" ::: "memory");
+
+  __device__ __forceinline__ void finish() {
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    sum[s] += __shfl_xor_sync(0xFFFFFFFFu, sum[s], 1);
-    sum[s] += __shfl_xor_sync(0xFFFFFFFFu, sum[s], 2);
+    for (int s = 0; s < 2; ++s) {
+      sum[s] += __shfl_xor_sync(0xFFFFFFFFu, sum[s], 1);
+      sum[s] += __shfl_xor_sync(0xFFFFFFFFu, sum[s], 2);
+    }
   }
+
+  // four columns of row gr + 8 s: 64 c + 16 t + 8 e + i ..
+  __device__ __forceinline__ float4 quad(int c, int s, int e, int i, float f) const {
+    return make_float4(o[c][i][2 * s + e] * f, o[c][i + 1][2 * s + e] * f, o[c][i + 2][2 * s + e] * f, o[c][i + 3][2 * s + e] * f);
+  }
+};
+
+// A warp alone: keys start, start + step, ... (16 at a time) below `end`, through its own ring.
+template <typename T, int HD, typename Lim>
+__device__ __forceinline__ void warp_core(const SharedParams& p, const Tile& tl, const T* k, const T* v, int64_t ld, int start,
+                                          int end, int step, int all_see, const Lim& lim, uint32_t ring, WarpTile<T, HD>& wt) {
+  constexpr int CH = HD / 8;
+  const int lane = threadIdx.x & 31;
+  auto issue = [&](int n) {
+    const int key0 = start + n * step;
+    if (key0 < end) {
+#pragma unroll
+      for (int i = 0; i < 16 * CH / 32; ++i) {
+        const int row = (i * 32 + lane) / CH, c = (i * 32 + lane) % CH;
+        copy_chunk<T, HD>(ring + (n % ST) * STAGE<HD>, k, v, ld, key0 + row, end, row, c);
+      }
+    }
+    cp_commit();
+  };
+#pragma unroll
+  for (int n = 0; n < ST - 1; ++n) issue(n);
+  wt.begin(p, tl, end, lim);
+  int n = 0;
+  for (int key0 = start; key0 < end; key0 += step, ++n) {
+    cp_wait<ST - 2>();
+    __syncwarp();                             // every lane's copies are there, and the stage before is read
+    issue(n + ST - 1);
+    wt.step(ring + (n % ST) * STAGE<HD>, key0, end, all_see, p.scale_log2);
+  }
+  cp_wait<0>();
+  wt.finish();
 }
 
 // Row m's part into scratch, from a row of O in shared memory.
@@ -289,6 +317,24 @@ __device__ __forceinline__ void store_ml(const SharedParams& p, const Tile& tl, 
   p.part_ml[(int64_t)part * p.R * p.n_q + (int64_t)tl.row(m, p.g) * p.n_q + tl.head(m, p.g)] = make_float2(mx, l);
 }
 
+// A warp's whole tile into scratch, from its registers.
+template <typename T, int HD>
+__device__ __forceinline__ void store_tile(const SharedParams& p, const Tile& tl, int part, const WarpTile<T, HD>& wt) {
+  const int lane = threadIdx.x & 31, gr = lane >> 2, t = lane & 3;
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const int m = gr + 8 * s;
+    if (!tl.valid(m)) continue;
+#pragma unroll
+    for (int c = 0; c < HD / 64; ++c)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) store_part<HD>(p, tl, part, m, 64 * c + 16 * t + 8 * e + i, wt.quad(c, s, e, i, 1.f));
+    if (t == 0) store_ml(p, tl, part, m, wt.mx[s], wt.sum[s]);
+  }
+}
+
 // One tile, the CTA's warps taking turns over its keys; joins them and leaves the part in scratch.
 template <typename T, int HD, typename Lim>
 __device__ __forceinline__ void cta_part(const SharedParams& p, const Tile& tl, const T* k, const T* v, int64_t ld, int start,
@@ -297,7 +343,7 @@ __device__ __forceinline__ void cta_part(const SharedParams& p, const Tile& tl, 
   constexpr int LD = HD + 4;                  // 16-byte rows that start in different banks
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gr = lane >> 2, t = lane & 3;
   float* raw = reinterpret_cast<float*>(smem);
-  WarpAcc<HD> acc;
+  WarpTile<T, HD> acc;
   warp_core<T, HD>(p, tl, k, v, ld, start + warp * 16, end, DIR_WARPS * 16, all_see, lim,
                    tc::smem_u32(smem) + warp * ST * STAGE<HD>, acc);
   if (t == 0)
@@ -318,9 +364,7 @@ __device__ __forceinline__ void cta_part(const SharedParams& p, const Tile& tl, 
       for (int i = 0; i < 8; i += 4)
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-          *reinterpret_cast<float4*>(dst + 64 * c + 8 * e + i) =
-              make_float4(acc.o[c][i][2 * s + e] * f, acc.o[c][i + 1][2 * s + e] * f, acc.o[c][i + 2][2 * s + e] * f,
-                          acc.o[c][i + 3][2 * s + e] * f);
+          *reinterpret_cast<float4*>(dst + 64 * c + 8 * e + i) = acc.quad(c, s, e, i, f);
   }
   __syncthreads();
   for (int i = threadIdx.x; i < MT * HD / 4; i += DIR_THREADS) {
@@ -448,15 +492,10 @@ __device__ __forceinline__ void tile_part(const SharedParams& p, const Tile& tl,
     cta_part<T, HD>(p, tl, k, v, ld, start, end, all_see, lim, smem, part);
 }
 
-// ---- 1. context: grid (split, kv head, tile of 16 stacked rows)
+// ---- 1. context, one split of it, for a tile of 16 stacked rows
 template <typename T, int HD>
-__global__ void __launch_bounds__(DIR_THREADS)
-context_direct_kernel(const __grid_constant__ SharedParams p) {
-  extern __shared__ __align__(16) uint8_t smem[];
-  pdl_wait();
-  pdl_trigger();                              // after the wait: see own_kernel
-  const int split = blockIdx.x, h = blockIdx.y;
-  const Tile tl{0, (int)blockIdx.z * MT, p.R * p.g, h};
+__device__ __forceinline__ void context_tile(const SharedParams& p, int split, int h, int tile, uint8_t* smem) {
+  const Tile tl{0, tile * MT, p.R * p.g, h};
   const int start = split * p.split_len, end = min(start + p.split_len, p.P);
   tile_part<T, HD>(p, tl, (const T*)p.pk + (int64_t)h * HD, (const T*)p.pv + (int64_t)h * HD, p.p_ld, start, end, end,
                    [&](int) { return end; }, smem, split);
@@ -477,8 +516,35 @@ __device__ __forceinline__ Seq sequence(const SharedParams& p, int s) {
   return q;
 }
 
-// ---- 2. own tokens: grid (sequence * own split, kv head, tiles in flight).
+// ---- 2. own tokens of a sequence, one split of them, tile z of nz in flight.
 // WIDE (sequences of many rows, one split): every warp has a tile of its own and runs all its keys.
+template <typename T, int HD, bool WIDE>
+__device__ __forceinline__ void own_tiles(const SharedParams& p, int s, int split, int h, int z, int nz, uint8_t* smem) {
+  const Seq sq = sequence(p, s);
+  const T* k = (const T*)p.sk + (int64_t)s * p.s_seq + (int64_t)h * HD;
+  const T* v = (const T*)p.sv + (int64_t)s * p.s_seq + (int64_t)h * HD;
+  const int count = sq.n * p.g;
+  constexpr int TILES = WIDE ? DIR_WARPS : 1;
+  const int warp = threadIdx.x >> 5;
+  for (int j0 = (z * TILES + (WIDE ? warp : 0)) * MT; j0 < count; j0 += nz * TILES * MT) {
+    const Tile tl{sq.r0, j0, count, h};
+    // row i of the sequence sees len - (n - 1 - i) own tokens: the tile's first row the fewest
+    auto lim = [&](int m) { return tl.valid(m) ? sq.len - (sq.n - 1 - (j0 + m) / p.g) : sq.len; };
+    const int most = max(0, lim(min(MT, count - j0) - 1)), fewest = max(0, lim(0));
+    if constexpr (WIDE) {
+      WarpTile<T, HD> wt;
+      warp_core<T, HD>(p, tl, k, v, p.s_ld, 0, most, 16, min(fewest, most), lim, tc::smem_u32(smem) + warp * ST * STAGE<HD>, wt);
+      store_tile<T, HD>(p, tl, p.splits, wt);
+      __syncwarp();                           // the ring is read
+    } else {
+      const int chunk = ((most + p.own_splits - 1) / p.own_splits + 63) / 64 * 64;
+      const int start = min(split * chunk, most), end = min(start + chunk, most);
+      tile_part<T, HD>(p, tl, k, v, p.s_ld, start, end, min(fewest, end), lim, smem, p.splits + split);
+    }
+  }
+}
+
+// beside the tcgen05 kernel: grid (sequence * own split, kv head, tiles in flight)
 template <typename T, int HD, bool WIDE>
 __global__ void __launch_bounds__(DIR_THREADS)
 own_kernel(const __grid_constant__ SharedParams p) {
@@ -488,46 +554,26 @@ own_kernel(const __grid_constant__ SharedParams p) {
   // there.  Without a context the kernel before is a stranger: wait for it first.
   if (p.splits == 0) pdl_wait();
   pdl_trigger();
-  const int s = blockIdx.x / p.own_splits, split = blockIdx.x % p.own_splits, h = blockIdx.y;
-  const Seq sq = sequence(p, s);
-  const T* k = (const T*)p.sk + (int64_t)s * p.s_seq + (int64_t)h * HD;
-  const T* v = (const T*)p.sv + (int64_t)s * p.s_seq + (int64_t)h * HD;
-  const int count = sq.n * p.g;
-  constexpr int TILES = WIDE ? DIR_WARPS : 1;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int j0 = (blockIdx.z * TILES + (WIDE ? warp : 0)) * MT; j0 < count; j0 += gridDim.z * TILES * MT) {
-    const Tile tl{sq.r0, j0, count, h};
-    // row i of the sequence sees len - (n - 1 - i) own tokens: the tile's first row the fewest
-    auto lim = [&](int m) { return tl.valid(m) ? sq.len - (sq.n - 1 - (j0 + m) / p.g) : sq.len; };
-    const int most = max(0, lim(min(MT, count - j0) - 1)), fewest = max(0, lim(0));
-    if constexpr (WIDE) {
-      WarpAcc<HD> acc;
-      warp_core<T, HD>(p, tl, k, v, p.s_ld, 0, most, 16, min(fewest, most), lim, tc::smem_u32(smem) + warp * ST * STAGE<HD>, acc);
-      const int gr = lane >> 2, t = lane & 3;
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int m = gr + 8 * x;
-        if (!tl.valid(m)) continue;
-#pragma unroll
-        for (int c = 0; c < HD / 64; ++c)
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-#pragma unroll
-            for (int i = 0; i < 8; i += 4)
-              store_part<HD>(p, tl, p.splits, m, 64 * c + 16 * t + 8 * e + i,
-                             make_float4(acc.o[c][i][2 * x + e], acc.o[c][i + 1][2 * x + e], acc.o[c][i + 2][2 * x + e],
-                                         acc.o[c][i + 3][2 * x + e]));
-        if (t == 0) store_ml(p, tl, p.splits, m, acc.mx[x], acc.sum[x]);
-      }
-      __syncwarp();
-    } else {
-      const int chunk = ((most + p.own_splits - 1) / p.own_splits + 63) / 64 * 64;
-      const int start = min(split * chunk, most), end = min(start + chunk, most);
-      tile_part<T, HD>(p, tl, k, v, p.s_ld, start, end, min(fewest, end), lim, smem, p.splits + split);
-    }
-  }
+  own_tiles<T, HD, WIDE>(p, blockIdx.x / p.own_splits, blockIdx.x % p.own_splits, blockIdx.y, blockIdx.z, gridDim.z, smem);
   // The join waits for this grid alone: its last CTA ends after the context's kernel.
   if (blockIdx.x == gridDim.x - 1 && blockIdx.y == gridDim.y - 1 && blockIdx.z == gridDim.z - 1) pdl_wait();
+}
+
+// context and own tokens in one launch: the first n_ctx CTAs of a kv head take the context
+template <typename T, int HD, bool WIDE>
+__global__ void __launch_bounds__(DIR_THREADS)
+direct_kernel(const __grid_constant__ SharedParams p, int n_ctx, int own_z) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  pdl_wait();
+  pdl_trigger();                              // after the wait: the join reads lengths and offsets without its own
+  int x = blockIdx.x;
+  if (x < n_ctx) {
+    context_tile<T, HD>(p, x % p.splits, blockIdx.y, x / p.splits, smem);
+  } else {
+    x -= n_ctx;
+    const int z = x % own_z, sx = x / own_z;
+    own_tiles<T, HD, WIDE>(p, sx / p.own_splits, sx % p.own_splits, blockIdx.y, z, own_z, smem);
+  }
 }
 
 // ---- 3. join: WPR warps per row, which share its parts.  grid (sequence, kv head, rows in flight)
@@ -621,16 +667,18 @@ struct Plan { bool tc; int splits, split_len, own_splits; bool wide; int z; };
 Plan make_plan(bool is16, int R, int P, int S, int cap, int g, int n_kv, int hd, bool ragged) {
   Plan pl = {false, 0, 0, 0, false, 1};
   if (R == 0 || S == 0) return pl;
+  // Up to one tile of stacked rows on mma.sync, more on tcgen05: over 12416 tokens of 8 kv heads one
+  // tile takes 16.2 us on mma.sync, two tiles 22.0 us against 18.9 us on tcgen05, four 42.8 against 21.8.
   if (P > 0 && is16 && (int64_t)R * g > MT) {
-    // One CTA per SM.  In units of a key tile: rounds of CTAs times (a CTA's tiles + 6 for its start
-    // and end), plus writing and reading the parts at memory speed (a tile takes about 0.7 us).
+    // One CTA per SM.  In units of a key tile (0.85 us): rounds of CTAs times (a CTA's tiles + 9 for its
+    // start and end), plus writing and reading the parts at memory speed.
     const int64_t base = (int64_t)akvs_cdiv(R, 128 / g) * n_kv;
     const int tiles = akvs_cdiv(P, 128);
-    const double part = 2.0 * R * g * n_kv * (hd + 2) * 4 / 6.4e6 / 0.7;
+    const double part = 2.0 * R * g * n_kv * (hd + 2) * 4 / 6.4e6 / 0.85;
     int best = 1;
     double best_cost = 1e300;
     for (int s = 1; s <= tiles && s <= 148; ++s) {
-      const double cost = (double)((base * s + 147) / 148) * (akvs_cdiv(tiles, s) + 6) + part * s;
+      const double cost = (double)((base * s + 147) / 148) * (akvs_cdiv(tiles, s) + 9) + part * s;
       if (cost < best_cost) { best_cost = cost; best = s; }
     }
     pl.tc = true;
@@ -665,43 +713,61 @@ int64_t parts_bytes(const Plan& pl, int R, int n_q, int hd) {
   return akvs_align_up(rows * hd * 4, 256) + akvs_align_up(rows * 8, 256) + 256;
 }
 
-template <typename T, int HD>
-int32_t run(SharedParams& p, int dtype, const Plan& pl, cudaStream_t st) {
+template <typename T, int HD, bool WIDE>
+int32_t launch_direct(const SharedParams& p, const Plan& pl, cudaStream_t st) {
   constexpr int smem = direct_smem<T, HD>();
   static bool attr_set = false;
   if (!attr_set) {
-    AKVS_CUDA(cudaFuncSetAttribute(context_direct_kernel<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    AKVS_CUDA(cudaFuncSetAttribute(own_kernel<T, HD, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    if constexpr (sizeof(T) == 2)
-      AKVS_CUDA(cudaFuncSetAttribute(own_kernel<T, HD, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    AKVS_CUDA(cudaFuncSetAttribute(direct_kernel<T, HD, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     attr_set = true;
   }
-  if (p.splits > 0 && pl.tc) {
-    AKVS_TRY(launch_attention_parts_tc(dtype, HD, p.q, p.q_ld, p.pk, p.pv, p.p_ld, p.R, p.P, p.n_q, p.n_kv, p.split_len,
-                                       p.part_o, p.part_ml, st));
-  } else if (p.splits > 0) {
-    const int64_t tiles = akvs_cdiv((int64_t)p.R * p.g, MT);
-    if (tiles > 65535) return AKVS_ERR_TOO_LARGE;
-    AKVS_CUDA(launch_pdl(context_direct_kernel<T, HD>, dim3(p.splits, p.n_kv, (unsigned)tiles), dim3(DIR_THREADS), smem, st, p));
-    AKVS_LAUNCHED();
+  const int64_t n_ctx = (int64_t)p.splits * akvs_cdiv((int64_t)p.R * p.g, MT);
+  const int64_t grid = n_ctx + (int64_t)p.S * p.own_splits * pl.z;
+  if (grid > 0x7fffffff) return AKVS_ERR_TOO_LARGE;
+  AKVS_CUDA(launch_pdl(direct_kernel<T, HD, WIDE>, dim3((unsigned)grid, p.n_kv), dim3(DIR_THREADS), smem, st, p, (int)n_ctx,
+                       pl.z));
+  AKVS_LAUNCHED();
+  return AKVS_OK;
+}
+
+template <typename T, int HD, bool WIDE>
+int32_t launch_own(const SharedParams& p, const Plan& pl, cudaStream_t st) {
+  constexpr int smem = direct_smem<T, HD>();
+  static bool attr_set = false;
+  if (!attr_set) {
+    AKVS_CUDA(cudaFuncSetAttribute(own_kernel<T, HD, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    attr_set = true;
   }
-  if (p.own_splits > 0) {
-    const dim3 grid((unsigned)(p.S * p.own_splits), p.n_kv, pl.z);
-    auto kernel = own_kernel<T, HD, false>;
-    if constexpr (sizeof(T) == 2)
-      if (pl.wide) kernel = own_kernel<T, HD, true>;
-    AKVS_CUDA(launch_pdl(kernel, grid, dim3(DIR_THREADS), smem, st, p));
-    AKVS_LAUNCHED();
+  AKVS_CUDA(launch_pdl(own_kernel<T, HD, WIDE>, dim3((unsigned)(p.S * p.own_splits), p.n_kv, pl.z), dim3(DIR_THREADS), smem, st, p));
+  AKVS_LAUNCHED();
+  return AKVS_OK;
+}
+
+template <typename T, int HD>
+int32_t run(SharedParams& p, int dtype, const Plan& pl, cudaStream_t st) {
+  if constexpr (sizeof(T) == 2) {
+    if (pl.tc) {
+      AKVS_TRY(launch_attention_parts_tc(dtype, HD, p.q, p.q_ld, p.pk, p.pv, p.p_ld, p.R, p.P, p.n_q, p.n_kv, p.split_len,
+                                         p.part_o, p.part_ml, st));
+      if (p.own_splits > 0) {
+        if (pl.wide) AKVS_TRY((launch_own<T, HD, true>(p, pl, st)));
+        else AKVS_TRY((launch_own<T, HD, false>(p, pl, st)));
+      }
+    } else if (p.splits + p.own_splits > 0) {
+      if (pl.wide) AKVS_TRY((launch_direct<T, HD, true>(p, pl, st)));
+      else AKVS_TRY((launch_direct<T, HD, false>(p, pl, st)));
+    }
+  } else if (p.splits + p.own_splits > 0) {
+    AKVS_TRY((launch_direct<T, HD, false>(p, pl, st)));
   }
-  // Few rows with many parts: four warps share a row's parts.
-  const int64_t rows_z = p.q_off ? (int64_t)akvs_cdiv(p.R, p.S) * p.g * 2 : p.g;
-  if ((int64_t)p.R * p.n_q <= 2048 && p.splits + p.own_splits > 8) {
-    const int z = (int)(rows_z < 256 ? rows_z : 256);
-    AKVS_CUDA(launch_pdl(join_kernel<T, HD, 4>, dim3(p.S, p.n_kv, z), dim3(DIR_THREADS), 0, st, p));
-  } else {
-    const int64_t z4 = (rows_z + DIR_WARPS - 1) / DIR_WARPS;
-    AKVS_CUDA(launch_pdl(join_kernel<T, HD, 1>, dim3(p.S, p.n_kv, (unsigned)(z4 < 256 ? z4 : 256)), dim3(DIR_THREADS), 0, st, p));
-  }
+  // Few rows with many parts: four warps share a row's parts.  CTAs in flight: what the SMs hold at a
+  // time; more of them would start late and find little.
+  const bool few = (int64_t)p.R * p.n_q <= 2048 && p.splits + p.own_splits > 8;
+  const int64_t rows = p.q_off ? (int64_t)akvs_cdiv(p.R, p.S) * p.g * 2 : p.g, per = few ? 1 : DIR_WARPS;
+  const int64_t fit = akvs_cdiv(148 * 8, (int64_t)p.S * p.n_kv), need = (rows + per - 1) / per;
+  const dim3 grid(p.S, p.n_kv, (unsigned)(need < fit ? need : fit < 1 ? 1 : fit));
+  if (few) AKVS_CUDA(launch_pdl(join_kernel<T, HD, 4>, grid, dim3(DIR_THREADS), 0, st, p));
+  else AKVS_CUDA(launch_pdl(join_kernel<T, HD, 1>, grid, dim3(DIR_THREADS), 0, st, p));
   AKVS_LAUNCHED();
   return AKVS_OK;
 }
