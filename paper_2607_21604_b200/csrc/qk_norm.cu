@@ -16,7 +16,7 @@
 
 namespace {
 
-constexpr int QKN_THREADS = 256;
+constexpr int QKN_THREADS = 256, QKN_BLOCKS = 4;      // per SM: 64 registers a thread
 constexpr int QKN_MAX_HALF = 128;           // head_dim <= 256
 
 struct QkNormParams {
@@ -31,15 +31,26 @@ struct QkNormParams {
   double turns[QKN_MAX_HALF];               // base^(-2i/hd) / 2pi
 };
 
+__device__ __forceinline__ void unpack(const uint4& w, float (&o)[4], float) {
+  o[0] = __uint_as_float(w.x); o[1] = __uint_as_float(w.y); o[2] = __uint_as_float(w.z); o[3] = __uint_as_float(w.w);
+}
+template <typename T>
+__device__ __forceinline__ void unpack(const uint4& w, float (&o)[8], T) {
+  ld16(reinterpret_cast<const T*>(&w), o);
+}
+
 template <typename T, int HD>
-__global__ void __launch_bounds__(QKN_THREADS)
+__global__ void __launch_bounds__(QKN_THREADS, QKN_BLOCKS)
 qk_norm_rope_kernel(const __grid_constant__ QkNormParams p) {
-  constexpr int V = VecOf<T>::N, HALF = HD / 2, LPH = HALF / V, HPW = 32 / LPH, UN = 2;
+  constexpr int V = VecOf<T>::N, HALF = HD / 2, LPH = HALF / V, HPW = 32 / LPH;
   __shared__ double turns[HALF];
+  __shared__ __align__(16) float gains[2][HD];
   pdl_trigger();
   for (int i = threadIdx.x; i < HALF; i += QKN_THREADS) turns[i] = p.turns[i];
-  __syncthreads();
   pdl_wait();
+  for (int i = threadIdx.x; i < 2 * HD; i += QKN_THREADS)
+    if (p.heads[i / HD] > 0) gains[i / HD][i % HD] = p.gain[i / HD][i % HD];
+  __syncthreads();
   const int64_t unit = (int64_t)blockIdx.x * (QKN_THREADS / 32) + (threadIdx.x >> 5);
   if (unit >= (int64_t)p.n * p.units_per_row) return;
   const int r = (int)(unit / p.units_per_row);
@@ -47,6 +58,22 @@ qk_norm_rope_kernel(const __grid_constant__ QkNormParams p) {
   const int n_heads = p.heads[0] + p.heads[1];
   const int h1 = min(h0 + p.heads_per_unit, n_heads);
   const int lane = threadIdx.x & 31, sub = lane / LPH, c = (lane % LPH) * V;
+
+  // The next group's chunks are on their way while a group is worked on, in the 8 registers of their
+  // packed form: the kernel lives on the number of warps that fit.
+  uint4 nlo, nhi;
+  auto fetch = [&](int hh) {
+    if (hh < h1) {
+      const int w = hh >= p.heads[0];
+      const uint4* x = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.x[w]) + (int64_t)r * p.ld_x[w] +
+                                                      (int64_t)(hh - (w ? p.heads[0] : 0)) * HD + c);
+      nlo = __ldcs(x);
+      nhi = __ldcs(x + LPH);
+    } else {
+      nlo = nhi = make_uint4(0u, 0u, 0u, 0u);
+    }
+  };
+  fetch(h0 + sub);
 
   float cs[V], sn[V];
   const double at = (double)p.pos[r];
@@ -62,45 +89,34 @@ qk_norm_rope_kernel(const __grid_constant__ QkNormParams p) {
     cs[i] = fmaf(-s_, lo, c_);
   }
 
-  // UN groups of HPW heads at a time: their loads are in flight together
-  for (int h = h0; h < h1; h += HPW * UN) {
-    float lo[UN][V], hi[UN][V];
+  for (int h = h0 + sub; h - sub < h1; h += HPW) {
+    float lo[V], hi[V];
+    unpack(nlo, lo, T{});
+    unpack(nhi, hi, T{});
+    fetch(h + HPW);
+    float ss = 0.f;
 #pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      const int hh = h + u * HPW + sub;
-      if (hh < h1) {
-        const int w = hh >= p.heads[0];
-        const T* x = reinterpret_cast<const T*>(p.x[w]) + (int64_t)r * p.ld_x[w] + (int64_t)(hh - (w ? p.heads[0] : 0)) * HD + c;
-        ld16(x, lo[u]);
-        ld16(x + HALF, hi[u]);
-      } else {
+    for (int i = 0; i < V; ++i) ss = fmaf(lo[i], lo[i], fmaf(hi[i], hi[i], ss));
 #pragma unroll
-        for (int i = 0; i < V; ++i) lo[u][i] = hi[u][i] = 0.f;
+    for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
+    const float scale = rsqrtf(ss * (1.f / HD) + p.eps);
+    if (h >= h1) continue;
+    const int w = h >= p.heads[0];
+    float olo[V], ohi[V];
+#pragma unroll
+    for (int i = 0; i < V; i += 4) {
+      const float4 gl = *reinterpret_cast<const float4*>(&gains[w][c + i]), gh = *reinterpret_cast<const float4*>(&gains[w][HALF + c + i]);
+      const float ga[4] = {gl.x, gl.y, gl.z, gl.w}, gb[4] = {gh.x, gh.y, gh.z, gh.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float a = lo[i + e] * scale * ga[e], b = hi[i + e] * scale * gb[e];
+        olo[i + e] = a * cs[i + e] - b * sn[i + e];
+        ohi[i + e] = b * cs[i + e] + a * sn[i + e];
       }
     }
-#pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      float ss = 0.f;
-#pragma unroll
-      for (int i = 0; i < V; ++i) ss = fmaf(lo[u][i], lo[u][i], fmaf(hi[u][i], hi[u][i], ss));
-#pragma unroll
-      for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
-      const float scale = rsqrtf(ss * (1.f / HD) + p.eps);
-      const int hh = h + u * HPW + sub;
-      if (hh >= h1) continue;
-      const int w = hh >= p.heads[0];
-      const float* g = p.gain[w] + c;
-      float olo[V], ohi[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float a = lo[u][i] * scale * __ldg(g + i), b = hi[u][i] * scale * __ldg(g + HALF + i);
-        olo[i] = a * cs[i] - b * sn[i];
-        ohi[i] = b * cs[i] + a * sn[i];
-      }
-      T* y = reinterpret_cast<T*>(p.y[w]) + (int64_t)r * p.ld_y[w] + (int64_t)(hh - (w ? p.heads[0] : 0)) * HD + c;
-      st16(y, olo);
-      st16(y + HALF, ohi);
-    }
+    T* y = reinterpret_cast<T*>(p.y[w]) + (int64_t)r * p.ld_y[w] + (int64_t)(h - (w ? p.heads[0] : 0)) * HD + c;
+    st16(y, olo);
+    st16(y + HALF, ohi);
   }
 }
 
@@ -108,12 +124,12 @@ template <typename T, int HD>
 int32_t run(QkNormParams& p, cudaStream_t st) {
   constexpr int HPW = 32 / (HD / 2 / VecOf<T>::N);
   const int n_heads = p.heads[0] + p.heads[1];
-  // Few rows: one group of heads per warp, so that all SMs get work.  Many rows: up to 8 groups,
+  // Few rows: one group of heads per warp, so that all SMs get work.  Many rows: up to 16 groups,
   // which share the angles of their row.
   int groups = akvs_cdiv(n_heads, HPW), per = 1;
-  while (per < 8 && per < groups && (int64_t)p.n * akvs_cdiv(groups, per * 2) >= 148 * 64) per *= 2;
-  p.heads_per_unit = per * HPW;
-  p.units_per_row = akvs_cdiv(n_heads, p.heads_per_unit);
+  while (per < 16 && per < groups && (int64_t)p.n * akvs_cdiv(groups, per * 2) >= 148 * 64) per *= 2;
+  p.units_per_row = akvs_cdiv(groups, per);
+  p.heads_per_unit = akvs_cdiv(groups, p.units_per_row) * HPW;       // even shares
   const int64_t blocks = ((int64_t)p.n * p.units_per_row + QKN_THREADS / 32 - 1) / (QKN_THREADS / 32);
   if (blocks > 0x7fffffff) return AKVS_ERR_TOO_LARGE;
   AKVS_CUDA(launch_pdl(qk_norm_rope_kernel<T, HD>, dim3((unsigned)blocks), dim3(QKN_THREADS), 0, st, p));
