@@ -3,21 +3,22 @@
 // tokens are kept (ties to the smaller index); the kept tokens' K, V and mass are packed in
 // ascending token order.
 //
-// select_kernel finds the threshold: a cluster of C CTAs owns one (layer, head) row of masses,
-// keeps it in shared memory as order-preserving 32-bit keys, and fixes the key of the last kept
-// token in four passes of 8 bits; the 256-bin histograms of the CTAs are added up through
-// distributed shared memory.  Counts of greater and equal keys per warp then give every kept
-// token its place without a sort.  Selection is latency bound (a row is read once from memory),
-// so a call with few rows spreads each over up to 8 SMs.
-// gather_kernel moves the kept K/V, 16 bytes per thread and step: memory bound, and nearly all
-// of the operator's bytes.
+// One launch: a cluster of C CTAs owns one (layer, head) row of masses, keeps it in shared memory as
+// order-preserving 32-bit keys, and fixes the key of the last kept token in four passes of 8 bits;
+// the 256-bin histograms of the CTAs are added up through distributed shared memory.  Counts of
+// greater and equal keys per warp then give every kept token its place without a sort, and the
+// cluster moves its head's K/V of the kept tokens, 16 bytes per lane, an equal share per CTA.
+// Selection is latency bound (a row is read once from memory), so a call with few rows spreads
+// each over up to 8 SMs; the copies are memory bound and nearly all of the operator's bytes.
 #include "tc_common.cuh"
 
 namespace {
 
 constexpr int SEL_THREADS = 512, SEL_WARPS = SEL_THREADS / 32;
+static_assert(SEL_THREADS >= 256, "a thread per bin");
+constexpr int COPY_UN = 4;                         // tokens of a lane in flight
 constexpr int SEL_MAX_C = 8;                       // portable cluster size
-constexpr int SEL_MAX_SEG = 50 * 1024;             // keys of a CTA's shared memory (200 KB)
+constexpr int SEL_MAX_SEG = 50 * 1024;             // keys of a CTA's shared memory (200 KB, beside 18 KB of counts)
 
 // Order of the masses as unsigned integers: greater mass, greater key; -0 equals +0, NaN is the
 // smallest of all, so that a broken mass is the first to go.
@@ -25,6 +26,9 @@ __device__ __forceinline__ uint32_t mass_key(float m) {
   if (m != m) return 0u;
   const uint32_t u = __float_as_uint(m + 0.f);     // -0 + 0 = +0
   return (u >> 31) ? ~u : (u | 0x80000000u);
+}
+__device__ __forceinline__ float key_mass(uint32_t k) {
+  return k == 0u ? __uint_as_float(0x7FFFFFFFu) : __uint_as_float((k >> 31) ? (k & 0x7FFFFFFFu) : ~k);
 }
 __device__ __forceinline__ uint32_t ld_cluster(uint32_t addr) {
   uint32_t v;
@@ -34,10 +38,12 @@ __device__ __forceinline__ uint32_t ld_cluster(uint32_t addr) {
 
 template <bool CACHED>
 __global__ void __launch_bounds__(SEL_THREADS)
-select_kernel(const float* __restrict__ mass, int T, int n_sink, int n_recent, int budget, int seg,
-              int32_t* __restrict__ idx, float* __restrict__ mass_out) {
+evict_kernel(const float* __restrict__ mass, int T, int n_sink, int n_recent, int budget, int seg, int32_t* idx,
+             float* __restrict__ mass_out, const uint4* __restrict__ k, const uint4* __restrict__ v, int n_kv, int log_cph,
+             int64_t layer_ld, int64_t tok_ld, uint4* __restrict__ k_out, uint4* __restrict__ v_out) {
   extern __shared__ uint32_t keys[];               // [seg] when CACHED
-  __shared__ uint32_t hist[2][256];
+  __shared__ uint32_t hist[2][256];                // this CTA's counts, read by the cluster
+  __shared__ uint32_t sub[SEL_WARPS][256];         // a warp's own: masses share exponents, and bins would be fought over
   __shared__ uint32_t warp_part[SEL_WARPS];
   __shared__ uint32_t found[2];                    // bin, keys still wanted from it
   __shared__ uint32_t cnt[2];                      // this CTA's kept-for-sure and tied tokens
@@ -52,35 +58,51 @@ select_kernel(const float* __restrict__ mass, int T, int n_sink, int n_recent, i
   pdl_wait();
   const float* m = mass + (int64_t)row * T + t0;
   if (CACHED) {
-    for (int i = tid; i < n; i += SEL_THREADS) keys[i] = mass_key(m[i]);
+#pragma unroll 8
+    for (int i = tid; i < n; i += SEL_THREADS) keys[i] = mass_key(__ldg(m + i));
   }
   auto key = [&](int i) { return CACHED ? keys[i] : mass_key(__ldg(m + i)); };
-  auto forced = [&](int i) { const int t = t0 + i; return t < n_sink || t >= T - n_recent; };
+  auto sync_cluster = [&]() {
+    if (C > 1) tc::cluster_sync_all();
+    else __syncthreads();
+  };
   const int from = max(n_sink - t0, 0), to = min(T - n_recent - t0, n);    // candidates of this CTA
 
   uint32_t want = (uint32_t)(budget - n_sink - n_recent);
   uint32_t prefix = 0, mask = 0;
-  for (int i = tid; i < 512; i += SEL_THREADS) (&hist[0][0])[i] = 0;
+  for (int i = tid; i < SEL_WARPS * 256; i += SEL_THREADS) (&sub[0][0])[i] = 0;
   __syncthreads();
   if (want > 0) {                                  // the same in all CTAs of the cluster
     for (int pass = 0; pass < 4; ++pass) {
       const int shift = 24 - 8 * pass;
       uint32_t* hb = hist[pass & 1];
-      // lanes of equal bins add together: masses share exponents, and untouched keys are all zero
-      for (int i = from + tid - lane; i < to; i += SEL_THREADS) {
-        const int j = i + lane;
-        const uint32_t kx = j < to ? key(j) : 0u;
-        const bool in = j < to && (kx & mask) == prefix;
-        const uint32_t bin = in ? ((kx >> shift) & 255u) : 256u;
-        const uint32_t peers = __match_any_sync(0xFFFFFFFFu, bin);
-        if (in && (peers & ((1u << lane) - 1u)) == 0) atomicAdd(&hb[bin], (uint32_t)__popc(peers));
+      // the loads of a batch before its counting: a key at a time, each would wait for the one before
+      constexpr int UN = 8;
+      for (int j0 = from + tid; j0 < to; j0 += UN * SEL_THREADS) {
+        uint32_t kx[UN];
+#pragma unroll
+        for (int u = 0; u < UN; ++u) kx[u] = key(min(j0 + u * SEL_THREADS, to - 1));
+#pragma unroll
+        for (int u = 0; u < UN; ++u)
+          if (j0 + u * SEL_THREADS < to && (kx[u] & mask) == prefix) atomicAdd(&sub[warp][(kx[u] >> shift) & 255u], 1u);
       }
-      tc::cluster_sync_all();
+      __syncthreads();
+      if (tid < 256) {
+        uint32_t sum = 0;
+#pragma unroll
+        for (int w = 0; w < SEL_WARPS; ++w) { sum += sub[w][tid]; sub[w][tid] = 0; }
+        hb[tid] = sum;
+      }
+      sync_cluster();
       // total of each bin, greatest bin first: thread i holds bin 255 - i
       uint32_t total = 0;
       if (tid < 256) {
         const uint32_t a = tc::smem_u32(&hb[255 - tid]);
-        for (int c = 0; c < C; ++c) total += ld_cluster(tc::map_to_rank(a, c));
+        uint32_t part[SEL_MAX_C];
+#pragma unroll
+        for (int c = 0; c < SEL_MAX_C; ++c) part[c] = c < C ? ld_cluster(tc::map_to_rank(a, c)) : 0u;
+#pragma unroll
+        for (int c = 0; c < SEL_MAX_C; ++c) total += part[c];
       }
       uint32_t incl = total;
 #pragma unroll
@@ -89,10 +111,10 @@ select_kernel(const float* __restrict__ mass, int T, int n_sink, int n_recent, i
         if (lane >= o) incl += up;
       }
       if (lane == 31) warp_part[warp] = incl;
-      if (pass < 3 && tid >= 256) hist[(pass + 1) & 1][tid - 256] = 0;   // last read before the sync above
       __syncthreads();
       if (tid < 256) {
-        for (int w = 0; w < warp; ++w) incl += warp_part[w];
+#pragma unroll
+        for (int w = 0; w < 7; ++w) incl += w < warp ? warp_part[w] : 0u;
         if (incl >= want && incl - total < want) {
           found[0] = 255 - tid;
           found[1] = want - (incl - total);
@@ -110,83 +132,81 @@ select_kernel(const float* __restrict__ mass, int T, int n_sink, int n_recent, i
   // every warp owns a run of consecutive tokens: count, exchange, then place
   const int per = (seg + SEL_THREADS - 1) / SEL_THREADS * 32;
   const int a = min(warp * per, n), b = min(a + per, n);
+  // bit 0: kept for sure; bit 1: tied with the last kept one
+  auto look = [&](int i, uint32_t& kx) {
+    const int j = i + lane, t = t0 + j;
+    kx = key(min(j, n - 1));
+    const bool in = j < b, f = (t < n_sink) | (t >= T - n_recent);
+    return (in & (f | (kx > cut)) ? 1 : 0) | (in & !f & (kx == cut) ? 2 : 0);
+  };
   uint32_t sure = 0, tied = 0;
+#pragma unroll 8
   for (int i = a; i < b; i += 32) {
-    const int j = i + lane;
-    const bool f = j < b && forced(j);
-    const uint32_t kx = j < b ? key(j) : 0u;
-    sure += __popc(__ballot_sync(0xFFFFFFFFu, f || (j < b && kx > cut)));
-    tied += __popc(__ballot_sync(0xFFFFFFFFu, j < b && !f && kx == cut));
+    uint32_t kx;
+    const int is = look(i, kx);
+    sure += __popc(__ballot_sync(0xFFFFFFFFu, is & 1));
+    tied += __popc(__ballot_sync(0xFFFFFFFFu, is & 2));
   }
   if (lane == 0) { w_sure[warp] = sure; w_tied[warp] = tied; }
   __syncthreads();
-  if (tid == 0) {
-    uint32_t s = 0, t = 0;
-    for (int w = 0; w < SEL_WARPS; ++w) { s += w_sure[w]; t += w_tied[w]; }
-    cnt[0] = s;
-    cnt[1] = t;
+  if (warp == 0) {
+    const uint32_t s = __reduce_add_sync(0xFFFFFFFFu, lane < SEL_WARPS ? w_sure[lane] : 0u);
+    const uint32_t t = __reduce_add_sync(0xFFFFFFFFu, lane < SEL_WARPS ? w_tied[lane] : 0u);
+    if (lane == 0) { cnt[0] = s; cnt[1] = t; }
   }
-  tc::cluster_sync_all();
+  sync_cluster();
   uint32_t before_s = 0, before_t = 0;
-  for (uint32_t c = 0; c < rank; ++c) {
-    before_s += ld_cluster(tc::map_to_rank(tc::smem_u32(&cnt[0]), c));
-    before_t += ld_cluster(tc::map_to_rank(tc::smem_u32(&cnt[1]), c));
+  // lane c holds the counts of CTA c, then of warp c
+  if (lane < (int)rank) {
+    before_s = ld_cluster(tc::map_to_rank(tc::smem_u32(&cnt[0]), lane));
+    before_t = ld_cluster(tc::map_to_rank(tc::smem_u32(&cnt[1]), lane));
   }
-  for (int w = 0; w < warp; ++w) { before_s += w_sure[w]; before_t += w_tied[w]; }
+  if (lane < warp) { before_s += w_sure[lane]; before_t += w_tied[lane]; }
+  before_s = __reduce_add_sync(0xFFFFFFFFu, before_s);
+  before_t = __reduce_add_sync(0xFFFFFFFFu, before_t);
   int32_t* out = idx + (int64_t)row * budget;
   float* mo = mass_out + (int64_t)row * budget;
+#pragma unroll 8
   for (int i = a; i < b; i += 32) {
-    const int j = i + lane;
-    const bool f = j < b && forced(j);
-    const uint32_t kx = j < b ? key(j) : 0u;
-    const bool is_sure = f || (j < b && kx > cut), is_tied = j < b && !f && kx == cut;
-    const uint32_t bs = __ballot_sync(0xFFFFFFFFu, is_sure), bt = __ballot_sync(0xFFFFFFFFu, is_tied);
+    uint32_t kx;
+    const int is = look(i, kx);
+    const uint32_t bs = __ballot_sync(0xFFFFFFFFu, is & 1), bt = __ballot_sync(0xFFFFFFFFu, is & 2);
     const uint32_t below = (1u << lane) - 1u;
     const uint32_t my_s = before_s + __popc(bs & below), my_t = before_t + __popc(bt & below);
-    if (is_sure || (is_tied && my_t < ties)) {
+    if ((is & 1) | ((is & 2) != 0 & my_t < ties)) {
       const uint32_t at = my_s + min(my_t, ties);
-      out[at] = t0 + j;
-      mo[at] = m[j];
+      out[at] = t0 + i + lane;
+      mo[at] = key_mass(kx);
     }
     before_s += __popc(bs);
     before_t += __popc(bt);
   }
-  tc::cluster_sync_all();                          // nobody leaves while its counts may be read
-}
+  sync_cluster();                                  // every CTA's indices are written, and its counts read
 
-constexpr int GATHER_THREADS = 256, GATHER_UN = 4;
-
-// One thread moves GATHER_UN 16-byte chunks of K and the same chunks of V.
-__global__ void __launch_bounds__(GATHER_THREADS)
-gather_kernel(const uint4* __restrict__ k, const uint4* __restrict__ v, const int32_t* __restrict__ idx, int budget,
-              int n_kv, int log_cph, int64_t layer_ld, int64_t tok_ld, uint4* __restrict__ k_out,
-              uint4* __restrict__ v_out) {
-  pdl_trigger();
-  pdl_wait();
-  const int l = blockIdx.y;
-  const int64_t total = ((int64_t)budget * n_kv) << log_cph;
-  const int64_t base = (int64_t)blockIdx.x * (GATHER_THREADS * GATHER_UN) + threadIdx.x;
-  const int32_t* ix = idx + (int64_t)l * n_kv * budget;
-  uint4 a[GATHER_UN], b[GATHER_UN];
+  // this CTA's share of the kept tokens: lanes of a head's 16-byte chunks, COPY_UN tokens each
+  const int l = row / n_kv, h = row % n_kv, cph = 1 << log_cph, tpw = 32 >> log_cph;
+  const int b0 = (int)((int64_t)budget * rank / C), b1 = (int)((int64_t)budget * (rank + 1) / C);
+  const int64_t src0 = l * layer_ld + (int64_t)h * cph + (lane & (cph - 1));
+  const int64_t dst0 = ((int64_t)l * budget * n_kv + h) * cph + (lane & (cph - 1));
+  for (int t = b0 + warp * tpw + (lane >> log_cph); t < b1; t += SEL_WARPS * tpw * COPY_UN) {
+    uint4 x[COPY_UN], y[COPY_UN];
 #pragma unroll
-  for (int u = 0; u < GATHER_UN; ++u) {
-    const int64_t i = base + u * GATHER_THREADS;
-    if (i < total) {
-      const int64_t s = i >> log_cph;
-      const int c = (int)(i & ((1 << log_cph) - 1));
-      const int64_t o = s / n_kv;
-      const int h = (int)(s - o * n_kv);
-      const int64_t at = l * layer_ld + (int64_t)__ldg(ix + (int64_t)h * budget + o) * tok_ld + ((int64_t)h << log_cph) + c;
-      a[u] = __ldcs(k + at);
-      b[u] = __ldcs(v + at);
+    for (int u = 0; u < COPY_UN; ++u) {
+      const int tu = t + u * SEL_WARPS * tpw;
+      if (tu < b1) {
+        const int64_t at = src0 + (int64_t)__ldcg(out + tu) * tok_ld;
+        x[u] = __ldcs(k + at);
+        y[u] = __ldcs(v + at);
+      }
     }
-  }
 #pragma unroll
-  for (int u = 0; u < GATHER_UN; ++u) {
-    const int64_t i = base + u * GATHER_THREADS;
-    if (i < total) {
-      __stcs(k_out + l * total + i, a[u]);
-      __stcs(v_out + l * total + i, b[u]);
+    for (int u = 0; u < COPY_UN; ++u) {
+      const int tu = t + u * SEL_WARPS * tpw;
+      if (tu < b1) {
+        const int64_t at = dst0 + (int64_t)tu * n_kv * cph;
+        __stcs(k_out + at, x[u]);
+        __stcs(v_out + at, y[u]);
+      }
     }
   }
 }
@@ -223,7 +243,7 @@ extern "C" int32_t akvs_op_evict(int32_t dtype, const float* mass, const void* k
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   static bool attr_set = false;
   if (!attr_set) {
-    AKVS_CUDA(cudaFuncSetAttribute(select_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SEL_MAX_SEG * 4));
+    AKVS_CUDA(cudaFuncSetAttribute(evict_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SEL_MAX_SEG * 4));
     attr_set = true;
   }
   // Rows are spread over clusters while SMs would idle and a CTA's share is still worth a pass
@@ -246,16 +266,11 @@ extern "C" int32_t akvs_op_evict(int32_t dtype, const float* mass, const void* k
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  AKVS_CUDA(cudaLaunchKernelEx(&cfg, cached ? select_kernel<true> : select_kernel<false>, mass, (int)T, (int)n_sink,
-                               (int)n_recent, (int)budget, seg, idx, mass_out));
-  AKVS_LAUNCHED();
   const int64_t cph = head_dim * es / 16;              // 8, 16 or 32 chunks of a head
   const int log_cph = cph == 8 ? 3 : cph == 16 ? 4 : 5;
-  const int64_t blocks = (((int64_t)budget * n_kv_heads << log_cph) + GATHER_THREADS * GATHER_UN - 1) / (GATHER_THREADS * GATHER_UN);
-  if (blocks > 0x7fffffff) return AKVS_ERR_TOO_LARGE;
-  AKVS_CUDA(launch_pdl(gather_kernel, dim3((unsigned)blocks, (unsigned)n_layers), dim3(GATHER_THREADS), 0, st,
-                       (const uint4*)k, (const uint4*)v, (const int32_t*)idx, (int)budget, (int)n_kv_heads, log_cph,
-                       layer_ld * es / 16, tok_ld * es / 16, (uint4*)k_out, (uint4*)v_out));
+  AKVS_CUDA(cudaLaunchKernelEx(&cfg, cached ? evict_kernel<true> : evict_kernel<false>, mass, (int)T, (int)n_sink,
+                               (int)n_recent, (int)budget, seg, idx, mass_out, (const uint4*)k, (const uint4*)v,
+                               (int)n_kv_heads, log_cph, layer_ld * es / 16, tok_ld * es / 16, (uint4*)k_out, (uint4*)v_out));
   AKVS_LAUNCHED();
   return AKVS_OK;
 }
