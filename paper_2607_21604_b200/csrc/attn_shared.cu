@@ -14,23 +14,27 @@
 //     the first and runs beside it, on SMs that it leaves idle.
 //  3. The parts of a row are joined and the row is written.
 //
-// Context, 16-bit types and more than one tile of 16 stacked rows: the tcgen05 attention kernel
-// (attn_tc.cu) on 128 stacked rows per CTA, so that K and V are read once for up to 128 of them.
-// The rest, and all own tokens, are memory bound with few rows, on mma.sync m16n8k16: a warp keeps a
-// tile of 16 stacked rows and streams keys through a cp.async ring of its own (16 keys a stage, two
-// stages in flight: 128 KB per SM).  The contraction index of an mma may be permuted at will, so a
-// lane's 16-byte chunk of K and of Q supplies four of its k positions in Q K^T, and in P V a lane's
-// chunk of V supplies one column of eight tiles: fragments are plain 16-byte loads.  Probabilities
-// enter P V as a 16-bit value and the 16-bit rounding of what it lost: with one 16-bit value alone
-// the rounding of P would cost the output as much accuracy as its own final rounding.  Scores,
-// maxima, sums and O are float.
+// Context, 16-bit types and more than 16 stacked rows: the tcgen05 attention kernel (attn_tc.cu) on
+// 128 stacked rows per CTA, so that K and V are read once for up to 128 of them.  The rest, and all
+// own tokens, are memory bound with few rows, on mma.sync m16n8k16 with the ROWS along N, so that 4
+// or 5 heads fill most of a tile (with the rows along M twice as many products were issued, and
+// their rate, not the memory's, bounded the kernel):
+//     S^T = K Q^T      16 keys x 8 rows, 8 products for head_dim 128
+//     O^T += V^T P^T   16 columns x 8 rows x 16 keys, P^T turned by movmatrix
+// A warp keeps a tile of 8 or 16 stacked rows and streams keys through a cp.async ring of its own (16
+// keys a stage, two stages in flight).  The contraction index of S^T and the columns of O^T may be
+// permuted at will, so fragments are plain 16-byte loads: a lane's chunk of K and of Q supplies four
+// of its k positions, and its chunks of four V rows, paired by byte permutes, eight columns.
+// Probabilities enter P V as a 16-bit value and the 16-bit rounding of what it lost: with one 16-bit
+// value alone the rounding of P would cost the output as much accuracy as its own final rounding.
+// Scores, maxima, sums and O are float.
 #include "tc_common.cuh"
 #include <math.h>
 
 namespace {
 
 constexpr int DIR_WARPS = 4, DIR_THREADS = DIR_WARPS * 32;
-constexpr int MT = 16;                        // stacked rows of a tile (the M of one mma)
+constexpr int MT = 16;                        // stacked rows of the largest tile
 constexpr int ST = 3;                         // stages of a warp's ring, 16 keys each
 constexpr int MAX_OWN_SPLITS = 64;
 constexpr float NO_MAX = -1.0e30f;            // running maximum before any key: exp2(x - NO_MAX) is never formed for x = -inf rows
@@ -115,113 +119,135 @@ __device__ __forceinline__ void copy_chunk(uint32_t stage, const T* k, const T* 
   cp16(stage + STAGE<HD> / 2 + (row * CH + (c ^ (row & 6))) * 16, v + at, ok);
 }
 
-template <typename T, int HD>
+// P^T of 8 keys x 8 rows from the layout of S^T (a key per lane group) to that of an operand (a row per
+// lane group).
+__device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+// NT: 8 NT stacked rows.  Lane = 4 gr + t.
+template <typename T, int HD, int NT>
 struct WarpTile {
   static constexpr int KC = HD / 32, VC = HD / 64, CH = HD / 8;
-  uint32_t qa[2][KC][4];
-  int limit[2];                               // rows gr and gr + 8 see the keys below these
-  float o[VC][8][4];                          // columns 64 c + 16 t + 8 e + i of row gr + 8 s at [c][i][2 s + e]
-  float mx[2], sum[2];
+  uint32_t qb[NT][KC][4];                     // row 8 x + gr, chunk 4 c + t
+  int limit[NT][2];                           // rows 8 x + 2 t + e see the keys below these
+  float o[NT][VC][4][4];                      // row 8 x + 2 t + e, column 64 c + 8 gr + 2 i + s at [x][c][i][2 s + e]
+  float mx[NT][2], sum[NT][2];
 
   template <typename Lim>
   __device__ __forceinline__ void begin(const SharedParams& p, const Tile& tl, int end, const Lim& lim) {
     const int lane = threadIdx.x & 31, gr = lane >> 2, t = lane & 3;
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const int m = gr + 8 * s;
+    for (int x = 0; x < NT; ++x) {
+      const int m = 8 * x + gr;
       const bool ok = tl.valid(m);
       const T* q = reinterpret_cast<const T*>(p.q) + (ok ? (int64_t)tl.row(m, p.g) * p.q_ld + (int64_t)tl.head(m, p.g) * HD : 0);
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
-        const uint4 x = ok ? __ldcg(reinterpret_cast<const uint4*>(q + 32 * c + 8 * t)) : make_uint4(0u, 0u, 0u, 0u);
-        qa[s][c][0] = x.x; qa[s][c][1] = x.y; qa[s][c][2] = x.z; qa[s][c][3] = x.w;
+        const uint4 w = ok ? __ldcg(reinterpret_cast<const uint4*>(q + 32 * c + 8 * t)) : make_uint4(0u, 0u, 0u, 0u);
+        qb[x][c][0] = w.x; qb[x][c][1] = w.y; qb[x][c][2] = w.z; qb[x][c][3] = w.w;
       }
-      limit[s] = min(lim(m), end);
-      mx[s] = NO_MAX;
-      sum[s] = 0.f;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        limit[x][e] = min(lim(8 * x + 2 * t + e), end);
+        mx[x][e] = NO_MAX;
+        sum[x][e] = 0.f;
+      }
+#pragma unroll
+      for (int c = 0; c < VC; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[x][c][i][e] = 0.f;
     }
-#pragma unroll
-    for (int a = 0; a < VC; ++a)
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[a][i][e] = 0.f;
   }
 
   // 16 keys from key0, staged at `ks`; no key from `end` on exists, all rows see those below all_see.
   __device__ __forceinline__ void step(uint32_t ks, int key0, int end, int all_see, float scale_log2) {
     const int lane = threadIdx.x & 31, gr = lane >> 2, t = lane & 3;
     const uint32_t vs = ks + STAGE<HD> / 2;
-    float sc[2][4];
+    float pr[NT][4];                                // [2 half + e]: key 8 half + gr, row 2 t + e
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      sc[hf][0] = sc[hf][1] = sc[hf][2] = sc[hf][3] = 0.f;
-      const int row = hf * 8 + gr;
+    for (int x = 0; x < NT; ++x) pr[x][0] = pr[x][1] = pr[x][2] = pr[x][3] = 0.f;
 #pragma unroll
-      for (int c = 0; c < KC; ++c) {
-        const uint4 x = lds16(ks + (row * CH + ((4 * c + t) ^ ((row & 1) << 2))) * 16);
-        mma16816<T>(sc[hf], qa[0][c][0], qa[1][c][0], qa[0][c][1], qa[1][c][1], x.x, x.y);
-        mma16816<T>(sc[hf], qa[0][c][2], qa[1][c][2], qa[0][c][3], qa[1][c][3], x.z, x.w);
+    for (int c = 0; c < KC; ++c) {
+      const int at = ((4 * c + t) ^ ((gr & 1) << 2)) * 16;      // rows gr and gr + 8 exchange alike
+      const uint4 a = lds16(ks + gr * CH * 16 + at), b = lds16(ks + (gr + 8) * CH * 16 + at);
+#pragma unroll
+      for (int x = 0; x < NT; ++x) {
+        mma16816<T>(pr[x], a.x, b.x, a.y, b.y, qb[x][c][0], qb[x][c][1]);
+        mma16816<T>(pr[x], a.z, b.z, a.w, b.w, qb[x][c][2], qb[x][c][3]);
       }
     }
     const bool every = key0 + 16 <= all_see;        // all rows see all 16 keys
-    float pr[2][4];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {                   // rows gr and gr + 8
-      float x[4];
+    for (int x = 0; x < NT; ++x) {
+      float m_new[2];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int key = key0 + (e >> 1) * 8 + 2 * t + (e & 1);
-        const float y = sc[e >> 1][2 * s + (e & 1)] * scale_log2;
-        x[e] = every || key < limit[s] ? y : -INFINITY;
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          const float y = pr[x][2 * hf + e] * scale_log2;
+          pr[x][2 * hf + e] = every || key0 + 8 * hf + gr < limit[x][e] ? y : -INFINITY;
+        }
+        float top = fmaxf(pr[x][e], pr[x][2 + e]);
+        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
+        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
+        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
+        m_new[e] = fmaxf(mx[x][e], top);
       }
-      float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-      top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-      top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-      const float m_new = fmaxf(mx[s], top);
-      if (__any_sync(0xFFFFFFFFu, m_new != mx[s])) {
-        const float f = ex2(mx[s] - m_new);
-        sum[s] *= f;
+      if (__any_sync(0xFFFFFFFFu, m_new[0] != mx[x][0] || m_new[1] != mx[x][1])) {
+        const float f[2] = {ex2(mx[x][0] - m_new[0]), ex2(mx[x][1] - m_new[1])};
+        sum[x][0] *= f[0];
+        sum[x][1] *= f[1];
 #pragma unroll
-        for (int a = 0; a < VC; ++a)
+        for (int c = 0; c < VC; ++c)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            o[a][i][2 * s] *= f;
-            o[a][i][2 * s + 1] *= f;
-          }
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[x][c][i][e] *= f[e & 1];
       }
-      mx[s] = m_new;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        pr[s][e] = ex2(x[e] - m_new);
-        sum[s] += pr[s][e];
+      for (int e = 0; e < 2; ++e) {
+        mx[x][e] = m_new[e];
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          pr[x][2 * hf + e] = ex2(pr[x][2 * hf + e] - m_new[e]);
+          sum[x][e] += pr[x][2 * hf + e];
+        }
       }
     }
     if (every || all_see >= end) {
-      uint32_t hi[4], lo[4];                        // A operand: (row, keys 2t..), (row + 8, ..), keys + 8
+      uint32_t hi[NT][2], lo[NT][2];                // B operand: keys 2 t, 2 t + 1 (and + 8) of row gr
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int s = i & 1, e = (i >> 1) * 2;
-        hi[i] = pack2<T>(pr[s][e], pr[s][e + 1]);
-        const float2 h2 = unpack2<T>(hi[i]);
-        lo[i] = pack2<T>(pr[s][e] - h2.x, pr[s][e + 1] - h2.y);
-      }
+      for (int x = 0; x < NT; ++x)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          const uint32_t h = pack2<T>(pr[x][2 * hf], pr[x][2 * hf + 1]);
+          const float2 h2 = unpack2<T>(h);
+          hi[x][hf] = turn8x8(h);
+          lo[x][hf] = turn8x8(pack2<T>(pr[x][2 * hf] - h2.x, pr[x][2 * hf + 1] - h2.y));
+        }
 #pragma unroll
       for (int c = 0; c < VC; ++c) {
-        uint32_t w[4][4];
+        uint32_t w[4][4];                           // rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9; columns 64 c + 8 gr ..
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int row = 2 * t + (i & 1) + (i >> 1) * 8;
-          const uint4 x = lds16(vs + (row * CH + ((8 * c + gr) ^ (row & 6))) * 16);
-          w[i][0] = x.x; w[i][1] = x.y; w[i][2] = x.z; w[i][3] = x.w;
+          const uint4 v = lds16(vs + (row * CH + ((8 * c + gr) ^ (row & 6))) * 16);
+          w[i][0] = v.x; w[i][1] = v.y; w[i][2] = v.z; w[i][3] = v.w;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint32_t sel = (i & 1) ? 0x7632u : 0x5410u;
-          const uint32_t b0 = __byte_perm(w[0][i >> 1], w[1][i >> 1], sel);
-          const uint32_t b1 = __byte_perm(w[2][i >> 1], w[3][i >> 1], sel);
-          mma16816<T>(o[c][i], hi[0], hi[1], hi[2], hi[3], b0, b1);
-          mma16816<T>(o[c][i], lo[0], lo[1], lo[2], lo[3], b0, b1);
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t a0 = __byte_perm(w[0][i], w[1][i], 0x5410u), a1 = __byte_perm(w[0][i], w[1][i], 0x7632u);
+          const uint32_t a2 = __byte_perm(w[2][i], w[3][i], 0x5410u), a3 = __byte_perm(w[2][i], w[3][i], 0x7632u);
+#pragma unroll
+          for (int x = 0; x < NT; ++x) {
+            mma16816<T>(o[x][c][i], a0, a1, a2, a3, hi[x][0], hi[x][1]);
+            mma16816<T>(o[x][c][i], a0, a1, a2, a3, lo[x][0], lo[x][1]);
+          }
         }
       }
     } else {
@@ -230,56 +256,55 @@ struct WarpTile {
       for (int kk = 0; kk < 16; ++kk) {
         const int key = key0 + kk;
         if (key >= end) break;
-        const int src = (lane & ~3) | ((kk & 7) >> 1);
-        const int e = (kk >> 3) * 2 + (kk & 1);
-        float pa = e == 0 ? pr[0][0] : e == 1 ? pr[0][1] : e == 2 ? pr[0][2] : pr[0][3];
-        float pb = e == 0 ? pr[1][0] : e == 1 ? pr[1][1] : e == 2 ? pr[1][2] : pr[1][3];
-        pa = __shfl_sync(0xFFFFFFFFu, pa, src);
-        pb = __shfl_sync(0xFFFFFFFFu, pb, src);
+        float v[VC][8];
 #pragma unroll
         for (int c = 0; c < VC; ++c) {
-          float x[2][8];
+          const uint4 w = lds16(vs + (kk * CH + ((8 * c + gr) ^ (kk & 6))) * 16);
+          const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const uint4 w = lds16(vs + (kk * CH + ((8 * c + 2 * t + b) ^ (kk & 6))) * 16);
-            const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float2 y = unpack2<T>(ws[i]);
-              x[b][2 * i] = y.x;
-              x[b][2 * i + 1] = y.y;
-            }
+          for (int i = 0; i < 4; ++i) {
+            const float2 y = unpack2<T>(ws[i]);
+            v[c][2 * i] = y.x;
+            v[c][2 * i + 1] = y.y;
           }
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int e2 = 0; e2 < 2; ++e2) {
-              if (key < limit[0]) o[c][i][e2] = fmaf(pa, x[e2][i], o[c][i][e2]);
-              if (key < limit[1]) o[c][i][2 + e2] = fmaf(pb, x[e2][i], o[c][i][2 + e2]);
-            }
         }
+#pragma unroll
+        for (int x = 0; x < NT; ++x)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float y = __shfl_sync(0xFFFFFFFFu, kk < 8 ? pr[x][e] : pr[x][2 + e], (kk & 7) * 4 + t);
+            if (key < limit[x][e])
+#pragma unroll
+              for (int c = 0; c < VC; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[x][c][i >> 1][2 * (i & 1) + e] = fmaf(y, v[c][i], o[x][c][i >> 1][2 * (i & 1) + e]);
+          }
       }
     }
   }
 
   __device__ __forceinline__ void finish() {
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      sum[s] += __shfl_xor_sync(0xFFFFFFFFu, sum[s], 1);
-      sum[s] += __shfl_xor_sync(0xFFFFFFFFu, sum[s], 2);
-    }
+    for (int x = 0; x < NT; ++x)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        sum[x][e] += __shfl_xor_sync(0xFFFFFFFFu, sum[x][e], 4);
+        sum[x][e] += __shfl_xor_sync(0xFFFFFFFFu, sum[x][e], 8);
+        sum[x][e] += __shfl_xor_sync(0xFFFFFFFFu, sum[x][e], 16);
+      }
   }
 
-  // four columns of row gr + 8 s: 64 c + 16 t + 8 e + i ..
-  __device__ __forceinline__ float4 quad(int c, int s, int e, int i, float f) const {
-    return make_float4(o[c][i][2 * s + e] * f, o[c][i + 1][2 * s + e] * f, o[c][i + 2][2 * s + e] * f, o[c][i + 3][2 * s + e] * f);
+  // columns 64 c + 8 gr + 4 half .. of row 8 x + 2 t + e
+  __device__ __forceinline__ float4 quad(int x, int e, int c, int half, float f) const {
+    return make_float4(o[x][c][2 * half][e] * f, o[x][c][2 * half][2 + e] * f, o[x][c][2 * half + 1][e] * f,
+                       o[x][c][2 * half + 1][2 + e] * f);
   }
 };
 
 // A warp alone: keys start, start + step, ... (16 at a time) below `end`, through its own ring.
-template <typename T, int HD, typename Lim>
+template <typename T, int HD, int NT, typename Lim>
 __device__ __forceinline__ void warp_core(const SharedParams& p, const Tile& tl, const T* k, const T* v, int64_t ld, int start,
-                                          int end, int step, int all_see, const Lim& lim, uint32_t ring, WarpTile<T, HD>& wt) {
+                                          int end, int step, int all_see, const Lim& lim, uint32_t ring, WarpTile<T, HD, NT>& wt) {
   constexpr int CH = HD / 8;
   const int lane = threadIdx.x & 31;
   auto issue = [&](int n) {
@@ -318,67 +343,68 @@ __device__ __forceinline__ void store_ml(const SharedParams& p, const Tile& tl, 
 }
 
 // A warp's whole tile into scratch, from its registers.
-template <typename T, int HD>
-__device__ __forceinline__ void store_tile(const SharedParams& p, const Tile& tl, int part, const WarpTile<T, HD>& wt) {
+template <typename T, int HD, int NT>
+__device__ __forceinline__ void store_tile(const SharedParams& p, const Tile& tl, int part, const WarpTile<T, HD, NT>& wt) {
   const int lane = threadIdx.x & 31, gr = lane >> 2, t = lane & 3;
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    const int m = gr + 8 * s;
-    if (!tl.valid(m)) continue;
+  for (int x = 0; x < NT; ++x)
 #pragma unroll
-    for (int c = 0; c < HD / 64; ++c)
+    for (int e = 0; e < 2; ++e) {
+      const int m = 8 * x + 2 * t + e;
+      if (!tl.valid(m)) continue;
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+      for (int c = 0; c < HD / 64; ++c)
 #pragma unroll
-        for (int i = 0; i < 8; i += 4) store_part<HD>(p, tl, part, m, 64 * c + 16 * t + 8 * e + i, wt.quad(c, s, e, i, 1.f));
-    if (t == 0) store_ml(p, tl, part, m, wt.mx[s], wt.sum[s]);
-  }
+        for (int half = 0; half < 2; ++half) store_part<HD>(p, tl, part, m, 64 * c + 8 * gr + 4 * half, wt.quad(x, e, c, half, 1.f));
+      if (gr == 0) store_ml(p, tl, part, m, wt.mx[x][e], wt.sum[x][e]);
+    }
 }
 
 // One tile, the CTA's warps taking turns over its keys; joins them and leaves the part in scratch.
-template <typename T, int HD, typename Lim>
+template <typename T, int HD, int NT, typename Lim>
 __device__ __forceinline__ void cta_part(const SharedParams& p, const Tile& tl, const T* k, const T* v, int64_t ld, int start,
                                          int end, int all_see, const Lim& lim, uint8_t* smem, int part) {
-  __shared__ float wm[DIR_WARPS][MT], wl[DIR_WARPS][MT];
-  constexpr int LD = HD + 4;                  // 16-byte rows that start in different banks
+  constexpr int TR = 8 * NT, LD = HD + 4;     // 16-byte rows that start in different banks
+  __shared__ float wm[DIR_WARPS][TR], wl[DIR_WARPS][TR];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gr = lane >> 2, t = lane & 3;
   float* raw = reinterpret_cast<float*>(smem);
-  WarpTile<T, HD> acc;
-  warp_core<T, HD>(p, tl, k, v, ld, start + warp * 16, end, DIR_WARPS * 16, all_see, lim,
-                   tc::smem_u32(smem) + warp * ST * STAGE<HD>, acc);
-  if (t == 0)
+  WarpTile<T, HD, NT> acc;
+  warp_core<T, HD, NT>(p, tl, k, v, ld, start + warp * 16, end, DIR_WARPS * 16, all_see, lim,
+                       tc::smem_u32(smem) + warp * ST * STAGE<HD>, acc);
+  if (gr == 0)
 #pragma unroll
-    for (int s = 0; s < 2; ++s) { wm[warp][gr + 8 * s] = acc.mx[s]; wl[warp][gr + 8 * s] = acc.sum[s]; }
+    for (int x = 0; x < NT; ++x)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) { wm[warp][8 * x + 2 * t + e] = acc.mx[x][e]; wl[warp][8 * x + 2 * t + e] = acc.sum[x][e]; }
   __syncthreads();                            // the rings become the warps' rows of O
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    const int m = gr + 8 * s;
-    float top = wm[0][m];
+  for (int x = 0; x < NT; ++x)
 #pragma unroll
-    for (int w = 1; w < DIR_WARPS; ++w) top = fmaxf(top, wm[w][m]);
-    const float f = ex2(acc.mx[s] - top);
-    float* dst = raw + (warp * MT + m) * LD + 16 * t;
+    for (int e = 0; e < 2; ++e) {
+      const int m = 8 * x + 2 * t + e;
+      float top = wm[0][m];
 #pragma unroll
-    for (int c = 0; c < HD / 64; ++c)
+      for (int w = 1; w < DIR_WARPS; ++w) top = fmaxf(top, wm[w][m]);
+      const float f = ex2(acc.mx[x][e] - top);
+      float* dst = raw + (warp * TR + m) * LD + 8 * gr;
 #pragma unroll
-      for (int i = 0; i < 8; i += 4)
+      for (int c = 0; c < HD / 64; ++c)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-          *reinterpret_cast<float4*>(dst + 64 * c + 8 * e + i) = acc.quad(c, s, e, i, f);
-  }
+        for (int half = 0; half < 2; ++half) *reinterpret_cast<float4*>(dst + 64 * c + 4 * half) = acc.quad(x, e, c, half, f);
+    }
   __syncthreads();
-  for (int i = threadIdx.x; i < MT * HD / 4; i += DIR_THREADS) {
+  for (int i = threadIdx.x; i < TR * HD / 4; i += DIR_THREADS) {
     const int m = i / (HD / 4), c4 = i % (HD / 4) * 4;
     if (!tl.valid(m)) continue;
     float4 a = *reinterpret_cast<const float4*>(raw + m * LD + c4);
 #pragma unroll
     for (int w = 1; w < DIR_WARPS; ++w) {
-      const float4 b = *reinterpret_cast<const float4*>(raw + (w * MT + m) * LD + c4);
+      const float4 b = *reinterpret_cast<const float4*>(raw + (w * TR + m) * LD + c4);
       a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
     }
     store_part<HD>(p, tl, part, m, c4, a);
   }
-  if (threadIdx.x < MT && tl.valid(threadIdx.x)) {
+  if (threadIdx.x < TR && tl.valid(threadIdx.x)) {
     const int m = threadIdx.x;
     float top = wm[0][m], l = 0.f;
     for (int w = 1; w < DIR_WARPS; ++w) top = fmaxf(top, wm[w][m]);
@@ -483,21 +509,21 @@ template <typename T, int HD> constexpr int direct_smem() {
   return std::is_same<T, float>::value ? (2 * FK * (HD + 4) + MT * (HD + 4) + MT * (FK + 1)) * 4 : DIR_WARPS * ST * STAGE<HD>;
 }
 
-template <typename T, int HD, typename Lim>
+template <typename T, int HD, int NT, typename Lim>
 __device__ __forceinline__ void tile_part(const SharedParams& p, const Tile& tl, const T* k, const T* v, int64_t ld, int start,
                                           int end, int all_see, const Lim& lim, uint8_t* smem, int part) {
   if constexpr (std::is_same<T, float>::value)
     cta_part_f32<HD>(p, tl, k, v, ld, start, end, lim, smem, part);
   else
-    cta_part<T, HD>(p, tl, k, v, ld, start, end, all_see, lim, smem, part);
+    cta_part<T, HD, NT>(p, tl, k, v, ld, start, end, all_see, lim, smem, part);
 }
 
-// ---- 1. context, one split of it, for a tile of 16 stacked rows
-template <typename T, int HD>
+// ---- 1. context, one split of it, for one tile of stacked rows
+template <typename T, int HD, int NT>
 __device__ __forceinline__ void context_tile(const SharedParams& p, int split, int h, int tile, uint8_t* smem) {
-  const Tile tl{0, tile * MT, p.R * p.g, h};
+  const Tile tl{0, tile * 8 * NT, p.R * p.g, h};
   const int start = split * p.split_len, end = min(start + p.split_len, p.P);
-  tile_part<T, HD>(p, tl, (const T*)p.pk + (int64_t)h * HD, (const T*)p.pv + (int64_t)h * HD, p.p_ld, start, end, end,
+  tile_part<T, HD, NT>(p, tl, (const T*)p.pk + (int64_t)h * HD, (const T*)p.pv + (int64_t)h * HD, p.p_ld, start, end, end,
                    [&](int) { return end; }, smem, split);
 }
 
@@ -518,34 +544,34 @@ __device__ __forceinline__ Seq sequence(const SharedParams& p, int s) {
 
 // ---- 2. own tokens of a sequence, one split of them, tile z of nz in flight.
 // WIDE (sequences of many rows, one split): every warp has a tile of its own and runs all its keys.
-template <typename T, int HD, bool WIDE>
+template <typename T, int HD, int NT, bool WIDE>
 __device__ __forceinline__ void own_tiles(const SharedParams& p, int s, int split, int h, int z, int nz, uint8_t* smem) {
   const Seq sq = sequence(p, s);
   const T* k = (const T*)p.sk + (int64_t)s * p.s_seq + (int64_t)h * HD;
   const T* v = (const T*)p.sv + (int64_t)s * p.s_seq + (int64_t)h * HD;
   const int count = sq.n * p.g;
-  constexpr int TILES = WIDE ? DIR_WARPS : 1;
+  constexpr int TILES = WIDE ? DIR_WARPS : 1, TR = 8 * NT;
   const int warp = threadIdx.x >> 5;
-  for (int j0 = (z * TILES + (WIDE ? warp : 0)) * MT; j0 < count; j0 += nz * TILES * MT) {
+  for (int j0 = (z * TILES + (WIDE ? warp : 0)) * TR; j0 < count; j0 += nz * TILES * TR) {
     const Tile tl{sq.r0, j0, count, h};
     // row i of the sequence sees len - (n - 1 - i) own tokens: the tile's first row the fewest
     auto lim = [&](int m) { return tl.valid(m) ? sq.len - (sq.n - 1 - (j0 + m) / p.g) : sq.len; };
-    const int most = max(0, lim(min(MT, count - j0) - 1)), fewest = max(0, lim(0));
+    const int most = max(0, lim(min(TR, count - j0) - 1)), fewest = max(0, lim(0));
     if constexpr (WIDE) {
-      WarpTile<T, HD> wt;
-      warp_core<T, HD>(p, tl, k, v, p.s_ld, 0, most, 16, min(fewest, most), lim, tc::smem_u32(smem) + warp * ST * STAGE<HD>, wt);
-      store_tile<T, HD>(p, tl, p.splits, wt);
+      WarpTile<T, HD, NT> wt;
+      warp_core<T, HD, NT>(p, tl, k, v, p.s_ld, 0, most, 16, min(fewest, most), lim, tc::smem_u32(smem) + warp * ST * STAGE<HD>, wt);
+      store_tile<T, HD, NT>(p, tl, p.splits, wt);
       __syncwarp();                           // the ring is read
     } else {
       const int chunk = ((most + p.own_splits - 1) / p.own_splits + 63) / 64 * 64;
       const int start = min(split * chunk, most), end = min(start + chunk, most);
-      tile_part<T, HD>(p, tl, k, v, p.s_ld, start, end, min(fewest, end), lim, smem, p.splits + split);
+      tile_part<T, HD, NT>(p, tl, k, v, p.s_ld, start, end, min(fewest, end), lim, smem, p.splits + split);
     }
   }
 }
 
 // beside the tcgen05 kernel: grid (sequence * own split, kv head, tiles in flight)
-template <typename T, int HD, bool WIDE>
+template <typename T, int HD, int NT, bool WIDE>
 __global__ void __launch_bounds__(DIR_THREADS)
 own_kernel(const __grid_constant__ SharedParams p) {
   extern __shared__ __align__(16) uint8_t smem[];
@@ -554,13 +580,13 @@ own_kernel(const __grid_constant__ SharedParams p) {
   // there.  Without a context the kernel before is a stranger: wait for it first.
   if (p.splits == 0) pdl_wait();
   pdl_trigger();
-  own_tiles<T, HD, WIDE>(p, blockIdx.x / p.own_splits, blockIdx.x % p.own_splits, blockIdx.y, blockIdx.z, gridDim.z, smem);
+  own_tiles<T, HD, NT, WIDE>(p, blockIdx.x / p.own_splits, blockIdx.x % p.own_splits, blockIdx.y, blockIdx.z, gridDim.z, smem);
   // The join waits for this grid alone: its last CTA ends after the context's kernel.
   if (blockIdx.x == gridDim.x - 1 && blockIdx.y == gridDim.y - 1 && blockIdx.z == gridDim.z - 1) pdl_wait();
 }
 
 // context and own tokens in one launch: the first n_ctx CTAs of a kv head take the context
-template <typename T, int HD, bool WIDE>
+template <typename T, int HD, int NT, bool WIDE>
 __global__ void __launch_bounds__(DIR_THREADS)
 direct_kernel(const __grid_constant__ SharedParams p, int n_ctx, int own_z) {
   extern __shared__ __align__(16) uint8_t smem[];
@@ -568,11 +594,11 @@ direct_kernel(const __grid_constant__ SharedParams p, int n_ctx, int own_z) {
   pdl_trigger();                              // after the wait: the join reads lengths and offsets without its own
   int x = blockIdx.x;
   if (x < n_ctx) {
-    context_tile<T, HD>(p, x % p.splits, blockIdx.y, x / p.splits, smem);
+    context_tile<T, HD, NT>(p, x % p.splits, blockIdx.y, x / p.splits, smem);
   } else {
     x -= n_ctx;
     const int z = x % own_z, sx = x / own_z;
-    own_tiles<T, HD, WIDE>(p, sx / p.own_splits, sx % p.own_splits, blockIdx.y, z, own_z, smem);
+    own_tiles<T, HD, NT, WIDE>(p, sx / p.own_splits, sx % p.own_splits, blockIdx.y, z, own_z, smem);
   }
 }
 
@@ -661,11 +687,11 @@ join_kernel(const __grid_constant__ SharedParams p) {
   }
 }
 
-struct Plan { bool tc; int splits, split_len, own_splits; bool wide; int z; };
+struct Plan { bool tc; int splits, split_len, own_splits; bool wide; int nt, z; };      // nt: tiles of 8 nt rows
 
 // How the context and the own tokens are cut.
 Plan make_plan(bool is16, int R, int P, int S, int cap, int g, int n_kv, int hd, bool ragged) {
-  Plan pl = {false, 0, 0, 0, false, 1};
+  Plan pl = {false, 0, 0, 0, false, 2, 1};
   if (R == 0 || S == 0) return pl;
   // Up to one tile of stacked rows on mma.sync, more on tcgen05: over 12416 tokens of 8 kv heads one
   // tile takes 16.2 us on mma.sync, two tiles 22.0 us against 18.9 us on tcgen05, four 42.8 against 21.8.
@@ -685,8 +711,9 @@ Plan make_plan(bool is16, int R, int P, int S, int cap, int g, int n_kv, int hd,
     pl.split_len = akvs_cdiv(tiles, best) * 128;
   } else if (P > 0) {
     // Two CTAs fit an SM; one runs 64 keys at a time (32 of the float kernel).
+    if (is16 && (int64_t)R * g <= 8) pl.nt = 1;
     const int unit = is16 ? 64 : 32;
-    const int64_t base = (int64_t)n_kv * akvs_cdiv((int64_t)R * g, MT);
+    const int64_t base = (int64_t)n_kv * akvs_cdiv((int64_t)R * g, 8 * pl.nt);
     const int units = akvs_cdiv(P, unit);
     const int splits = (int)(base >= 296 ? 1 : akvs_cdiv(296, base));
     pl.split_len = akvs_cdiv(units, splits < units ? splits : units) * unit;
@@ -696,7 +723,8 @@ Plan make_plan(bool is16, int R, int P, int S, int cap, int g, int n_kv, int hd,
   // the mean at once, and a CTA walks what is left.
   const int64_t stacked = ragged ? (int64_t)akvs_cdiv(R, S) * g * 2 : g;
   pl.wide = is16 && ragged && (int64_t)akvs_cdiv(R, S) * g > MT;
-  const int64_t tiles = (stacked + MT - 1) / MT, z = pl.wide ? (tiles + DIR_WARPS - 1) / DIR_WARPS : tiles;
+  if (is16 && (P == 0 || pl.tc) && !ragged && g <= 8) pl.nt = 1;
+  const int64_t tiles = (stacked + 8 * pl.nt - 1) / (8 * pl.nt), z = pl.wide ? (tiles + DIR_WARPS - 1) / DIR_WARPS : tiles;
   pl.z = (int)(z < 64 ? z : 64);
   if (cap > 0) {
     pl.own_splits = 1;
@@ -713,32 +741,32 @@ int64_t parts_bytes(const Plan& pl, int R, int n_q, int hd) {
   return akvs_align_up(rows * hd * 4, 256) + akvs_align_up(rows * 8, 256) + 256;
 }
 
-template <typename T, int HD, bool WIDE>
+template <typename T, int HD, int NT, bool WIDE>
 int32_t launch_direct(const SharedParams& p, const Plan& pl, cudaStream_t st) {
   constexpr int smem = direct_smem<T, HD>();
   static bool attr_set = false;
   if (!attr_set) {
-    AKVS_CUDA(cudaFuncSetAttribute(direct_kernel<T, HD, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    AKVS_CUDA(cudaFuncSetAttribute(direct_kernel<T, HD, NT, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     attr_set = true;
   }
-  const int64_t n_ctx = (int64_t)p.splits * akvs_cdiv((int64_t)p.R * p.g, MT);
+  const int64_t n_ctx = (int64_t)p.splits * akvs_cdiv((int64_t)p.R * p.g, 8 * NT);
   const int64_t grid = n_ctx + (int64_t)p.S * p.own_splits * pl.z;
   if (grid > 0x7fffffff) return AKVS_ERR_TOO_LARGE;
-  AKVS_CUDA(launch_pdl(direct_kernel<T, HD, WIDE>, dim3((unsigned)grid, p.n_kv), dim3(DIR_THREADS), smem, st, p, (int)n_ctx,
+  AKVS_CUDA(launch_pdl(direct_kernel<T, HD, NT, WIDE>, dim3((unsigned)grid, p.n_kv), dim3(DIR_THREADS), smem, st, p, (int)n_ctx,
                        pl.z));
   AKVS_LAUNCHED();
   return AKVS_OK;
 }
 
-template <typename T, int HD, bool WIDE>
+template <typename T, int HD, int NT, bool WIDE>
 int32_t launch_own(const SharedParams& p, const Plan& pl, cudaStream_t st) {
   constexpr int smem = direct_smem<T, HD>();
   static bool attr_set = false;
   if (!attr_set) {
-    AKVS_CUDA(cudaFuncSetAttribute(own_kernel<T, HD, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    AKVS_CUDA(cudaFuncSetAttribute(own_kernel<T, HD, NT, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     attr_set = true;
   }
-  AKVS_CUDA(launch_pdl(own_kernel<T, HD, WIDE>, dim3((unsigned)(p.S * p.own_splits), p.n_kv, pl.z), dim3(DIR_THREADS), smem, st, p));
+  AKVS_CUDA(launch_pdl(own_kernel<T, HD, NT, WIDE>, dim3((unsigned)(p.S * p.own_splits), p.n_kv, pl.z), dim3(DIR_THREADS), smem, st, p));
   AKVS_LAUNCHED();
   return AKVS_OK;
 }
@@ -750,15 +778,17 @@ int32_t run(SharedParams& p, int dtype, const Plan& pl, cudaStream_t st) {
       AKVS_TRY(launch_attention_parts_tc(dtype, HD, p.q, p.q_ld, p.pk, p.pv, p.p_ld, p.R, p.P, p.n_q, p.n_kv, p.split_len,
                                          p.part_o, p.part_ml, st));
       if (p.own_splits > 0) {
-        if (pl.wide) AKVS_TRY((launch_own<T, HD, true>(p, pl, st)));
-        else AKVS_TRY((launch_own<T, HD, false>(p, pl, st)));
+        if (pl.wide) AKVS_TRY((launch_own<T, HD, 2, true>(p, pl, st)));
+        else if (pl.nt == 2) AKVS_TRY((launch_own<T, HD, 2, false>(p, pl, st)));
+        else AKVS_TRY((launch_own<T, HD, 1, false>(p, pl, st)));
       }
     } else if (p.splits + p.own_splits > 0) {
-      if (pl.wide) AKVS_TRY((launch_direct<T, HD, true>(p, pl, st)));
-      else AKVS_TRY((launch_direct<T, HD, false>(p, pl, st)));
+      if (pl.wide) AKVS_TRY((launch_direct<T, HD, 2, true>(p, pl, st)));
+      else if (pl.nt == 2) AKVS_TRY((launch_direct<T, HD, 2, false>(p, pl, st)));
+      else AKVS_TRY((launch_direct<T, HD, 1, false>(p, pl, st)));
     }
   } else if (p.splits + p.own_splits > 0) {
-    AKVS_TRY((launch_direct<T, HD, false>(p, pl, st)));
+    AKVS_TRY((launch_direct<T, HD, 2, false>(p, pl, st)));
   }
   // Few rows with many parts: four warps share a row's parts.  CTAs in flight: what the SMs hold at a
   // time; more of them would start late and find little.
