@@ -479,6 +479,7 @@ def op_quantize(x, bits):
 # checks below read every tensor's shape, strides and device once and build no objects.
 
 _CODE = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+_PACKED = torch.contiguous_format
 _device = torch._C._cuda_getDevice                     # the current device, without the lookup of its properties
 _raw_stream = torch._C._cuda_getCurrentRawStream       # the current stream's handle, without a Stream object
 
@@ -508,8 +509,8 @@ def op_qk_norm_rope(q, k, q_gain, k_gain, pos, eps, base, q_out=None, k_out=None
     pos [n]; rows may be strided (column ranges of one projection).  q_out / k_out may be q / k."""
     w = "akvs_op_qk_norm_rope"
     dev, dt, qs, ks = _current(w, q.get_device()), q.dtype, q.shape, k.shape
-    q_out = q.new_empty(qs) if q_out is None else q_out
-    k_out = q.new_empty(ks) if k_out is None else k_out
+    q_out = torch.empty_like(q, memory_format=_PACKED) if q_out is None else q_out
+    k_out = torch.empty_like(k, memory_format=_PACKED) if k_out is None else k_out
     if not (dev == k.get_device() == q_gain.get_device() == k_gain.get_device() == pos.get_device() == q_out.get_device()
             == k_out.get_device()):
         _refuse(w)
@@ -569,7 +570,7 @@ def op_attention_shared(q, ctx_k, ctx_v, own_k, own_v, own_len, q_off=None, out=
         off = q_off.data_ptr()
     if scratch is None:
         need = lib.akvs_op_attention_shared_scratch_bytes(_CODE[dt], R, P, S, cap, nq, nkv, hd)
-        scratch = torch.empty(max(need, 0), dtype=torch.uint8, device=q.device)
+        scratch = lse.new_empty(max(need, 0) // 4)
     elif scratch.get_device() != dev or not scratch.is_contiguous():
         _refuse(w)
     _chk(lib.akvs_op_attention_shared(_CODE[dt], q.data_ptr(), _ld(w, qs, q.stride()), R, ctx_k.data_ptr(),
@@ -587,7 +588,8 @@ def op_attention_mass(q, k, lse, k_lo, k_hi, mass=None, out=None):
     w = "akvs_op_attention_mass"
     dev, dt, qs, ks = _current(w, q.get_device()), q.dtype, q.shape, k.shape
     (R, nq, hd), (T, nkv, _) = qs, ks
-    out = lse.new_empty((nkv, T)) if out is None else out
+    if out is None:
+        out = lse.new_empty((nkv, T)) if mass is None else torch.empty_like(mass, memory_format=_PACKED)
     if not (dev == k.get_device() == lse.get_device() == k_lo.get_device() == k_hi.get_device() == out.get_device()):
         _refuse(w)
     if not (dt in _CODE and dt == k.dtype and lse.dtype == out.dtype == torch.float32

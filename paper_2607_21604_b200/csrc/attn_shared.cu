@@ -694,7 +694,7 @@ Plan make_plan(bool is16, int R, int P, int S, int cap, int g, int n_kv, int hd,
   Plan pl = {false, 0, 0, 0, false, 2, 1};
   if (R == 0 || S == 0) return pl;
   // Up to one tile of stacked rows on mma.sync, more on tcgen05: over 12416 tokens of 8 kv heads one
-  // tile takes 16.2 us on mma.sync, two tiles 22.0 us against 18.9 us on tcgen05, four 42.8 against 21.8.
+  // tile takes 17.2 us on mma.sync, two tiles 22.0 us against 18.3 us on tcgen05, four 42.8 against 20.8.
   if (P > 0 && is16 && (int64_t)R * g > MT) {
     // One CTA per SM.  In units of a key tile (0.85 us): rounds of CTAs times (a CTA's tiles + 9 for its
     // start and end), plus writing and reading the parts at memory speed.
@@ -703,7 +703,7 @@ Plan make_plan(bool is16, int R, int P, int S, int cap, int g, int n_kv, int hd,
     const double part = 2.0 * R * g * n_kv * (hd + 2) * 4 / 6.4e6 / 0.85;
     int best = 1;
     double best_cost = 1e300;
-    for (int s = 1; s <= tiles && s <= 148; ++s) {
+    for (int s = 1; s <= tiles && (s == 1 || base * s <= 3 * 148); ++s) {
       const double cost = (double)((base * s + 147) / 148) * (akvs_cdiv(tiles, s) + 9) + part * s;
       if (cost < best_cost) { best_cost = cost; best = s; }
     }
