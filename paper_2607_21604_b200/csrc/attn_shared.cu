@@ -697,14 +697,17 @@ Plan make_plan(bool is16, int R, int P, int S, int cap, int g, int n_kv, int hd,
   // tile takes 17.2 us on mma.sync, two tiles 22.0 us against 18.3 us on tcgen05, four 42.8 against 20.8.
   if (P > 0 && is16 && (int64_t)R * g > MT) {
     // One CTA per SM.  In units of a key tile (0.85 us): rounds of CTAs times (a CTA's tiles + 9 for its
-    // start and end), plus writing and reading the parts at memory speed.
+    // start and end), plus writing and reading the parts at memory speed.  A last round that is not
+    // full counts half of what it leaves idle: own tokens and the next CTAs' starts use some of it
+    // (58 row blocks x 2 heads over 128 tiles, 1 / 2 / 4 / 5 / 14 splits: 150 / 144 / 155 / 152 / 209 us).
     const int64_t base = (int64_t)akvs_cdiv(R, 128 / g) * n_kv;
     const int tiles = akvs_cdiv(P, 128);
     const double part = 2.0 * R * g * n_kv * (hd + 2) * 4 / 6.4e6 / 0.85;
     int best = 1;
     double best_cost = 1e300;
     for (int s = 1; s <= tiles && (s == 1 || base * s <= 3 * 148); ++s) {
-      const double cost = (double)((base * s + 147) / 148) * (akvs_cdiv(tiles, s) + 9) + part * s;
+      const double full = (double)((base * s + 147) / 148), used = base * s / 148.0;
+      const double cost = 0.5 * (full + (used > 1.0 ? used : 1.0)) * (akvs_cdiv(tiles, s) + 9) + part * s;
       if (cost < best_cost) { best_cost = cost; best = s; }
     }
     pl.tc = true;
