@@ -577,8 +577,7 @@ own_kernel(const __grid_constant__ SharedParams p) {
   extern __shared__ __align__(16) uint8_t smem[];
   // A CTA of this kernel starts once every CTA of the context's kernel has passed its own wait, so
   // q, the own tokens, lengths and offsets (older than that kernel) are complete in L2 and are read
-  // there.  Without a context the kernel before is a stranger: wait for it first.
-  if (p.splits == 0) pdl_wait();
+  // there.
   pdl_trigger();
   own_tiles<T, HD, NT, WIDE>(p, blockIdx.x / p.own_splits, blockIdx.x % p.own_splits, blockIdx.y, blockIdx.z, gridDim.z, smem);
   // The join waits for this grid alone: its last CTA ends after the context's kernel.
@@ -610,9 +609,11 @@ join_kernel(const __grid_constant__ SharedParams p) {
   __shared__ float jo[DIR_WARPS][HD], jm[DIR_WARPS], jl[DIR_WARPS];
   pdl_trigger();
   const int s = blockIdx.x, h = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % WPR;
+  const int parts = p.splits + p.own_splits;
+  if (parts == 0) pdl_wait();                 // no kernel of this call before this one: a stranger's results
   const Seq sq = sequence(p, s);              // older than the kernels before, which have started: no wait
   pdl_wait();
-  const int parts = p.splits + p.own_splits, mine = parts > sub ? (parts - sub + WPR - 1) / WPR : 0;
+  const int mine = parts > sub ? (parts - sub + WPR - 1) / WPR : 0;
   const int64_t rows = (int64_t)p.R * p.n_q;
   const int count = sq.n * p.g;
   for (int j0 = blockIdx.z * RPC; j0 < count; j0 += gridDim.z * RPC) {

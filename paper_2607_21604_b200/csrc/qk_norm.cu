@@ -165,6 +165,13 @@ extern "C" int32_t akvs_op_qk_norm_rope(int32_t dtype, const void* q, int64_t q_
     if (ld[i] < row || ld_out[i] < row) return AKVS_ERR_SHAPE;
     if (!aligned16(in[i]) || !aligned16(out[i]) || ld[i] * es % 16 || ld_out[i] * es % 16) return AKVS_ERR_INVALID_ARG;
   }
+  for (int o = 0; o < 2; ++o) {
+    if (heads[o] == 0) continue;
+    const int64_t bytes = ((n - 1) * ld_out[o] + (int64_t)heads[o] * head_dim) * es;
+    if (bytes_overlap(pos, n * 4ll, out[o], bytes)) return AKVS_ERR_INVALID_ARG;
+    for (int i = 0; i < 2; ++i)
+      if (heads[i] > 0 && bytes_overlap(gain[i], head_dim * 4ll, out[o], bytes)) return AKVS_ERR_INVALID_ARG;
+  }
   // In place is one tensor with one stride; any other overlap would be read after it was written.
   for (int o = 0; o < 2; ++o)
     for (int i = 0; i < 2; ++i) {

@@ -46,6 +46,7 @@ INVALID, SHAPE, WORKSPACE, UNSUPPORTED, TOO_LARGE = -1, -2, -3, -4, -8
     (dict(k_out=_at(5) + 256), INVALID),                                   # outputs that meet
     (dict(q_out=_at(0), q_out_ld=768), INVALID),                           # in place with another stride
     (dict(q_out=_at(1)), INVALID),                                         # q's output over k
+    (dict(k_out=_at(4)), INVALID), (dict(q_out=_at(3) - 1024), INVALID),   # over the positions, over a gain
 ])
 def test_norm_rope_refuses(b, change, code):
     assert b.lib.akvs_op_qk_norm_rope(*{**NORM, **change}.values()) == code

@@ -169,6 +169,31 @@ def test_shared_one_row_each(akvs, dt, hd, nq, nkv, P):
 
 
 @pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("hd,nq", [(128, 128), (64, 100), (128, 65)])
+def test_shared_many_heads_per_kv_head(akvs, dt, hd, nq):
+    """One query row alone fills a tile or leaves it ragged."""
+    lens = [9, 0, 33]
+    c = shared_case(nq, dt, hd, nq, 1, 300, 40, lens, [1, 1, 1])
+    check_shared(akvs.op_attention_shared(*c[:5], ints(lens)), *c)
+    c = shared_case(nq + 1, dt, hd, nq, 1, 0, 40, lens, [2, 1, 4], behind=1)
+    check_shared(akvs.op_attention_shared(*c[:5], ints(lens), ints(c[6])), *c)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_shared_without_any_key(akvs, dt):
+    """Neither context nor room for own tokens: zeros, and a log-sum-exp of -inf."""
+    g = gen(1)
+    q, none, room = rnd(g, 4, 8, 128, dt=dt), rnd(g, 0, 2, 128, dt=dt), rnd(g, 3, 0, 2, 128, dt=dt)
+    out, lse = torch.full_like(q, 5.0), torch.full((4, 8), 5.0, device="cuda")
+    akvs.op_attention_shared(q, none, none, room, room, ints([0, 0, 0]), None, out, lse)
+    assert (out[:3] == 0).all() and (lse[:3] == -math.inf).all() and (out[3] == 5).all() and (lse[3] == 5).all()
+    # a context alone
+    ctx = rnd(g, 70, 2, 128, dt=dt)
+    got = akvs.op_attention_shared(q[:3], ctx, ctx.flip(0), room, room, ints([0, 0, 0]))
+    check_shared(got, q[:3], ctx, ctx.flip(0), room, room, [0, 0, 0], [0, 1, 2, 3])
+
+
+@pytest.mark.parametrize("dt", TYPES)
 @pytest.mark.parametrize("hd,nq,nkv", [(128, 8, 2), (64, 5, 1), (128, 16, 1)])
 @pytest.mark.parametrize("P", [0, 50, 1000])
 def test_shared_ragged_rows(akvs, dt, hd, nq, nkv, P):
@@ -381,6 +406,15 @@ def test_mass(akvs, dt, hd, nq, nkv, R, T, kind):
     want = old + got
     akvs.op_attention_mass(q, k, lse, lo, hi, old, old)      # in place, and the same bits again
     assert torch.equal(old, more) and torch.equal(want, more)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("hd,nq,nkv", [(128, 128, 1), (64, 100, 1), (128, 65, 1), (64, 14, 2), (128, 6, 2)])
+@pytest.mark.parametrize("R", [1, 3, 150])
+def test_mass_many_heads_per_kv_head(akvs, dt, hd, nq, nkv, R):
+    """Groups that fill a tile of rows, leave it ragged, or need several of them, with ragged ranges."""
+    q, k, lse, lo, hi = mass_case(nq + R, dt, hd, nq, nkv, R, 530, "ragged")
+    check_mass(akvs.op_attention_mass(q, k, lse, lo, hi), q, k, lse, lo, hi)
 
 
 def test_mass_hidden_keys_and_blind_rows(akvs):
