@@ -7,16 +7,14 @@
 //
 // 16-bit types run on the tensor cores with the keys along M, so that a thread owns one key and its
 // sum over the rows needs no shuffle; the score matrix never leaves tensor memory:
-//     S^T = K Q^T     tcgen05.mma, two tiles of 128 keys against one tile of up to 256 stacked rows
+//     S^T = K Q^T     tcgen05.mma, two tiles of 128 keys against one tile of stacked rows
 //     sum             two warp groups, one per key tile: exp2 of a row of S^T, added up in registers
-// A CTA keeps 256 keys in shared memory while the rows' Q tiles stream past them (each is used
-// twice), then goes on to its next 256 keys.  Two warps work out what each column sees; a tile whose
-// columns all see its keys runs without a mask.  The exponentials bound it from below (16 per clock
-// and SM: 4096 clocks for 256 keys x 256 rows, 160 us of the 229 us that 512 rows x 40 heads x 32768
-// keys take); the rest is the MMA of a group's next tile, which waits for its only buffer.  With few
-// rows it is bound by reading K once (16 rows x 32 heads over 12416 keys: 8.9 us, 3.0 TB/s).
-// Few keys and many rows: a cluster shares the row tiles of its keys and adds the
-// partial sums through distributed shared memory.
+// A CTA keeps 256 keys while the rows' Q tiles stream past them (each is used twice), then goes on to
+// its next 256 keys.  Two warps work out what each column sees; a tile whose columns all see its
+// keys runs without a mask.  With many rows the exponentials bound it (16 per clock and SM), with few
+// rows reading K once (16 rows x 32 heads over 12416 keys: 7.6 us, 3.5 TB/s).  Few keys and many rows: a
+// cluster shares the row tiles of its keys and adds the partial sums through distributed shared
+// memory.
 #include "tc_common.cuh"
 #include <math.h>
 
@@ -39,46 +37,316 @@ constexpr float LOG2E = 1.4426950408889634f;
 
 // ---- tensor cores
 constexpr int BK = 128;              // keys of a tile, two tiles per item
-constexpr int M_THREADS = 384;       // warp group 0: TMA and MMA, warp groups 1 and 2: sums
+constexpr int M_THREADS = 384;       // warp group 0: TMA, MMA and columns; warp groups 1 and 2: sums
 constexpr int M_SLAB = 128 * 128;    // 128 rows of 64 values
-// FEW: all stacked rows fit 128 columns.  One Q tile stays as long as the head does, K streams
-// through two stages and S^T has two buffers, so that items overlap.  Otherwise row tiles of 256
-// columns stream past one K item: an MMA of 256 columns reads its A operand from shared memory half
-// as often per column, and the load of the next K hides behind the sums of the last tile (512 rows
-// x 40 heads x 32768 keys: 229 us, against 238 us with two buffers of 128 columns).
-template <bool FEW> struct MassCfg {
-  static constexpr int BQ = FEW ? 128 : 256, NB = FEW ? 2 : 1, KST = FEW ? 2 : 1, QST = FEW ? 1 : 2;
-};
-template <int HD> constexpr int M_TILE = HD / 64 * M_SLAB;               // 128 rows
-// shared memory: K[KST][2 tiles] | Q[QST] | barriers (256 B) | what a column sees, twice | partial sums | flags
-template <bool FEW> constexpr int M_COLS = 2 * MassCfg<FEW>::BQ * (4 + 8);
-template <int HD, bool FEW> constexpr int M_SMEM = (2 * MassCfg<FEW>::KST + MassCfg<FEW>::QST * MassCfg<FEW>::BQ / 128) * M_TILE<HD> +
-                                                   256 + M_COLS<FEW> + 2 * 128 * 4 + 64;
-enum { MB_KFULL = 0, MB_KEMPTY = 2, MB_QFULL = 4, MB_QEMPTY = 6,
-       MB_SFULL = 8,                          // [2 groups][2 buffers] S^T of a tile is complete
-       MB_SEMPTY = 12,                        // [2][2] the group has taken it into registers (4 warps)
-       MB_CFULL = 16, MB_CEMPTY = 18,         // [2] what the columns of a tile see has been written / read (2 warps, 8 warps)
-       MB_COUNT = 20 };
-static_assert(MB_COUNT * 8 + 8 <= 256, "barriers, the tensor-memory slot and the abort flag share 256 bytes");
-static_assert(M_SMEM<128, true> <= 232448 && M_SMEM<128, false> <= 232448, "shared memory of one CTA");
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-template <typename T, int HD, bool FEW>
+
+// A row of a tile is a column of S^T: BR rows x g heads, rows from rt * BR.
+struct Cols { int BR, gb; };
+
+// What the columns of a tile see, worked out by NWARP warps (`half` of them) for the summing warps, with
+// all loads of a lane in flight together.  col_z: -lse in log2 units; col_rng: first visible key and how
+// many follow; flag[w][half]: some column of the half needs a mask for key tile w.
+template <int BQ, int NWARP>
+struct ColumnLane {                  // a lane's columns, the same in every tile: row and head inside it
+  static constexpr int N = BQ / (32 * NWARP);
+  static_assert(BQ % (32 * NWARP) == 0, "every lane has as many columns");
+  int r_in[N], head_in[N];           // r_in = BR: a column that is never loaded
+  __device__ __forceinline__ ColumnLane(const Cols& cl, int half, int lane) {
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+      const int i = (x * NWARP + half) * 32 + lane;
+      r_in[x] = min(i / cl.gb, cl.BR);
+      head_in[x] = i % cl.gb;
+    }
+  }
+};
+template <int BQ, int NWARP, int NW>
+struct ColumnLoad {                  // NW: key tiles of an item
+  static constexpr int N = BQ / (32 * NWARP);
+  float z[N];
+  int lo[N], hi[N];
+  __device__ __forceinline__ void fetch(const MassParams& p, const Cols& cl, const ColumnLane<BQ, NWARP>& ln, int rt, int h) {
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+      const int r = min(rt * cl.BR + ln.r_in[x], p.R - 1);
+      z[x] = __ldg(p.lse + (int64_t)r * p.n_q + h * p.g + ln.head_in[x]);
+      lo[x] = __ldg(p.k_lo + r);
+      hi[x] = __ldg(p.k_hi + r);
+    }
+  }
+  __device__ __forceinline__ void store(const MassParams& p, const Cols& cl, const ColumnLane<BQ, NWARP>& ln, int rt, int k0, int half,
+                                        int lane, float* col_z, int2* col_rng, volatile int* flag) const {
+    bool masked[NW] = {};
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+      const int i = (x * NWARP + half) * 32 + lane;
+      const bool real = ln.r_in[x] < cl.BR && rt * cl.BR + ln.r_in[x] < p.R;
+      const int a = max(lo[x], 0), b = min(hi[x], p.T - 1);
+      const bool blind = !real || z[x] == -INFINITY || a > b;              // such a column adds nothing
+      // columns of zeros behind the last row need no mask: exp2(0 - inf) = 0
+#pragma unroll
+      for (int w = 0; w < NW; ++w)
+        masked[w] |= real && (blind || a > k0 + w * BK || b < min(k0 + (w + 1) * BK, p.T) - 1);
+      col_z[i] = blind ? -INFINITY : -z[x] * LOG2E;
+      // seen <=> (unsigned)(key - first) <= length: never for a blind column (keys are not negative)
+      col_rng[i] = blind ? make_int2(0x7fffffff, 0) : make_int2(a, b - a);
+    }
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const bool any = __any_sync(0xFFFFFFFFu, masked[w]);
+      if (lane == 0) flag[w * NWARP + half] = any;
+    }
+    __syncwarp();
+  }
+};
+
+// N columns of a key's row of S^T: no branch inside, so that the loads, exponentials and sums of
+// different columns overlap.
+template <int N>
+__device__ __forceinline__ void add_columns(const float (&t)[N], const float* z, const int2* ranges, bool mask, int key,
+                                            float scale2, float2 (&acc)[4]) {
+  const float2 sc = make_float2(scale2, scale2);
+  if (!mask) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const float4 zz = *reinterpret_cast<const float4*>(z + i);
+      const float2 x = __ffma2_rn(make_float2(t[i], t[i + 1]), sc, make_float2(zz.x, zz.y));
+      const float2 y = __ffma2_rn(make_float2(t[i + 2], t[i + 3]), sc, make_float2(zz.z, zz.w));
+      acc[(i >> 1) & 3] = __fadd2_rn(acc[(i >> 1) & 3], make_float2(ex2(x.x), ex2(x.y)));
+      acc[((i >> 1) + 1) & 3] = __fadd2_rn(acc[((i >> 1) + 1) & 3], make_float2(ex2(y.x), ex2(y.y)));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const float2 zz = *reinterpret_cast<const float2*>(z + i);
+      const int4 rng = *reinterpret_cast<const int4*>(ranges + i);
+      const float2 x = __ffma2_rn(make_float2(t[i], t[i + 1]), sc, zz);
+      const float e0 = ex2(x.x), e1 = ex2(x.y);
+      acc[(i >> 1) & 3] = __fadd2_rn(acc[(i >> 1) & 3], make_float2((unsigned)(key - rng.x) <= (unsigned)rng.y ? e0 : 0.f,
+                                                                  (unsigned)(key - rng.z) <= (unsigned)rng.w ? e1 : 0.f));
+    }
+  }
+}
+__device__ __forceinline__ float total(const float2 (&acc)[4]) {
+  const float2 a = __fadd2_rn(acc[0], acc[1]), b = __fadd2_rn(acc[2], acc[3]);
+  return (a.x + a.y) + (b.x + b.y);
+}
+
+// A 128-byte-swizzled operand `bytes` further on in shared memory.  The address sits in the descriptor's
+// low bits in units of 16 bytes, so a constant is added instead of building it anew.
+__device__ __forceinline__ uint64_t desc_at(uint64_t desc, uint32_t bytes) { return desc + (bytes >> 4); }
+
+// Bounded waits all over: whoever runs out raises the flag, and the others follow.
+struct Waiter {
+  uint64_t* bar;
+  volatile int* abort_flag;
+  __device__ __forceinline__ bool operator()(int b, uint32_t parity) const { return tc::mbar_wait(&bar[b], parity & 1, abort_flag); }
+};
+
+// -- few rows: all columns fit one tile of 128.  The Q tile stays as long as the head does, K streams
+// through two stages by TMA and S^T has two buffers, so that items overlap; bound by reading K.
+namespace few {
+constexpr int BQ = 128, KST = 2;
+template <int HD> constexpr int TILE = HD / 64 * M_SLAB;
+// shared memory: K[2][2 tiles] | Q | barriers (256 B) | what a column sees, twice | flags
+template <int HD> constexpr int SMEM = (2 * KST + 1) * TILE<HD> + 256 + 2 * BQ * 12 + 64;
+enum { KFULL = 0, KEMPTY = 2, QFULL = 4, QEMPTY = 5, SFULL = 6 /*[2 groups][2]*/, SEMPTY = 10, CFULL = 14, CEMPTY = 16, COUNT = 18 };
+static_assert(COUNT * 8 + 8 <= 256 && SMEM<128> <= 232448, "shared memory of one CTA");
+
+template <typename T, int HD>
 __global__ void __launch_bounds__(M_THREADS, 1)
-mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmQ, const MassParams p,
-               int C, int key_items, int n_items, int BR, int q_boxes, uint32_t fmt) {
-  using Cfg = MassCfg<FEW>;
-  constexpr int TILE = M_TILE<HD>, BQ = Cfg::BQ, NB = Cfg::NB, KST = Cfg::KST, QST = Cfg::QST, Q_BYTES = BQ / 128 * TILE;
-  constexpr int OFF_Q = 2 * KST * TILE, OFF_BAR = OFF_Q + QST * Q_BYTES, OFF_COL = OFF_BAR + 256;
-  constexpr int OFF_PART = OFF_COL + M_COLS<FEW>, OFF_FLAG = OFF_PART + 2 * 128 * 4, Q_SLAB = BQ * 128;
+mass_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmQ, const MassParams p,
+                const Cols cols, int key_items, int n_items, uint32_t fmt) {
+  constexpr int OFF_Q = 2 * KST * TILE<HD>, OFF_BAR = OFF_Q + TILE<HD>, OFF_COL = OFF_BAR + 256, OFF_FLAG = OFF_COL + 2 * BQ * 12;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  if (tc::smem_u32(smem) & 1023u) return;           // swizzled tiles need 1024-byte alignment
+  uint64_t* bar = reinterpret_cast<uint64_t*>(smem + OFF_BAR);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + COUNT);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  float* col_z = reinterpret_cast<float*>(smem + OFF_COL);
+  int2* col_rng = reinterpret_cast<int2*>(col_z + 2 * BQ);
+  volatile int* flag = reinterpret_cast<volatile int*>(smem + OFF_FLAG);    // [2][2 groups][2 halves]
+  const Waiter wait{bar, abort_flag};
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  pdl_trigger();
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < COUNT; ++i) tc::mbar_init(&bar[i], i >= CEMPTY ? 8 : i >= CFULL ? 2 : i >= SEMPTY ? 4 : 1);
+    *abort_flag = 0;
+    tc::fence_barrier_init();
+  }
+  if (warp == 1) {
+    tc::tmem_alloc(tmem_slot, 512);
+    tc::tmem_relinquish();
+  }
+  for (int i = threadIdx.x; i < TILE<HD> / 16; i += M_THREADS)      // what the load leaves out behind the rows stays zero
+    *reinterpret_cast<uint4*>(smem + OFF_Q + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+  tc::fence_proxy_async();
+  pdl_wait();
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot;
+  // consecutive items, of one head mostly
+  const int item0 = (int)((int64_t)n_items * blockIdx.x / gridDim.x), item1 = (int)((int64_t)n_items * (blockIdx.x + 1) / gridDim.x);
+  const bool rows = p.R > 0;
+  const int n_cols = p.R * p.g;
+  auto head_ends = [&](int item) { return item + 1 == item1 || (item + 1) / key_items != item / key_items; };
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    bool ok = true;
+    if (warp == 0 && lane == 0) {
+      // ------------------------------------------------------------------ TMA producer
+      tc::prefetch_tmap(&tmK);
+      tc::prefetch_tmap(&tmQ);
+      int nq = 0;
+      for (int item = item0, it = 0; item < item1; ++item, ++it) {
+        const int h = item / key_items, j0 = (item % key_items) * (2 * BK), ks = it % KST;
+        if (!(ok = wait(KEMPTY + ks, (it / KST) ^ 1))) break;
+        tc::mbar_expect_tx(&bar[KFULL + ks], 2 * TILE<HD>);
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+          for (int c = 0; c < HD / 64; ++c)
+            tc::tma_load_2d(smem + (2 * ks + w) * TILE<HD> + c * M_SLAB, &tmK, h * HD + c * 64, j0 + w * BK, &bar[KFULL + ks]);
+        if (!rows || (it > 0 && (item - 1) / key_items == h)) continue;      // the head's rows are there
+        if (!(ok = wait(QEMPTY, nq ^ 1))) break;
+        tc::mbar_expect_tx(&bar[QFULL], (uint32_t)(cols.BR * cols.gb) * 128u * (HD / 64));
+#pragma unroll
+        for (int c = 0; c < HD / 64; ++c) tc::tma_load_3d(smem + OFF_Q + c * M_SLAB, &tmQ, c * 64, h * p.g, 0, &bar[QFULL]);
+        ++nq;
+      }
+    } else if (warp == 1 && lane == 0) {
+      // ------------------------------------------------------------------ MMA issuer
+      const uint32_t idesc = tc::idesc_f16(fmt, BK, (n_cols + 63) / 64 * 64, 0);      // whole chunks of 64 columns
+      const uint64_t q_desc = tc::smem_desc_k_sw128(tc::smem_u32(smem + OFF_Q)), k_desc = tc::smem_desc_k_sw128(tc::smem_u32(smem));
+      int nq = 0;
+      for (int item = item0, it = 0; item < item1 && ok; ++item, ++it) {
+        const int ks = it % KST, b = it & 1;
+        if (!(ok = wait(KFULL + ks, it / KST))) break;
+        if (rows) {
+          if (!(ok = wait(QFULL, nq))) break;
+          for (int w = 0; w < 2; ++w) {
+            if (!(ok = wait(SEMPTY + 2 * w + b, (it >> 1) ^ 1))) break;
+            tc::fence_after_sync();
+            const uint64_t kd = desc_at(k_desc, (2 * ks + w) * TILE<HD>);
+#pragma unroll
+            for (int k = 0; k < HD / 16; ++k) {
+              const uint32_t off = (k >> 2) * M_SLAB + (k & 3) * 32;
+              tc::mma_f16(tmem_base + w * 256 + b * BQ, desc_at(kd, off), desc_at(q_desc, off), idesc, k != 0);
+            }
+            tc::mma_commit(&bar[SFULL + 2 * w + b]);
+          }
+          if (!ok) break;
+          if (head_ends(item)) { tc::mma_commit(&bar[QEMPTY]); ++nq; }
+        }
+        tc::mma_commit(&bar[KEMPTY + ks]);
+      }
+    } else if (warp >= 2 && rows) {
+      // ------------------------------------------------------------------ what the columns see
+      const ColumnLane<BQ, 2> ln(cols, warp - 2, lane);
+      ColumnLoad<BQ, 2, 2> cl;
+      for (int item = item0, it = 0; item < item1; ++item, ++it) {
+        const int h = item / key_items, cb = it & 1;
+        if (it == 0 || (item - 1) / key_items != h) cl.fetch(p, cols, ln, 0, h);
+        if (!(ok = wait(CEMPTY + cb, (it >> 1) ^ 1))) break;
+        cl.store(p, cols, ln, 0, (item % key_items) * (2 * BK), warp - 2, lane, col_z + cb * BQ, col_rng + cb * BQ, flag + cb * 4);
+        if (lane == 0) tc::mbar_arrive(&bar[CFULL + cb]);
+      }
+    }
+    if (!ok) *abort_flag = 1;
+  } else {
+    // ---------------------------------------------------------------------- a key per thread
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+    const int w = (warp >> 2) - 1, m = threadIdx.x & 127, quad = warp & 3;
+    const uint32_t lane_addr = tmem_base + ((uint32_t)(quad * 32) << 16);
+    bool ok = true;
+    for (int item = item0, it = 0; item < item1; ++item, ++it) {
+      const int h = item / key_items, key = (item % key_items) * (2 * BK) + w * BK + m, b = it & 1;
+      const int64_t at = (int64_t)h * p.T + key;
+      const float old = p.mass_in && key < p.T ? p.mass_in[at] : 0.f;
+      float2 acc[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+      if (rows) {
+        if (!(ok = wait(CFULL + b, it >> 1))) break;
+        const bool mask = (flag[(b * 2 + w) * 2] | flag[(b * 2 + w) * 2 + 1]) != 0;
+        if (!(ok = wait(SFULL + 2 * w + b, it >> 1))) break;
+        tc::fence_after_sync();
+        // 64 columns at a time, the next ones on their way from tensor memory meanwhile
+        const uint32_t s_addr = lane_addr + w * 256 + b * BQ;
+        const int chunks = (n_cols + 63) / 64;
+        float ta[64], tb[64];
+        auto fetch = [&](float(&t)[64], int c) {
+          tc::tmem_ld32(s_addr + c * 64, *reinterpret_cast<float(*)[32]>(&t[0]));
+          tc::tmem_ld32(s_addr + c * 64 + 32, *reinterpret_cast<float(*)[32]>(&t[32]));
+        };
+        auto taken = [&]() {                              // all of the tile is in registers: its buffer is free
+          tc::fence_before_sync();
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(&bar[SEMPTY + 2 * w + b]);
+        };
+        const float* z = col_z + b * BQ;
+        const int2* rng = col_rng + b * BQ;
+        fetch(ta, 0);
+        tc::tmem_ld_wait();
+        if (chunks > 1) fetch(tb, 1);
+        else taken();
+        add_columns<64>(ta, z, rng, mask, key, p.scale * LOG2E, acc);
+        if (chunks > 1) {
+          tc::tmem_ld_wait();
+          taken();
+          add_columns<64>(tb, z + 64, rng + 64, mask, key, p.scale * LOG2E, acc);
+        }
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&bar[CEMPTY + b]);
+      }
+      if (key < p.T) p.mass_out[at] = old + total(acc);
+    }
+    if (!ok) *abort_flag = 1;
+  }
+  if (*abort_flag) __nanosleep(200000);
+  tc::fence_before_sync();
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc::fence_after_sync();
+    tc::tmem_dealloc(tmem_base, 512);
+  }
+}
+}  // namespace few
+
+// -- many rows: tiles of up to 256 columns stream past the K of 256 keys.  The width halves what an MMA
+// reads of its A operand per column and spreads a tile's barriers over more work; one buffer of S^T per
+// group is all that fits then, and a group's next product waits until its last columns are taken.
+// 512 rows x 40 heads x 32768 keys: 229 to 238 us, of which the exponentials are 160 us (16 per clock and
+// SM).  Built and measured instead of it: 128 columns with two buffers 238 us (against 229); an issuing
+// thread per group (and a warp less for the columns) 237 us; K in tensor memory as the A operand with
+// tiles of 96 columns, two groups of two buffers 276 us, three groups of one buffer 253 us.
+namespace many {
+constexpr int BQ = 256, QST = 2;
+template <int HD> constexpr int KTILE = HD / 64 * M_SLAB;                // 128 keys
+template <int HD> constexpr int QTILE = HD / 64 * BQ * 128;
+// shared memory: K[2 tiles] | Q[2] | barriers (256 B) | what a column sees, twice | partial sums | flags
+template <int HD> constexpr int SMEM = 2 * KTILE<HD> + QST * QTILE<HD> + 256 + 2 * BQ * 12 + 2 * 128 * 4 + 64;
+enum { QFULL = 0, QEMPTY = QFULL + QST, KFULL = QEMPTY + QST, KEMPTY, SFULL /*[2 groups]*/, SEMPTY = SFULL + 2, CFULL = SEMPTY + 2,
+       CEMPTY = CFULL + 2, COUNT = CEMPTY + 2 };
+static_assert(COUNT * 8 + 8 <= 256 && SMEM<128> <= 232448, "shared memory of one CTA");
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(M_THREADS, 1)
+mass_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmQ, const MassParams p,
+                 int C, int key_items, int n_items, int BR, int q_boxes, uint32_t fmt) {
+  constexpr int OFF_Q = 2 * KTILE<HD>, OFF_BAR = OFF_Q + QST * QTILE<HD>, OFF_COL = OFF_BAR + 256, OFF_PART = OFF_COL + 2 * BQ * 12;
+  constexpr int OFF_FLAG = OFF_PART + 2 * 128 * 4, Q_SLAB = BQ * 128;
   extern __shared__ __align__(1024) uint8_t smem[];
   if (tc::smem_u32(smem) & 1023u) return;           // swizzled tiles need 1024-byte alignment (the same in every CTA)
   uint64_t* bar = reinterpret_cast<uint64_t*>(smem + OFF_BAR);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + MB_COUNT);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + COUNT);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   float* part = reinterpret_cast<float*>(smem + OFF_PART);          // [2][128]
   float* col_z = reinterpret_cast<float*>(smem + OFF_COL);          // [2][BQ] -lse of a column in log2 units
@@ -87,7 +355,7 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_trigger();
   if (threadIdx.x == 0) {
-    for (int i = 0; i < MB_COUNT; ++i) tc::mbar_init(&bar[i], i >= MB_CEMPTY ? 8 : i >= MB_CFULL ? 2 : i >= MB_SEMPTY ? 4 : 1);
+    for (int i = 0; i < COUNT; ++i) tc::mbar_init(&bar[i], i >= CEMPTY ? 8 : i >= CFULL ? 2 : i >= SEMPTY ? 4 : 1);
     *abort_flag = 0;
     tc::fence_barrier_init();
   }
@@ -96,7 +364,7 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     tc::tmem_relinquish();
   }
   // Q tiles hold BR * g rows; what the loads leave out behind them stays zero
-  for (int i = threadIdx.x; i < QST * Q_BYTES / 16; i += M_THREADS)
+  for (int i = threadIdx.x; i < QST * QTILE<HD> / 16; i += M_THREADS)
     *reinterpret_cast<uint4*>(smem + OFF_Q + i * 16) = make_uint4(0u, 0u, 0u, 0u);
   tc::fence_proxy_async();
   pdl_wait();
@@ -104,13 +372,9 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
   __syncthreads();
   tc::fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
-  // FEW: consecutive items (of one head, mostly) for each cluster.  Otherwise every n_cl-th, so that
-  // masked items (the end of a causal window) spread.
-  const int rank = blockIdx.x % C, n_cl = gridDim.x / C, cl = blockIdx.x / C;
-  const int item0 = FEW ? (int)((int64_t)n_items * cl / n_cl) : cl, step = FEW ? 1 : n_cl;
-  const int item1 = FEW ? (int)((int64_t)n_items * (cl + 1) / n_cl) : n_items;
+  // every n_cl-th item for a cluster, so that masked items (the end of a causal window) spread
+  const int rank = blockIdx.x % C, item0 = blockIdx.x / C, step = gridDim.x / C;
   const int row_tiles = (p.R + BR - 1) / BR;
-  auto head_ends = [&](int item) { return item + 1 == item1 || (item + 1) / key_items != item / key_items; };
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
@@ -123,25 +387,24 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
         const int box_rows = BR / q_boxes, box_bytes = box_rows * p.g * 128;
         bool ok = true;
         int it = 0, n = 0;
-        for (int item = item0; item < item1 && ok; item += step, ++it) {
-          const int h = item / key_items, j0 = (item % key_items) * (2 * BK), ks = it % KST;
-          if (!tc::mbar_wait(&bar[MB_KEMPTY + ks], ((it / KST) & 1) ^ 1, abort_flag)) { ok = false; break; }
-          tc::mbar_expect_tx(&bar[MB_KFULL + ks], 2 * TILE);
+        for (int item = item0; item < n_items && ok; item += step, ++it) {
+          const int h = item / key_items, j0 = (item % key_items) * (2 * BK);
+          if (!tc::mbar_wait(&bar[KEMPTY], (it & 1) ^ 1, abort_flag)) { ok = false; break; }
+          tc::mbar_expect_tx(&bar[KFULL], 2 * KTILE<HD>);
 #pragma unroll
           for (int w = 0; w < 2; ++w)
 #pragma unroll
             for (int c = 0; c < HD / 64; ++c)
-              tc::tma_load_2d(smem + (2 * ks + w) * TILE + c * M_SLAB, &tmK, h * HD + c * 64, j0 + w * BK, &bar[MB_KFULL + ks]);
-          if (FEW && it > 0 && (item - 1) / key_items == h) continue;    // the head's rows are there
+              tc::tma_load_2d(smem + w * KTILE<HD> + c * M_SLAB, &tmK, h * HD + c * 64, j0 + w * BK, &bar[KFULL]);
           for (int rt = rank; rt < row_tiles; rt += C, ++n) {
             const int qs = n % QST;
-            if (!tc::mbar_wait(&bar[MB_QEMPTY + qs], ((n / QST) & 1) ^ 1, abort_flag)) { ok = false; break; }
-            tc::mbar_expect_tx(&bar[MB_QFULL + qs], (uint32_t)(q_boxes * box_bytes * (HD / 64)));
+            if (!tc::mbar_wait(&bar[QEMPTY + qs], ((n / QST) & 1) ^ 1, abort_flag)) { ok = false; break; }
+            tc::mbar_expect_tx(&bar[QFULL + qs], (uint32_t)(q_boxes * box_bytes * (HD / 64)));
             for (int x = 0; x < q_boxes; ++x)
 #pragma unroll
               for (int c = 0; c < HD / 64; ++c)
-                tc::tma_load_3d(smem + OFF_Q + qs * Q_BYTES + c * Q_SLAB + x * box_bytes, &tmQ, c * 64, h * p.g,
-                                rt * BR + x * box_rows, &bar[MB_QFULL + qs]);
+                tc::tma_load_3d(smem + OFF_Q + qs * QTILE<HD> + c * Q_SLAB + x * box_bytes, &tmQ, c * 64, h * p.g,
+                                rt * BR + x * box_rows, &bar[QFULL + qs]);
           }
         }
         if (!ok) *abort_flag = 1;
@@ -150,29 +413,28 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       // ------------------------------------------------------------------ MMA issuer
       if (lane == 0) {
         bool ok = true;
-        int it = 0, n = 0, nq = 0;                    // items, tiles, Q tiles so far
-        for (int item = item0; item < item1 && ok; item += step, ++it) {
-          const int ks = it % KST;
-          if (!tc::mbar_wait(&bar[MB_KFULL + ks], (it / KST) & 1, abort_flag)) { ok = false; break; }
+        int it = 0, n = 0;
+        for (int item = item0; item < n_items && ok; item += step, ++it) {
+          if (!tc::mbar_wait(&bar[KFULL], it & 1, abort_flag)) { ok = false; break; }
           for (int rt = rank; rt < row_tiles && ok; rt += C, ++n) {
-            const int qs = nq % QST, b = n % NB;
-            if (!tc::mbar_wait(&bar[MB_QFULL + qs], (nq / QST) & 1, abort_flag)) { ok = false; break; }
+            const int qs = n % QST;
+            if (!tc::mbar_wait(&bar[QFULL + qs], (n / QST) & 1, abort_flag)) { ok = false; break; }
             const int cols = min(BR, p.R - rt * BR) * p.g;
             const uint32_t idesc = tc::idesc_f16(fmt, BK, (cols + 63) / 64 * 64, 0);      // whole chunks: rows of zeros behind the last
-            const uint32_t q_addr = tc::smem_u32(smem + OFF_Q + qs * Q_BYTES);
+            const uint32_t q_addr = tc::smem_u32(smem + OFF_Q + qs * QTILE<HD>);
             for (int w = 0; w < 2; ++w) {
-              if (!tc::mbar_wait(&bar[MB_SEMPTY + 2 * w + b], ((n / NB) & 1) ^ 1, abort_flag)) { ok = false; break; }
+              if (!tc::mbar_wait(&bar[SEMPTY + w], (n & 1) ^ 1, abort_flag)) { ok = false; break; }
               tc::fence_after_sync();
-              const uint32_t k_addr = tc::smem_u32(smem + (2 * ks + w) * TILE);
+              const uint32_t k_addr = tc::smem_u32(smem + w * KTILE<HD>);
 #pragma unroll
               for (int k = 0; k < HD / 16; ++k)
-                tc::mma_f16(tmem_base + w * 256 + b * BQ, tc::smem_desc_k_sw128(k_addr + (k >> 2) * M_SLAB + (k & 3) * 32),
+                tc::mma_f16(tmem_base + w * BQ, tc::smem_desc_k_sw128(k_addr + (k >> 2) * M_SLAB + (k & 3) * 32),
                             tc::smem_desc_k_sw128(q_addr + (k >> 2) * Q_SLAB + (k & 3) * 32), idesc, k != 0);
-              tc::mma_commit(&bar[MB_SFULL + 2 * w + b]);
+              tc::mma_commit(&bar[SFULL + w]);
             }
-            if (ok && (!FEW || head_ends(item))) { tc::mma_commit(&bar[MB_QEMPTY + qs]); ++nq; }
+            if (ok) tc::mma_commit(&bar[QEMPTY + qs]);
           }
-          if (ok) tc::mma_commit(&bar[MB_KEMPTY + ks]);
+          if (ok) tc::mma_commit(&bar[KEMPTY]);
         }
         if (!ok) *abort_flag = 1;
       }
@@ -192,7 +454,7 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       }
       bool ok = true;
       int n = 0;
-      for (int item = item0; item < item1 && ok; item += step) {
+      for (int item = item0; item < n_items && ok; item += step) {
         const int h = item / key_items, k0 = (item % key_items) * (2 * BK);
         for (int rt = rank; rt < row_tiles; rt += C, ++n) {
           const int cb = n & 1;
@@ -205,7 +467,7 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
             lo[x] = __ldg(p.k_lo + r);
             hi[x] = __ldg(p.k_hi + r);
           }
-          if (!tc::mbar_wait(&bar[MB_CEMPTY + cb], ((n >> 1) & 1) ^ 1, abort_flag)) { ok = false; break; }
+          if (!tc::mbar_wait(&bar[CEMPTY + cb], ((n >> 1) & 1) ^ 1, abort_flag)) { ok = false; break; }
           bool masked[2] = {false, false};
 #pragma unroll
           for (int x = 0; x < CPL; ++x) {
@@ -228,7 +490,7 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
             if (lane == 0) flag[(cb * 2 + w) * 2 + half] = any;
           }
           __syncwarp();
-          if (lane == 0) tc::mbar_arrive(&bar[MB_CFULL + cb]);
+          if (lane == 0) tc::mbar_arrive(&bar[CFULL + cb]);
         }
       }
       if (!ok && lane == 0) *abort_flag = 1;
@@ -241,18 +503,18 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     const float scale2 = p.scale * LOG2E;
     bool ok = true;
     int n = 0;
-    for (int item = item0; item < item1 && ok; item += step) {
+    for (int item = item0; item < n_items && ok; item += step) {
       const int h = item / key_items, key = (item % key_items) * (2 * BK) + w * BK + m;
       float2 acc[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
       for (int rt = rank; rt < row_tiles; rt += C, ++n) {
-        const int b = n % NB, cb = n & 1;
+        const int cb = n & 1;
         const int all_cols = min(BR, p.R - rt * BR) * p.g;
-        if (!tc::mbar_wait(&bar[MB_CFULL + cb], (n >> 1) & 1, abort_flag)) { ok = false; break; }
+        if (!tc::mbar_wait(&bar[CFULL + cb], (n >> 1) & 1, abort_flag)) { ok = false; break; }
         const bool mask = (flag[(cb * 2 + w) * 2] | flag[(cb * 2 + w) * 2 + 1]) != 0;
-        if (!tc::mbar_wait(&bar[MB_SFULL + 2 * w + b], (n / NB) & 1, abort_flag)) { ok = false; break; }
+        if (!tc::mbar_wait(&bar[SFULL + w], n & 1, abort_flag)) { ok = false; break; }
         tc::fence_after_sync();
         // 64 columns at a time, the next ones on their way from tensor memory meanwhile
-        const uint32_t s_addr = lane_addr + w * 256 + b * BQ;
+        const uint32_t s_addr = lane_addr + w * BQ;
         const int chunks = (all_cols + 63) / 64;
         float ta[64], tb[64];
         auto fetch = [&](float(&t)[64], int c) {
@@ -264,34 +526,11 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
           if (c + 1 == chunks) {                          // all of the tile is in registers: its buffer is free
             tc::fence_before_sync();
             __syncwarp();
-            if (lane == 0) tc::mbar_arrive(&bar[MB_SEMPTY + 2 * w + b]);
+            if (lane == 0) tc::mbar_arrive(&bar[SEMPTY + w]);
           }
         };
         auto add = [&](const float(&t)[64], int c) {
-          const float* z = col_z + cb * BQ + c * 64;
-          const float2 sc = make_float2(scale2, scale2);
-          // no branch inside: the loads, exponentials and sums of different columns overlap
-          if (!mask) {
-#pragma unroll
-            for (int i = 0; i < 64; i += 4) {
-              const float4 zz = *reinterpret_cast<const float4*>(z + i);
-              const float2 x = __ffma2_rn(make_float2(t[i], t[i + 1]), sc, make_float2(zz.x, zz.y));
-              const float2 y = __ffma2_rn(make_float2(t[i + 2], t[i + 3]), sc, make_float2(zz.z, zz.w));
-              acc[(i >> 1) & 3] = __fadd2_rn(acc[(i >> 1) & 3], make_float2(ex2(x.x), ex2(x.y)));
-              acc[((i >> 1) + 1) & 3] = __fadd2_rn(acc[((i >> 1) + 1) & 3], make_float2(ex2(y.x), ex2(y.y)));
-            }
-          } else {
-            const int2* ranges = col_rng + cb * BQ + c * 64;
-#pragma unroll
-            for (int i = 0; i < 64; i += 2) {
-              const float2 zz = *reinterpret_cast<const float2*>(z + i);
-              const int4 rng = *reinterpret_cast<const int4*>(ranges + i);
-              const float2 x = __ffma2_rn(make_float2(t[i], t[i + 1]), sc, zz);
-              const float e0 = ex2(x.x), e1 = ex2(x.y);
-              acc[(i >> 1) & 3] = __fadd2_rn(acc[(i >> 1) & 3], make_float2((unsigned)(key - rng.x) <= (unsigned)rng.y ? e0 : 0.f,
-                                                                          (unsigned)(key - rng.z) <= (unsigned)rng.w ? e1 : 0.f));
-            }
-          }
+          add_columns<64>(t, col_z + cb * BQ + c * 64, col_rng + cb * BQ + c * 64, mask, key, scale2, acc);
         };
         fetch(ta, 0);
         for (int c = 0; c < chunks; c += 2) {
@@ -304,11 +543,10 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
           add(tb, c + 1);
         }
         __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&bar[MB_CEMPTY + cb]);
+        if (lane == 0) tc::mbar_arrive(&bar[CEMPTY + cb]);
       }
       if (!ok) break;
-      const float2 s01 = __fadd2_rn(acc[0], acc[1]), s23 = __fadd2_rn(acc[2], acc[3]);
-      const float sum = (s01.x + s01.y) + (s23.x + s23.y);
+      const float sum = total(acc);
       const int64_t at = (int64_t)h * p.T + key;
       if (C == 1) {
         if (key < p.T) p.mass_out[at] = (p.mass_in ? p.mass_in[at] : 0.f) + sum;
@@ -343,56 +581,61 @@ mass_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     tc::tmem_dealloc(tmem_base, 512);
   }
 }
+}  // namespace many
 
-template <typename T, int HD, bool FEW>
+template <typename T, int HD>
 int32_t run_tc(const MassParams& p, cudaStream_t st) {
   static bool attr_set = false;
   if (!attr_set) {
-    AKVS_CUDA(cudaFuncSetAttribute(mass_tc_kernel<T, HD, FEW>, cudaFuncAttributeMaxDynamicSharedMemorySize, M_SMEM<HD, FEW>));
+    AKVS_CUDA(cudaFuncSetAttribute(few::mass_few_kernel<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, few::SMEM<HD>));
+    AKVS_CUDA(cudaFuncSetAttribute(many::mass_many_kernel<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, many::SMEM<HD>));
     attr_set = true;
   }
-  // rows of a tile: 1 or 2 boxes whose rows fill whole groups of 8 (a swizzle atom), so that boxes lie back to back
-  int box_rows = 128 / p.g, q_boxes = FEW ? 1 : 2;
-  if (!FEW) {
-    while (box_rows > 1 && box_rows * p.g % 8) --box_rows;
-    if (box_rows * p.g % 8) { box_rows = 128 / p.g; q_boxes = 1; }
-  }
-  const int BR = box_rows * q_boxes;
-  const int row_tiles = akvs_cdiv(p.R, BR), key_items = akvs_cdiv(p.T, 2 * BK);
+  const uint32_t fmt = std::is_same<T, f16>::value ? tc::kF16 : tc::kBF16;
+  const bool rows = p.R > 0, is_few = (int64_t)p.R * p.g <= few::BQ;
+  const int key_items = akvs_cdiv(p.T, 2 * BK);
   const int64_t n_items = (int64_t)key_items * p.n_kv;
   if (n_items > 0x7fffffff) return AKVS_ERR_TOO_LARGE;
+  // rows of a tile: one or two boxes, whose rows fill whole groups of 8 (a swizzle atom) where there are two
+  int box_rows = 128 / p.g, boxes = 1;
+  if (!is_few) {
+    int b = box_rows;
+    while (b > 1 && b * p.g % 8) --b;
+    if (b * p.g % 8 == 0) { box_rows = b; boxes = 2; }
+  }
+  const Cols cols = {box_rows * boxes, p.g};
   CUtensorMap tmK, tmQ;
   AKVS_TRY(make_tmap_2d_16bit(&tmK, p.k, p.T, (uint64_t)p.n_kv * HD, (uint64_t)p.k_ld, BK));
   // without rows there is no tile to load either; the map only has to be well formed
-  AKVS_TRY(encode_tmap_3d_16bit(&tmQ, p.R > 0 ? p.q : p.k, HD, p.R > 0 ? p.n_q : p.n_kv, p.R > 0 ? p.R : p.T, HD,
-                                p.R > 0 ? p.q_ld : p.k_ld, p.g, box_rows));
-  int C = 1;
-  while (C < 8 && n_items * C * 2 <= 148 && row_tiles >= C * 4) C *= 2;
-  const int64_t grid = C > 1 ? n_items * C : (n_items < 148 ? n_items : 148);
+  AKVS_TRY(encode_tmap_3d_16bit(&tmQ, rows ? p.q : p.k, HD, rows ? p.n_q : p.n_kv, rows ? p.R : p.T, HD, rows ? p.q_ld : p.k_ld,
+                                p.g, box_rows));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3(M_THREADS);
-  cfg.dynamicSmemBytes = M_SMEM<HD, FEW>;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = C;
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  AKVS_CUDA(cudaLaunchKernelEx(&cfg, mass_tc_kernel<T, HD, FEW>, tmK, tmQ, p, C, key_items, (int)n_items, BR, q_boxes,
-                               std::is_same<T, f16>::value ? tc::kF16 : tc::kBF16));
+  if (is_few) {
+    cfg.gridDim = dim3((unsigned)(n_items < 148 ? n_items : 148));
+    cfg.dynamicSmemBytes = few::SMEM<HD>;
+    cfg.numAttrs = 1;
+    AKVS_CUDA(cudaLaunchKernelEx(&cfg, few::mass_few_kernel<T, HD>, tmK, tmQ, p, cols, key_items, (int)n_items, fmt));
+  } else {
+    const int row_tiles = akvs_cdiv(p.R, cols.BR);
+    int C = 1;
+    while (C < 8 && n_items * C * 2 <= 148 && row_tiles >= C * 4) C *= 2;
+    cfg.gridDim = dim3((unsigned)(C > 1 ? n_items * C : n_items < 148 ? n_items : 148));
+    cfg.dynamicSmemBytes = many::SMEM<HD>;
+    attr[1].val.clusterDim.x = C;
+    cfg.numAttrs = 2;
+    AKVS_CUDA(cudaLaunchKernelEx(&cfg, many::mass_many_kernel<T, HD>, tmK, tmQ, p, C, key_items, (int)n_items, cols.BR, boxes, fmt));
+  }
   AKVS_LAUNCHED();
   return AKVS_OK;
-}
-
-template <typename T, int HD>
-int32_t run_tc(const MassParams& p, cudaStream_t st) {
-  // up to 128 stacked rows: one tile of whole rows
-  return (int64_t)akvs_cdiv(p.R, 128 / p.g) <= 1 ? run_tc<T, HD, true>(p, st) : run_tc<T, HD, false>(p, st);
 }
 
 // ---- CUDA cores: 64 keys per CTA, the stacked rows 64 at a time, 4 x 4 scores per thread.
