@@ -414,106 +414,145 @@ __device__ __forceinline__ void cta_part(const SharedParams& p, const Tile& tl, 
   __syncthreads();                            // before another tile reuses the shared memory
 }
 
-// ---- float core: the same on the CUDA cores, 32 keys at a time through shared memory.
-constexpr int FK = 32;
+// ---- float core: 16 stacked rows on the CUDA cores, 64 keys at a time through shared memory.  A thread
+// forms 2 x 4 scores, then 4 rows x 4 columns of O: 6 and 2 shared-memory reads of 16 bytes for 32 and 16
+// products of 4 (a thread per row with 4 keys, 5 reads for 16 products, took 363 us where this takes
+// 145 us: 50 rows x 16 heads over 5000 keys).
+constexpr int FK = 64, FP_LD = MT + 4;
 template <int HD, typename Lim>
 __device__ __forceinline__ void cta_part_f32(const SharedParams& p, const Tile& tl, const float* k, const float* v, int64_t ld,
-                                             int start, int end, const Lim& lim, uint8_t* smem, int part) {
-  constexpr int LD = HD + 4, OC = HD / 32;
+                                             int start, int end, int all_see, const Lim& lim, uint8_t* smem, int part) {
+  constexpr int LD = HD + 4, CH = HD / 4;
   float* kt = reinterpret_cast<float*>(smem); // [FK][LD]
   float* vt = kt + FK * LD;                   // [FK][LD]
   float* qt = vt + FK * LD;                   // [MT][LD]
-  float* pt = qt + MT * LD;                   // [MT][FK + 1]
-  const int m = threadIdx.x >> 3, e = threadIdx.x & 7;
-  for (int i = threadIdx.x; i < MT * HD / 4; i += DIR_THREADS) {
-    const int mm = i / (HD / 4), c = i % (HD / 4) * 4;
+  float* pt = qt + MT * LD;                   // [FK][FP_LD]: probabilities, a key per row
+  float* ft = pt + FK * FP_LD;                // [MT]: what O is rescaled by
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rp = tid >> 4, kq = tid & 15;     // scores of rows 2 rp, 2 rp + 1 and keys kq + 16 j
+  const int col = lane % CH * 4, sub = lane / CH;      // O: rows 4 warp .., columns col ..; head_dim 64: the half-warps share the keys
+  for (int i = tid; i < MT * CH; i += DIR_THREADS) {
+    const int m = i / CH, c = i % CH * 4;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (tl.valid(mm))
-      x = __ldcg(reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.q) + (int64_t)tl.row(mm, p.g) * p.q_ld +
-                                                 (int64_t)tl.head(mm, p.g) * HD + c));
-    *reinterpret_cast<float4*>(qt + mm * LD + c) = x;
+    if (tl.valid(m))
+      x = __ldcg(reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.q) + (int64_t)tl.row(m, p.g) * p.q_ld +
+                                                 (int64_t)tl.head(m, p.g) * HD + c));
+    *reinterpret_cast<float4*>(qt + m * LD + c) = x;
   }
-  const int limit = min(lim(m), end);
-  float4 o[OC];
+  int limit[2], o_limit[4];
 #pragma unroll
-  for (int c = 0; c < OC; ++c) o[c] = make_float4(0.f, 0.f, 0.f, 0.f);
-  float mx = NO_MAX, sum = 0.f;
+  for (int a = 0; a < 2; ++a) limit[a] = min(lim(2 * rp + a), end);
+#pragma unroll
+  for (int r = 0; r < 4; ++r) o_limit[r] = min(lim(4 * warp + r), end);
+  float4 o[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) o[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+  float mx[2] = {NO_MAX, NO_MAX}, sum[2] = {0.f, 0.f};
   for (int key0 = start; key0 < end; key0 += FK) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < FK * HD / 4; i += DIR_THREADS) {
-      const int kk = i / (HD / 4), c = i % (HD / 4) * 4;
-      float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-      if (key0 + kk < end) {
-        a = __ldcg(reinterpret_cast<const float4*>(k + (int64_t)(key0 + kk) * ld + c));
-        b = __ldcg(reinterpret_cast<const float4*>(v + (int64_t)(key0 + kk) * ld + c));
-      }
-      *reinterpret_cast<float4*>(kt + kk * LD + c) = a;
-      *reinterpret_cast<float4*>(vt + kk * LD + c) = b;
+    __syncthreads();                          // the tile before is read
+    for (int i = tid; i < FK * CH; i += DIR_THREADS) {
+      const int kk = i / CH, c = i % CH * 4;
+      const bool ok = key0 + kk < end;        // keys behind the end arrive as zeros
+      const int64_t at = (int64_t)(ok ? key0 + kk : end - 1) * ld + c;
+      cp16(tc::smem_u32(kt + kk * LD + c), k + at, ok);
+      cp16(tc::smem_u32(vt + kk * LD + c), v + at, ok);
     }
+    cp_commit();
+    cp_wait<0>();
     __syncthreads();
-    float x[FK / 8];
+    float x[2][4];
 #pragma unroll
-    for (int j = 0; j < FK / 8; ++j) x[j] = 0.f;
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[a][j] = 0.f;
 #pragma unroll 4
     for (int c = 0; c < HD; c += 4) {
-      const float4 a = *reinterpret_cast<const float4*>(qt + m * LD + c);
+      float4 q[2], y[4];
 #pragma unroll
-      for (int j = 0; j < FK / 8; ++j) {
-        const float4 b = *reinterpret_cast<const float4*>(kt + (e + 8 * j) * LD + c);
-        x[j] = fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, fmaf(a.w, b.w, x[j]))));
+      for (int a = 0; a < 2; ++a) q[a] = *reinterpret_cast<const float4*>(qt + (2 * rp + a) * LD + c);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4*>(kt + (kq + 16 * j) * LD + c);
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          x[a][j] = fmaf(q[a].x, y[j].x, fmaf(q[a].y, y[j].y, fmaf(q[a].z, y[j].z, fmaf(q[a].w, y[j].w, x[a][j]))));
+    }
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      float top = mx[a];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[a][j] = key0 + kq + 16 * j < limit[a] ? x[a][j] * p.scale_log2 : -INFINITY;
+        top = fmaxf(top, x[a][j]);
+      }
+#pragma unroll
+      for (int w = 8; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, w));
+      const float f = exp2f(mx[a] - top);
+      mx[a] = top;
+      sum[a] *= f;
+      if (kq == 0) ft[2 * rp + a] = f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[a][j] = exp2f(x[a][j] - top);
+        sum[a] += x[a][j];
       }
     }
-    float top = mx;
 #pragma unroll
-    for (int j = 0; j < FK / 8; ++j) {
-      x[j] = key0 + e + 8 * j < limit ? x[j] * p.scale_log2 : -INFINITY;
-      top = fmaxf(top, x[j]);
+    for (int j = 0; j < 4; ++j) *reinterpret_cast<float2*>(pt + (kq + 16 * j) * FP_LD + 2 * rp) = make_float2(x[0][j], x[1][j]);
+    __syncthreads();
+    const float4 f4 = *reinterpret_cast<const float4*>(ft + 4 * warp);
+    const float fr[4] = {f4.x, f4.y, f4.z, f4.w};
+#pragma unroll
+    for (int r = 0; r < 4; ++r) { o[r].x *= fr[r]; o[r].y *= fr[r]; o[r].z *= fr[r]; o[r].w *= fr[r]; }
+    const bool every = key0 + FK <= all_see || all_see >= end;
+    auto add = [&](int kk, bool check) {
+      const float4 y4 = *reinterpret_cast<const float4*>(pt + kk * FP_LD + 4 * warp);
+      const float4 b = *reinterpret_cast<const float4*>(vt + kk * LD + col);
+      const float y[4] = {y4.x, y4.y, y4.z, y4.w};
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (!check || key0 + kk < o_limit[r]) {       // a hidden key's V may be NaN: it is not touched
+          o[r].x = fmaf(y[r], b.x, o[r].x); o[r].y = fmaf(y[r], b.y, o[r].y);
+          o[r].z = fmaf(y[r], b.z, o[r].z); o[r].w = fmaf(y[r], b.w, o[r].w);
+        }
+    };
+    if (every) {
+#pragma unroll 8
+      for (int kk = sub; kk < FK; kk += 32 / CH) add(kk, false);
+    } else {
+      for (int kk = sub; kk < FK; kk += 32 / CH) add(kk, true);
     }
-#pragma unroll
-    for (int s = 4; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
-    const float f = exp2f(mx - top);
-    mx = top;
-    sum *= f;
-#pragma unroll
-    for (int c = 0; c < OC; ++c) { o[c].x *= f; o[c].y *= f; o[c].z *= f; o[c].w *= f; }
-#pragma unroll
-    for (int j = 0; j < FK / 8; ++j) {
-      const float y = exp2f(x[j] - top);
-      sum += y;
-      pt[m * (FK + 1) + e + 8 * j] = y;
-    }
-    __syncwarp();                             // a row's eight threads are in one warp
-    const int n = min(FK, limit - key0);      // hidden keys are not touched: their V may be NaN
-    for (int kk = 0; kk < n; ++kk) {
-      const float y = pt[m * (FK + 1) + kk];
-#pragma unroll
-      for (int c = 0; c < OC; ++c) {
-        const float4 b = *reinterpret_cast<const float4*>(vt + kk * LD + 32 * c + 4 * e);
-        o[c].x = fmaf(y, b.x, o[c].x); o[c].y = fmaf(y, b.y, o[c].y);
-        o[c].z = fmaf(y, b.z, o[c].z); o[c].w = fmaf(y, b.w, o[c].w);
-      }
-    }
-    __syncwarp();
   }
 #pragma unroll
-  for (int s = 4; s > 0; s >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, s);
-  if (tl.valid(m)) {
+  for (int a = 0; a < 2; ++a)
 #pragma unroll
-    for (int c = 0; c < OC; ++c) store_part<HD>(p, tl, part, m, 32 * c + 4 * e, o[c]);
-    if (e == 0) store_ml(p, tl, part, m, mx, sum);
+    for (int w = 8; w > 0; w >>= 1) sum[a] += __shfl_xor_sync(0xFFFFFFFFu, sum[a], w);
+  if constexpr (CH < 32) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      o[r].x += __shfl_xor_sync(0xFFFFFFFFu, o[r].x, CH); o[r].y += __shfl_xor_sync(0xFFFFFFFFu, o[r].y, CH);
+      o[r].z += __shfl_xor_sync(0xFFFFFFFFu, o[r].z, CH); o[r].w += __shfl_xor_sync(0xFFFFFFFFu, o[r].w, CH);
+    }
   }
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (sub == 0 && tl.valid(4 * warp + r)) store_part<HD>(p, tl, part, 4 * warp + r, col, o[r]);
+#pragma unroll
+  for (int a = 0; a < 2; ++a)
+    if (kq == 0 && tl.valid(2 * rp + a)) store_ml(p, tl, part, 2 * rp + a, mx[a], sum[a]);
   __syncthreads();                            // before another tile reuses the shared memory
 }
 
 template <typename T, int HD> constexpr int direct_smem() {
-  return std::is_same<T, float>::value ? (2 * FK * (HD + 4) + MT * (HD + 4) + MT * (FK + 1)) * 4 : DIR_WARPS * ST * STAGE<HD>;
+  return std::is_same<T, float>::value ? (2 * FK * (HD + 4) + MT * (HD + 4) + FK * FP_LD + MT) * 4 : DIR_WARPS * ST * STAGE<HD>;
 }
 
 template <typename T, int HD, int NT, typename Lim>
 __device__ __forceinline__ void tile_part(const SharedParams& p, const Tile& tl, const T* k, const T* v, int64_t ld, int start,
                                           int end, int all_see, const Lim& lim, uint8_t* smem, int part) {
   if constexpr (std::is_same<T, float>::value)
-    cta_part_f32<HD>(p, tl, k, v, ld, start, end, lim, smem, part);
+    cta_part_f32<HD>(p, tl, k, v, ld, start, end, all_see, lim, smem, part);
   else
     cta_part<T, HD, NT>(p, tl, k, v, ld, start, end, all_see, lim, smem, part);
 }
@@ -714,13 +753,12 @@ Plan make_plan(bool is16, int R, int P, int S, int cap, int g, int n_kv, int hd,
     pl.tc = true;
     pl.split_len = akvs_cdiv(tiles, best) * 128;
   } else if (P > 0) {
-    // Two CTAs fit an SM; one runs 64 keys at a time (32 of the float kernel).
+    // Two CTAs fit an SM; one runs 64 keys at a time.
     if (is16 && (int64_t)R * g <= 8) pl.nt = 1;
-    const int unit = is16 ? 64 : 32;
     const int64_t base = (int64_t)n_kv * akvs_cdiv((int64_t)R * g, 8 * pl.nt);
-    const int units = akvs_cdiv(P, unit);
+    const int units = akvs_cdiv(P, 64);
     const int splits = (int)(base >= 296 ? 1 : akvs_cdiv(296, base));
-    pl.split_len = akvs_cdiv(units, splits < units ? splits : units) * unit;
+    pl.split_len = akvs_cdiv(units, splits < units ? splits : units) * 64;
   }
   if (P > 0) pl.splits = akvs_cdiv(P, pl.split_len);
   // Stacked rows of a sequence: g, or the mean of a ragged batch.  Ragged batches get room for twice
