@@ -638,8 +638,11 @@ int32_t run_tc(const MassParams& p, cudaStream_t st) {
   return AKVS_OK;
 }
 
-// ---- CUDA cores: 64 keys per CTA, the stacked rows 64 at a time, 4 x 4 scores per thread.
-constexpr int SK = 64, SR = 64, S_THREADS = 256;
+// ---- CUDA cores (float): 64 keys per CTA, the stacked rows SR at a time, SR/16 x 4 scores per thread.
+// 64 rows a tile are bound by the products (64 rows x 16 heads over 20000 keys: 189 us, 28 TFLOP/s); up to
+// 16 rows take small tiles, which leave room for more CTAs on an SM to read K.  Few keys and many rows: a
+// cluster shares the row tiles and adds its sums through distributed shared memory.
+constexpr int SK = 64, S_THREADS = 256;
 
 template <typename T, int HD>
 __device__ __forceinline__ void load_row_chunk(float* dst, const T* src, bool ok) {
@@ -655,10 +658,10 @@ __device__ __forceinline__ void load_row_chunk(float* dst, const T* src, bool ok
   for (int i = 0; i < V; i += 4) *reinterpret_cast<float4*>(dst + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
 }
 
-template <typename T, int HD>
+template <typename T, int HD, int SR>
 __global__ void __launch_bounds__(S_THREADS)
-mass_simt_kernel(const __grid_constant__ MassParams p) {
-  constexpr int LD = HD + 4, V = VecOf<T>::N, CH = HD / V;
+mass_simt_kernel(const __grid_constant__ MassParams p, int C) {
+  constexpr int LD = HD + 4, V = VecOf<T>::N, CH = HD / V, RPT = SR / 16;
   extern __shared__ __align__(16) float sm[];
   float* kt = sm;                    // [SK][LD]
   float* qt = kt + SK * LD;          // [SR][LD]
@@ -667,14 +670,14 @@ mass_simt_kernel(const __grid_constant__ MassParams p) {
   __shared__ float part[16][SK];
   pdl_trigger();
   pdl_wait();
-  const int h = blockIdx.y, j0 = blockIdx.x * SK, tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
+  const int rank = blockIdx.x % C, h = blockIdx.y, j0 = blockIdx.x / C * SK, tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
   const int rows = p.R * p.g;
   for (int i = tid; i < SK * CH; i += S_THREADS) {
     const int j = i / CH, c = i % CH * V;
     load_row_chunk<T, HD>(kt + j * LD + c, (const T*)p.k + (int64_t)min(j0 + j, p.T - 1) * p.k_ld + (int64_t)h * HD + c, j0 + j < p.T);
   }
   float acc[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int m0 = 0; m0 < rows; m0 += SR) {
+  for (int m0 = rank * SR; m0 < rows; m0 += C * SR) {
     __syncthreads();
     bool any = false;
     if (tid < SR) {
@@ -693,27 +696,27 @@ mass_simt_kernel(const __grid_constant__ MassParams p) {
                             (const T*)p.q + (int64_t)(mm / p.g) * p.q_ld + (int64_t)(h * p.g + mm % p.g) * HD + c, m < rows);
     }
     __syncthreads();
-    float s[4][4];
+    float s[RPT][4];
 #pragma unroll
-    for (int a = 0; a < 4; ++a)
+    for (int a = 0; a < RPT; ++a)
 #pragma unroll
       for (int b = 0; b < 4; ++b) s[a][b] = 0.f;
 #pragma unroll 4
     for (int c = 0; c < HD; c += 4) {
-      float4 x[4], y[4];
+      float4 x[RPT], y[4];
 #pragma unroll
-      for (int a = 0; a < 4; ++a) x[a] = *reinterpret_cast<const float4*>(qt + (ty * 4 + a) * LD + c);
+      for (int a = 0; a < RPT; ++a) x[a] = *reinterpret_cast<const float4*>(qt + (ty * RPT + a) * LD + c);
 #pragma unroll
       for (int b = 0; b < 4; ++b) y[b] = *reinterpret_cast<const float4*>(kt + (tx + 16 * b) * LD + c);
 #pragma unroll
-      for (int a = 0; a < 4; ++a)
+      for (int a = 0; a < RPT; ++a)
 #pragma unroll
         for (int b = 0; b < 4; ++b)
           s[a][b] = fmaf(x[a].x, y[b].x, fmaf(x[a].y, y[b].y, fmaf(x[a].z, y[b].z, fmaf(x[a].w, y[b].w, s[a][b]))));
     }
 #pragma unroll
-    for (int a = 0; a < 4; ++a) {
-      const int m = ty * 4 + a, lo = row_lo[m], hi = row_hi[m];
+    for (int a = 0; a < RPT; ++a) {
+      const int m = ty * RPT + a, lo = row_lo[m], hi = row_hi[m];
       const float z = row_lse[m];
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
@@ -725,26 +728,60 @@ mass_simt_kernel(const __grid_constant__ MassParams p) {
 #pragma unroll
   for (int b = 0; b < 4; ++b) part[ty][tx + 16 * b] = acc[b];
   __syncthreads();
-  if (tid < SK && j0 + tid < p.T) {
+  __shared__ float tot[SK];
+  if (tid < SK) {
     float s = 0.f;
 #pragma unroll
     for (int y = 0; y < 16; ++y) s += part[y][tid];
+    tot[tid] = s;
+  }
+  if (C > 1) tc::cluster_sync_all();
+  if (rank == 0 && tid < SK && j0 + tid < p.T) {
+    float s = tot[tid];
+    for (int c = 1; c < C; ++c) {
+      float x;
+      asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(tc::map_to_rank(tc::smem_u32(&tot[tid]), c)) : "memory");
+      s += x;
+    }
     const int64_t at = (int64_t)h * p.T + j0 + tid;
     p.mass_out[at] = (p.mass_in ? p.mass_in[at] : 0.f) + s;
   }
+  if (C > 1) tc::cluster_sync_all();
 }
 
-template <typename T, int HD>
+template <typename T, int HD, int SR>
 int32_t run_simt(const MassParams& p, cudaStream_t st) {
   constexpr int smem = (SK + SR) * (HD + 4) * 4;
   static bool attr_set = false;
   if (!attr_set) {
-    AKVS_CUDA(cudaFuncSetAttribute(mass_simt_kernel<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    AKVS_CUDA(cudaFuncSetAttribute(mass_simt_kernel<T, HD, SR>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     attr_set = true;
   }
-  AKVS_CUDA(launch_pdl(mass_simt_kernel<T, HD>, dim3(akvs_cdiv(p.T, SK), p.n_kv), dim3(S_THREADS), smem, st, p));
+  const int64_t ctas = (int64_t)akvs_cdiv(p.T, SK) * p.n_kv;
+  const int row_tiles = akvs_cdiv((int64_t)p.R * p.g, SR);
+  int C = 1;
+  while (C < 8 && ctas * C * 2 <= 296 && row_tiles >= C * 2) C *= 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(akvs_cdiv(p.T, SK) * C), p.n_kv);
+  cfg.blockDim = dim3(S_THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = C;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  AKVS_CUDA(cudaLaunchKernelEx(&cfg, mass_simt_kernel<T, HD, SR>, p, C));
   AKVS_LAUNCHED();
   return AKVS_OK;
+}
+template <typename T, int HD>
+int32_t run_simt(const MassParams& p, cudaStream_t st) {
+  return (int64_t)p.R * p.g <= 16 ? run_simt<T, HD, 16>(p, st) : run_simt<T, HD, 64>(p, st);
 }
 
 }  // namespace
