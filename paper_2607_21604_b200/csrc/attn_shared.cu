@@ -676,8 +676,8 @@ join_kernel(const __grid_constant__ SharedParams p) {
         float x[UN][V];
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
-          // a part without a key (weight times zeros) is read like the others; beyond the last one nothing is
-          const float* src = p.part_o + ((int64_t)(sub + (b + min(c + u, n - 1)) * WPR) * rows + at) * HD + lane * V;
+          if (c + u >= n) break;               // (the same for the whole warp)
+          const float* src = p.part_o + ((int64_t)(sub + (b + c + u) * WPR) * rows + at) * HD + lane * V;
           if constexpr (V == 4) {
             const float4 y = __ldcg(reinterpret_cast<const float4*>(src));
             x[u][0] = y.x; x[u][1] = y.y; x[u][2] = y.z; x[u][3] = y.w;
@@ -688,10 +688,10 @@ join_kernel(const __grid_constant__ SharedParams p) {
         }
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
-          const float wu = __shfl_sync(0xFFFFFFFFu, w, min(c + u, 31));
-          if (c + u < n)
+          if (c + u >= n) break;
+          const float wu = __shfl_sync(0xFFFFFFFFu, w, c + u);
 #pragma unroll
-            for (int i = 0; i < V; ++i) o[i] = fmaf(wu, x[u][i], o[i]);
+          for (int i = 0; i < V; ++i) o[i] = fmaf(wu, x[u][i], o[i]);
         }
       }
     }
