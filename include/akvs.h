@@ -326,8 +326,10 @@ int32_t akvs_op_quantize(int32_t dtype, const void* x, int32_t n, int32_t n_kv_h
  * other output, unless stated (AKVS_ERR_INVALID_ARG).  dtype outside the three types:
  * AKVS_ERR_UNSUPPORTED; a stride shorter than its row, n_q_heads no multiple of n_kv_heads or
  * more than 128 query heads per kv head: AKVS_ERR_SHAPE.  All are asynchronous, read nothing
- * on the host, and may be captured into a CUDA graph after one eager call.  Arrays of lengths,
- * offsets and key ranges are device memory and are read when the kernels run.
+ * on the host, and may be captured into a CUDA graph after one eager call of the same sizes.
+ * Arrays of lengths, offsets and key ranges are device memory and are read when the kernels
+ * run.  There is no status word: should a bounded wait in a kernel run out, the outputs
+ * concerned are NaN.
  * ------------------------------------------------------------------------------------ */
 
 /* RMSNorm of every query and key head with its own gain, then RoPE, in one pass:
@@ -349,7 +351,8 @@ int32_t akvs_op_qk_norm_rope(int32_t dtype, const void* q, int64_t q_ld, const v
  *   q_off[s+1] - 1 are the new tokens of sequence s, its last ones: device [S+1], non-decreasing.
  * Row i of the n rows of a sequence sees the whole context and the first own_len[s] - (n - 1 - i)
  * of its sequence's tokens (its own K/V are expected in the slot already).  What a row does not
- * see never reaches it, NaN and infinities included.  Scores are scaled by 1/sqrt(head_dim).
+ * see never reaches it, NaN and infinities included (an infinity in a V that it does see gives
+ * infinity or NaN).  Scores are scaled by 1/sqrt(head_dim).
  *   out [R][n_q][hd], contiguous; lse float [R][n_q]: log of the row's sum of exponentials.
  * A row that sees nothing gives zeros and lse = -inf; rows of no sequence are left as they were.
  * Values of own_len outside [0, cap] and of q_off outside [0, R] are clamped, a range that runs

@@ -307,7 +307,13 @@ mass_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
       }
       if (key < p.T) p.mass_out[at] = old + total(acc);
     }
-    if (!ok) *abort_flag = 1;
+    if (!ok) {                                            // a wait ran out: NaN rather than masses that lack terms
+      *abort_flag = 1;
+      for (int item = item0; item < item1; ++item) {
+        const int key = (item % key_items) * (2 * BK) + w * BK + m;
+        if (key < p.T) p.mass_out[(int64_t)(item / key_items) * p.T + key] = NAN;
+      }
+    }
   }
   if (*abort_flag) __nanosleep(200000);
   tc::fence_before_sync();
@@ -554,7 +560,14 @@ mass_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         part[w * 128 + m] = sum;
       }
     }
-    if (!ok) *abort_flag = 1;
+    if (!ok) {                                            // a wait ran out: NaN rather than masses that lack terms
+      *abort_flag = 1;
+      part[w * 128 + m] = NAN;
+      for (int item = item0; item < n_items && C == 1; item += step) {
+        const int key = (item % key_items) * (2 * BK) + w * BK + m;
+        if (key < p.T) p.mass_out[(int64_t)(item / key_items) * p.T + key] = NAN;
+      }
+    }
   }
   if (*abort_flag) __nanosleep(200000);
   tc::fence_before_sync();
@@ -585,12 +598,9 @@ mass_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
 
 template <typename T, int HD>
 int32_t run_tc(const MassParams& p, cudaStream_t st) {
-  static bool attr_set = false;
-  if (!attr_set) {
-    AKVS_CUDA(cudaFuncSetAttribute(few::mass_few_kernel<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, few::SMEM<HD>));
-    AKVS_CUDA(cudaFuncSetAttribute(many::mass_many_kernel<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, many::SMEM<HD>));
-    attr_set = true;
-  }
+  static std::atomic<uint64_t> few_set{0}, many_set{0};
+  AKVS_CUDA(smem_opt_in((const void*)few::mass_few_kernel<T, HD>, few::SMEM<HD>, few_set));
+  AKVS_CUDA(smem_opt_in((const void*)many::mass_many_kernel<T, HD>, many::SMEM<HD>, many_set));
   const uint32_t fmt = std::is_same<T, f16>::value ? tc::kF16 : tc::kBF16;
   const bool rows = p.R > 0, is_few = (int64_t)p.R * p.g <= few::BQ;
   const int key_items = akvs_cdiv(p.T, 2 * BK);
@@ -752,11 +762,8 @@ mass_simt_kernel(const __grid_constant__ MassParams p, int C) {
 template <typename T, int HD, int SR>
 int32_t run_simt(const MassParams& p, cudaStream_t st) {
   constexpr int smem = (SK + SR) * (HD + 4) * 4;
-  static bool attr_set = false;
-  if (!attr_set) {
-    AKVS_CUDA(cudaFuncSetAttribute(mass_simt_kernel<T, HD, SR>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    attr_set = true;
-  }
+  static std::atomic<uint64_t> smem_set{0};
+  AKVS_CUDA(smem_opt_in((const void*)mass_simt_kernel<T, HD, SR>, smem, smem_set));
   const int64_t ctas = (int64_t)akvs_cdiv(p.T, SK) * p.n_kv;
   const int row_tiles = akvs_cdiv((int64_t)p.R * p.g, SR);
   int C = 1;

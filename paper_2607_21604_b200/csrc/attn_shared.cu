@@ -786,11 +786,8 @@ int64_t parts_bytes(const Plan& pl, int R, int n_q, int hd) {
 template <typename T, int HD, int NT, bool WIDE>
 int32_t launch_direct(const SharedParams& p, const Plan& pl, cudaStream_t st) {
   constexpr int smem = direct_smem<T, HD>();
-  static bool attr_set = false;
-  if (!attr_set) {
-    AKVS_CUDA(cudaFuncSetAttribute(direct_kernel<T, HD, NT, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    attr_set = true;
-  }
+  static std::atomic<uint64_t> smem_set{0};
+  AKVS_CUDA(smem_opt_in((const void*)direct_kernel<T, HD, NT, WIDE>, smem, smem_set));
   const int64_t n_ctx = (int64_t)p.splits * akvs_cdiv((int64_t)p.R * p.g, 8 * NT);
   const int64_t grid = n_ctx + (int64_t)p.S * p.own_splits * pl.z;
   if (grid > 0x7fffffff) return AKVS_ERR_TOO_LARGE;
@@ -803,11 +800,8 @@ int32_t launch_direct(const SharedParams& p, const Plan& pl, cudaStream_t st) {
 template <typename T, int HD, int NT, bool WIDE>
 int32_t launch_own(const SharedParams& p, const Plan& pl, cudaStream_t st) {
   constexpr int smem = direct_smem<T, HD>();
-  static bool attr_set = false;
-  if (!attr_set) {
-    AKVS_CUDA(cudaFuncSetAttribute(own_kernel<T, HD, NT, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    attr_set = true;
-  }
+  static std::atomic<uint64_t> smem_set{0};
+  AKVS_CUDA(smem_opt_in((const void*)own_kernel<T, HD, NT, WIDE>, smem, smem_set));
   AKVS_CUDA(launch_pdl(own_kernel<T, HD, NT, WIDE>, dim3((unsigned)(p.S * p.own_splits), p.n_kv, pl.z), dim3(DIR_THREADS), smem, st, p));
   AKVS_LAUNCHED();
   return AKVS_OK;

@@ -397,6 +397,10 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
     if (ok && !tc::mbar_wait(&bar[B_FIN + quad], 0, abort_flag)) ok = false;
     if (ok && n_tiles > 0 && !tc::mbar_wait(&bar[B_OFINAL], 0, abort_flag)) ok = false;
     if (!ok && lane == 0) { *abort_flag = 1; set_status(p.status, AKVS_ERR_TIMEOUT); }
+    if (PART && !ok && valid) {                     // no status word: the rows become NaN where the parts are joined
+      const size_t row = (size_t)split * p.R * p.n_q + (size_t)r * p.n_q + (size_t)hk * p.g + head;
+      p.part_ml[row] = make_float2(0.f, NAN);
+    }
     if (ok) {
       tc::fence_after_sync();
       const float ma = m_part[m], mb = m_part[128 + m];
@@ -446,11 +450,8 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
 
 template <typename T, int HD, bool PART>
 int32_t launch(AttnParams& p, const void* k, const void* v, int64_t kv_ld, int n_cta, cudaStream_t st) {
-  static bool attr_set = false;
-  if (!attr_set) {
-    AKVS_CUDA(cudaFuncSetAttribute(attention_tc_kernel<T, HD, PART>, cudaFuncAttributeMaxDynamicSharedMemorySize, ATT_SMEM<HD>));
-    attr_set = true;
-  }
+  static std::atomic<uint64_t> smem_set{0};
+  AKVS_CUDA(smem_opt_in((const void*)attention_tc_kernel<T, HD, PART>, ATT_SMEM<HD>, smem_set));
   p.scale_log2 = 1.4426950408889634f / sqrtf((float)HD);
   const uint32_t fmt = std::is_same<T, f16>::value ? tc::kF16 : tc::kBF16;
   p.idesc_qk = tc::idesc_f16(fmt, 128, BN, 0);

@@ -5,6 +5,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <stdint.h>
+#include <atomic>
 
 #include "akvs.h"
 
@@ -205,6 +206,19 @@ static inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 b
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+
+// Opt-in of a kernel to more than 48 KB of dynamic shared memory, once per device: `done` has a bit
+// for each device that has it.
+static inline cudaError_t smem_opt_in(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  const cudaError_t r = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (r == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return r;
 }
 
 // Device status word: first error wins.
