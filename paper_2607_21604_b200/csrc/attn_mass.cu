@@ -332,7 +332,9 @@ mass_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
 // 512 rows x 40 heads x 32768 keys: 229 to 238 us, of which the exponentials are 160 us (16 per clock and
 // SM).  Built and measured instead of it: 128 columns with two buffers 238 us (against 229); an issuing
 // thread per group (and a warp less for the columns) 237 us; K in tensor memory as the A operand with
-// tiles of 96 columns, two groups of two buffers 276 us, three groups of one buffer 253 us.
+// tiles of 96 columns, two groups of two buffers 276 us, three groups of one buffer 253 us; exp2 of an
+// eighth / a quarter / half of the columns by a polynomial on the FMA units 235 / 239 / 261 us (against
+// 236): two warps per scheduler do not hide its chain.
 namespace many {
 constexpr int BQ = 256, QST = 2;
 template <int HD> constexpr int KTILE = HD / 64 * M_SLAB;                // 128 keys
