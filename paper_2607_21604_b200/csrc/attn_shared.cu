@@ -736,22 +736,44 @@ Plan make_plan(bool is16, int R, int P, int S, int cap, int g, int n_kv, int hd,
   // Up to one tile of stacked rows on mma.sync, more on tcgen05: over 12416 tokens of 8 kv heads one
   // tile takes 17.2 us on mma.sync, two tiles 22.0 us against 18.3 us on tcgen05, four 42.8 against 20.8.
   if (P > 0 && is16 && (int64_t)R * g > MT) {
-    // One CTA per SM.  In units of a key tile (0.85 us): rounds of CTAs times (a CTA's tiles + 9 for its
-    // start and end), plus writing and reading the parts at memory speed.  A last round that is not
-    // full counts half of what it leaves idle: own tokens and the next CTAs' starts use some of it
-    // (58 row blocks x 2 heads over 128 tiles, 1 / 2 / 4 / 5 / 14 splits: 150 / 144 / 155 / 152 / 209 us).
+    // One CTA per SM, longer key ranges first: every split but the last has `len` tiles, the last what is
+    // left.  In units of a key tile (0.85 us), with 9 for a CTA's start and end, the CTAs of the last split
+    // fill what the last round of the others leaves idle.  The mean of that end and of the work per SM
+    // counts, since CTAs do not run in step and own tokens use idle SMs, plus writing and reading the
+    // parts at memory speed (58 row blocks x 2 heads over 128 tiles: 108 + 20 tiles 137 us, 64 + 64 146 us;
+    // one row block x 8 heads over 97 tiles: 11 splits 19.5 us, 17 splits 22.6 us).
     const int64_t base = (int64_t)akvs_cdiv(R, 128 / g) * n_kv;
     const int tiles = akvs_cdiv(P, 128);
     const double part = 2.0 * R * g * n_kv * (hd + 2) * 4 / 6.4e6 / 0.85;
-    int best = 1;
+    int best = tiles, last = 0;
     double best_cost = 1e300;
+    auto consider = [&](int len, double uneven) {
+      const int s = (tiles + len - 1) / len, longs = s > 1 ? (s - 1) * (int)base : 0, q = longs / 148, r = longs % 148;
+      const double a = len + 9, b = tiles - (s - 1) * len + 9;
+      double end;
+      const int64_t fit = r > 0 ? (int)(a / b) * (148 - r) : 0;        // last ones that end with the others
+      if (r > 0 && fit >= base) end = (q + 1) * a;
+      else end = (q + (r > 0)) * a + (double)((base - fit + 147) / 148) * b;
+      const double work = (longs * a + base * b) * (1.0 / 148);
+      const double cost = uneven * (0.5 * (end + work) + part * s);
+      if (cost < best_cost) { best_cost = cost; best = len; }
+    };
     for (int s = 1; s <= tiles && (s == 1 || base * s <= 3 * 148); ++s) {
-      const double full = (double)((base * s + 147) / 148), used = base * s / 148.0;
-      const double cost = 0.5 * (full + (used > 1.0 ? used : 1.0)) * (akvs_cdiv(tiles, s) + 9) + part * s;
-      if (cost < best_cost) { best_cost = cost; best = s; }
+      const int even = (tiles + s - 1) / s;
+      if (even == last) continue;
+      last = even;
+      consider(even, 1.0);
+      // a last split so short that k of its CTAs take as long as one of the others; it has to gain 2 %
+      // over equal ones, which leave idle SMs to the own tokens from the start (32 row blocks and heads
+      // over 256 tiles with 268 MB of own tokens: 4 equal splits 126 us, 4 x 58 + 24 tiles 128 us)
+      const int r = s > 1 ? (s - 1) * (int)base % 148 : 0, k = r > 0 ? ((int)base + 147 - r) / (148 - r) : 1;
+      if (k > 1) {
+        const int len = (int)((k * (tiles + 9.0) - 9) / (1 + (double)k * (s - 1))) + 1;
+        if (len < tiles) consider(len, 1.02);
+      }
     }
     pl.tc = true;
-    pl.split_len = akvs_cdiv(tiles, best) * 128;
+    pl.split_len = best * 128;
   } else if (P > 0) {
     // Two CTAs fit an SM; one runs 64 keys at a time.
     if (is16 && (int64_t)R * g <= 8) pl.nt = 1;
@@ -830,7 +852,7 @@ int32_t run(SharedParams& p, int dtype, const Plan& pl, cudaStream_t st) {
   // time; more of them would start late and find little.
   const bool few = (int64_t)p.R * p.n_q <= 2048 && p.splits + p.own_splits > 8;
   const int64_t rows = p.q_off ? (int64_t)akvs_cdiv(p.R, p.S) * p.g * 2 : p.g, per = few ? 1 : DIR_WARPS;
-  const int64_t fit = akvs_cdiv(148 * 8, (int64_t)p.S * p.n_kv), need = (rows + per - 1) / per;
+  const int64_t fit = akvs_cdiv(148 * 15, (int64_t)p.S * p.n_kv), need = (rows + per - 1) / per;
   const dim3 grid(p.S, p.n_kv, (unsigned)(need < fit ? need : fit < 1 ? 1 : fit));
   if (few) AKVS_CUDA(launch_pdl(join_kernel<T, HD, 4>, grid, dim3(DIR_THREADS), 0, st, p));
   else AKVS_CUDA(launch_pdl(join_kernel<T, HD, 1>, grid, dim3(DIR_THREADS), 0, st, p));
