@@ -247,6 +247,14 @@ def test_shared_many_rows(akvs, dt, hd, nq, nkv, S, P):
     check_shared(akvs.op_attention_shared(*c[:5], ints(lens)), *c)
 
 
+@pytest.mark.parametrize("dt,hd,P", [(BF16, 64, 6090), (F16, 128, 6144), (F16, 64, 6018)])
+def test_shared_key_ranges_of_unequal_length(akvs, dt, hd, P):
+    """80 blocks of rows and heads, more than half of the SMs: a long and a short range of the context."""
+    rows = [60] * 5
+    c = shared_case(P, dt, hd, 32, 8, P, 70, [64, 70, 61, 60, 3], rows)
+    check_shared(akvs.op_attention_shared(*c[:5], ints(c[5]), ints(c[6])), *c)
+
+
 @pytest.mark.parametrize("dt", TYPES)
 @pytest.mark.parametrize("S", [2, 70])
 @pytest.mark.parametrize("shape", ["rising", "falling", "spiky"])
