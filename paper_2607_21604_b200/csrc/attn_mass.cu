@@ -89,7 +89,7 @@ struct ColumnLoad {                  // NW: key tiles of an item
       const bool real = ln.r_in[x] < cl.BR && rt * cl.BR + ln.r_in[x] < p.R;
       const int a = max(lo[x], 0), b = min(hi[x], p.T - 1);
       const bool blind = !real || z[x] == -INFINITY || a > b;              // such a column adds nothing
-      // columns of zeros behind the last row need no mask: exp2(0 - inf) = 0
+      // columns of zeros behind the last row ask for no mask (add_columns)
 #pragma unroll
       for (int w = 0; w < NW; ++w)
         masked[w] |= real && (blind || a > k0 + w * BK || b < min(k0 + (w + 1) * BK, p.T) - 1);
@@ -107,11 +107,16 @@ struct ColumnLoad {                  // NW: key tiles of an item
 };
 
 // N columns of a key's row of S^T: no branch inside, so that the loads, exponentials and sums of
-// different columns overlap.
+// different columns overlap.  Columns behind the last row hold a row of zeros and a z of -inf: exp2(0 - inf)
+// = 0 without a mask, unless the key holds an infinity or a NaN, with which 0 gives NaN.  Such columns end
+// a tile, so the last column shows it, and its NaN turns the mask on (for a real column, too: it changes
+// no result).  One compare and vote per 64 columns; the window of 512 rows x 40 heads over 32768 keys
+// takes as long as without.
 template <int N>
 __device__ __forceinline__ void add_columns(const float (&t)[N], const float* z, const int2* ranges, bool mask, int key,
                                             float scale2, float2 (&acc)[4]) {
   const float2 sc = make_float2(scale2, scale2);
+  mask |= __any_sync(0xFFFFFFFFu, t[N - 1] != t[N - 1]) != 0;
   if (!mask) {
 #pragma unroll
     for (int i = 0; i < N; i += 4) {
@@ -484,7 +489,7 @@ mass_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
             lo[x] = max(lo[x], 0);
             hi[x] = min(hi[x], p.T - 1);
             const bool blind = !real || z[x] == -INFINITY || lo[x] > hi[x];     // such a row adds nothing
-            // a column of zeros behind the last row needs no mask: exp2(0 - inf) = 0
+            // a column of zeros behind the last row asks for no mask (add_columns)
 #pragma unroll
             for (int w = 0; w < 2; ++w)
               masked[w] |= real && (blind || lo[x] > k0 + w * BK || hi[x] < min(k0 + (w + 1) * BK, p.T) - 1);
