@@ -189,7 +189,7 @@ struct WarpTile {
       for (int e = 0; e < 2; ++e) {
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
-          const float y = pr[x][2 * hf + e] * scale_log2;
+          const float y = __fmul_rn(pr[x][2 * hf + e], scale_log2);      // not fused with the subtraction below: both round alike
           pr[x][2 * hf + e] = every || key0 + 8 * hf + gr < limit[x][e] ? y : -INFINITY;
         }
         float top = fmaxf(pr[x][e], pr[x][2 + e]);
@@ -483,7 +483,7 @@ __device__ __forceinline__ void cta_part_f32(const SharedParams& p, const Tile& 
       float top = mx[a];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        x[a][j] = key0 + kq + 16 * j < limit[a] ? x[a][j] * p.scale_log2 : -INFINITY;
+        x[a][j] = key0 + kq + 16 * j < limit[a] ? __fmul_rn(x[a][j], p.scale_log2) : -INFINITY;
         top = fmaxf(top, x[a][j]);
       }
 #pragma unroll

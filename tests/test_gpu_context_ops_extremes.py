@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from test_gpu_context_ops import TYPES, gen, mass_case
+from test_gpu_context_ops import BF16, F16, F32, TINY, TYPES, gen, half, ints, mass_case, rnd
 
 pytestmark = pytest.mark.gpu
 
@@ -42,3 +42,69 @@ def test_mass_of_infinite_keys_that_all_rows_see(akvs, dt, hd, nq, nkv, R):
         rest = torch.ones(300, dtype=torch.bool, device="cuda")
         rest[at] = False
         assert torch.equal(got[:, rest], clean[:, rest])
+
+
+# ------------------------------------------------------------------------- scores far from zero
+
+# (type, values of q and k): sums of their products are exact, and the scores are about +-1.5e12 and +-1.5e9 in
+# units of log2
+FAR = [(F32, 2.0 ** 20, 1.375 * 2.0 ** 20),
+       (BF16, 2.0 ** 20, 1.375 * 2.0 ** 20), (BF16, 2.0 ** 20, -1.375 * 2.0 ** 20), (F16, 2.0 ** 15, 1.375 * 2.0 ** 15),
+       (F16, 2.0 ** 15, -1.375 * 2.0 ** 15)]
+WIDTH = 8                                                     # values of a row that are not zero
+
+
+def far_keys(n, nkv, hd, dt, kv):
+    """Keys of one score, but every third of a score so much lower that it has no weight."""
+    k = torch.zeros((n, nkv, hd), dtype=dt, device="cuda")
+    k[..., :WIDTH] = kv
+    k[::3, :, :WIDTH] = kv / 2 if kv > 0 else max(2 * kv, torch.finfo(dt).min)
+    return k
+
+
+def check_far(o, v, dt):
+    """The mean of the values that the rows see: v [n][n_kv][hd] with no weight on every third of each part."""
+    ref = v.double().mean(0).repeat_interleave(o.shape[1] // v.shape[1], 0)
+    mag = v.double().abs().mean(0).repeat_interleave(o.shape[1] // v.shape[1], 0)
+    # equal weights, which may be rounded once to the 16-bit type; sums of n terms in float
+    tol = half(dt) * ref.abs() + (2.0 ** -16 + (0.0 if dt == F32 else half(dt))) * mag + TINY[dt]
+    assert ((o.double() - ref).abs() <= tol).all(), (o.double() - ref).abs().max()
+
+
+def weighty(x):
+    keep = torch.ones(x.shape[0], dtype=torch.bool, device="cuda")
+    keep[::3] = False
+    return x[keep]
+
+
+@pytest.mark.parametrize("dt,qv,kv", FAR)
+@pytest.mark.parametrize("S", [1, 3, 9, 40])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_shared_attention_of_far_scores(akvs, dt, qv, kv, S, hd):
+    """The softmax depends on differences of scores alone, however far they are from zero."""
+    g = gen(S + hd)
+    nq, nkv, P, cap = 8, 2, 600, 45
+    q = torch.zeros((S, nq, hd), dtype=dt, device="cuda")
+    q[..., :WIDTH] = qv
+    ck, cv = far_keys(P, nkv, hd, dt, kv), rnd(g, P, nkv, hd, dt=dt)
+    one = far_keys(cap, nkv, hd, dt, kv)
+    sk, sv = one.expand(S, cap, nkv, hd).contiguous(), rnd(g, 1, cap, nkv, hd, dt=dt).expand(S, cap, nkv, hd).contiguous()
+    out, lse = akvs.op_attention_shared(q, ck, cv, sk, sv, ints([cap] * S))
+    v = torch.cat([weighty(cv), weighty(sv[0])])
+    check_far(out, v, dt)
+    top = qv * kv * WIDTH / math.sqrt(hd)
+    want = top + math.log(v.shape[0])
+    # seven roundings of up to 2^-24: log2(e), the root and its quotient, the product with the score, the sum
+    # with log2 of the row's sum, log(2) and its product
+    assert ((lse.double() - want).abs() <= 2.0 ** -21 * abs(want)).all()
+
+
+@pytest.mark.parametrize("dt,qv,kv", FAR)
+def test_attention_of_far_scores(akvs, dt, qv, kv):
+    g = gen(3)
+    nq, nkv, hd, n = 8, 2, 128, 400
+    q = torch.zeros((50, nq, hd), dtype=dt, device="cuda")
+    q[..., :WIDTH] = qv
+    k, v = far_keys(n, nkv, hd, dt, kv), rnd(g, n, nkv, hd, dt=dt)
+    lo, hi = ints([0] * 50), ints([n - 1] * 50)
+    check_far(akvs.op_attention(q, k, v, lo, hi), weighty(v), dt)
