@@ -29,6 +29,7 @@
 // value alone the rounding of P would cost the output as much accuracy as its own final rounding.
 // Scores, maxima, sums and O are float.
 #include "tc_common.cuh"
+#include <float.h>
 #include <math.h>
 
 namespace {
@@ -37,7 +38,8 @@ constexpr int DIR_WARPS = 4, DIR_THREADS = DIR_WARPS * 32;
 constexpr int MT = 16;                        // stacked rows of the largest tile
 constexpr int ST = 3;                         // stages of a warp's ring, 16 keys each
 constexpr int MAX_OWN_SPLITS = 64;
-constexpr float NO_MAX = -1.0e30f;            // running maximum before any key: exp2(x - NO_MAX) is never formed for x = -inf rows
+constexpr float NO_MAX = -FLT_MAX;            // running maximum before any key: below every finite score (in log2
+                                              // units they are products with less than 0.2), and exp2(-inf - NO_MAX) = 0
 constexpr float LN2 = 0.69314718f, LOG2E = 1.4426950408889634f;
 
 struct SharedParams {

@@ -40,6 +40,7 @@
 // splits so that few row blocks still fill the device, and a CTA leaves its rows' unnormalised
 // output, reference maximum and row sum in float for a later join; head_dim may also be 64.
 #include "tc_common.cuh"
+#include <float.h>
 
 namespace {
 
@@ -49,7 +50,7 @@ template <int HD> constexpr int TILE_OF = HD / 64 * SLAB;      // 32 KB for head
 constexpr int ATT_THREADS = 384;     // warp group 0: TMA / MMA, warp groups 1 and 2: softmax
 constexpr int K_STAGES = 3, V_STAGES = 4;
 constexpr float RESCALE_STEP = 8.f;  // the reference maximum may lag a tile's maximum by this much
-constexpr float NO_MAX = -1.0e30f;       // reference before any key
+constexpr float NO_MAX = -FLT_MAX;       // reference before any key: below a fifth of it lies no finite score in log2 units
 constexpr float FAR_MAX = 16777216.f;    // 2^24: up to here the rounding of a maximum shifts exponents by less than 1
 // shared memory: K[3] | V[4] | barriers | reference maxima and row sums
 // (float m_ref[128], l_part[2][128], m_part[2][128])

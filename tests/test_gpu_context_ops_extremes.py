@@ -46,9 +46,9 @@ def test_mass_of_infinite_keys_that_all_rows_see(akvs, dt, hd, nq, nkv, R):
 
 # ------------------------------------------------------------------------- scores far from zero
 
-# (type, values of q and k): sums of their products are exact, and the scores are about +-1.5e12 and +-1.5e9 in
-# units of log2
-FAR = [(F32, 2.0 ** 20, 1.375 * 2.0 ** 20),
+# (type, values of q and k): sums of their products are exact, and the scores are about -2e33, +-1.5e12 and
+# +-1.5e9 in units of log2
+FAR = [(F32, 2.0 ** 50, -1.375 * 2.0 ** 60), (BF16, 2.0 ** 50, -1.375 * 2.0 ** 60), (F32, 2.0 ** 20, 1.375 * 2.0 ** 20),
        (BF16, 2.0 ** 20, 1.375 * 2.0 ** 20), (BF16, 2.0 ** 20, -1.375 * 2.0 ** 20), (F16, 2.0 ** 15, 1.375 * 2.0 ** 15),
        (F16, 2.0 ** 15, -1.375 * 2.0 ** 15)]
 WIDTH = 8                                                     # values of a row that are not zero
