@@ -411,9 +411,14 @@ attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_consta
     if (ok && !tc::mbar_wait(&bar[B_FIN + quad], 0, abort_flag)) ok = false;
     if (ok && n_tiles > 0 && !tc::mbar_wait(&bar[B_OFINAL], 0, abort_flag)) ok = false;
     if (!ok && lane == 0) { *abort_flag = 1; set_status(p.status, AKVS_ERR_TIMEOUT); }
-    if (PART && !ok && valid) {                     // no status word: the rows become NaN where the parts are joined
+    if (PART && !ok && valid) {
+      // No status word: the row becomes NaN where the parts are joined.  The two groups of a row may fare
+      // differently, so each writes only what it would have written anyway: its half of O, and the first
+      // group the maximum and sum.
       const size_t row = (size_t)split * p.R * p.n_q + (size_t)r * p.n_q + (size_t)hk * p.g + head;
-      p.part_ml[row] = make_float2(0.f, NAN);
+      float* op = p.part_o + row * HD + grp * (HD / 2);
+      for (int i = 0; i < HD / 2; ++i) op[i] = NAN;
+      if (grp == 0) p.part_ml[row] = make_float2(0.f, NAN);
     }
     if (ok) {
       tc::fence_after_sync();
