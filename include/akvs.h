@@ -359,7 +359,9 @@ int32_t akvs_op_qk_norm_rope(int32_t dtype, const void* q, int64_t q_ld, const v
  * backwards is empty; ranges must not overlap.  P = 0 or cap = 0 (then own_k, own_v and own_len
  * may be NULL) are allowed.  head_dim 64 or 128.
  * scratch: device, 256-byte aligned, akvs_op_attention_shared_scratch_bytes(...) bytes (else
- * AKVS_ERR_WORKSPACE); two calls that may overlap on the GPU need two. */
+ * AKVS_ERR_WORKSPACE); two calls that may overlap on the GPU need two.  The size never shrinks when R,
+ * S, P or cap grows: one for the largest call (of the same type and heads) serves all smaller ones.
+ * It is -1 for arguments that the call refuses. */
 int64_t akvs_op_attention_shared_scratch_bytes(int32_t dtype, int32_t R, int32_t P, int32_t S, int32_t cap,
                                                int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim);
 int32_t akvs_op_attention_shared(int32_t dtype, const void* q, int64_t q_ld, int32_t R, const void* ctx_k,

@@ -802,9 +802,25 @@ Plan make_plan(bool is16, int R, int P, int S, int cap, int g, int n_kv, int hd,
   return pl;
 }
 
-int64_t parts_bytes(const Plan& pl, int R, int n_q, int hd) {
-  const int64_t rows = (int64_t)(pl.splits + pl.own_splits) * R * n_q;
-  return akvs_align_up(rows * hd * 4, 256) + akvs_align_up(rows * 8, 256) + 256;
+int64_t parts_bytes(int64_t rows, int hd) { return akvs_align_up(rows * hd * 4, 256) + akvs_align_up(rows * 8, 256) + 256; }
+int64_t part_rows(const Plan& pl, int R, int n_q) { return (int64_t)(pl.splits + pl.own_splits) * R * n_q; }
+
+// Rows of parts of any plan for up to R rows, P context tokens, cap own ones and any number of sequences:
+// it grows with each of them, which a single plan's need does not (fewer rows are split further).
+int64_t part_rows_bound(bool is16, int R, int P, int cap, int g, int n_kv) {
+  const int64_t n_q = (int64_t)n_kv * g;
+  auto least = [](int64_t a, int64_t b) { return a < b ? a : b; };
+  auto most = [](int64_t a, int64_t b) { return a > b ? a : b; };
+  int64_t ctx = 0;
+  // mma.sync and float: up to ceil(296 / base) splits of 64 keys or more, base >= r * n_q / MT
+  const int64_t r = is16 ? least(R, MT / g) : R;
+  if (r > 0) ctx = least(least(akvs_cdiv(P, 64), akvs_cdiv(296, n_kv)) * r * n_q, 296 * MT + r * n_q);
+  // tcgen05: at most 3 * 148 CTAs or one split, base >= r * n_q / 128
+  if (is16 && (int64_t)R * g > MT)
+    ctx = most(ctx, least(least(akvs_cdiv(P, 128), most(1, 3 * 148 / n_kv)) * R * n_q, most((int64_t)R * n_q, 3 * 148 * 128)));
+  int own = cap > 0;
+  while (own > 0 && own < MAX_OWN_SPLITS && (int64_t)n_kv * own * 2 <= 296 && cap / (own * 2) >= 128) own *= 2;
+  return ctx + own * (int64_t)R * n_q;
 }
 
 template <typename T, int HD, int NT, bool WIDE>
@@ -870,11 +886,8 @@ extern "C" int64_t akvs_op_attention_shared_scratch_bytes(int32_t dtype, int32_t
                                                           int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim) {
   if (dtype != AKVS_F32 && dtype != AKVS_BF16 && dtype != AKVS_F16) return -1;
   if (R < 0 || P < 0 || S < 0 || cap < 0 || !heads_ok(n_q_heads, n_kv_heads) || (head_dim != 64 && head_dim != 128)) return -1;
-  // one row per sequence and ragged rows are cut differently: room for either
-  const int g = n_q_heads / n_kv_heads;
-  const int64_t a = parts_bytes(make_plan(dtype != AKVS_F32, R, P, S, cap, g, n_kv_heads, head_dim, false), R, n_q_heads, head_dim);
-  const int64_t b = parts_bytes(make_plan(dtype != AKVS_F32, R, P, S, cap, g, n_kv_heads, head_dim, true), R, n_q_heads, head_dim);
-  return a > b ? a : b;
+  if ((int64_t)R * n_q_heads > 0x7fffffff) return -1;
+  return parts_bytes(part_rows_bound(dtype != AKVS_F32, R, P, cap, n_q_heads / n_kv_heads, n_kv_heads), head_dim);
 }
 
 extern "C" int32_t akvs_op_attention_shared(int32_t dtype, const void* q, int64_t q_ld, int32_t R, const void* ctx_k,
@@ -898,7 +911,7 @@ extern "C" int32_t akvs_op_attention_shared(int32_t dtype, const void* q, int64_
     return AKVS_ERR_INVALID_ARG;
   if ((int64_t)R * n_q_heads > 0x7fffffff || (int64_t)S * MAX_OWN_SPLITS > 0x7fffffff) return AKVS_ERR_TOO_LARGE;
   const Plan pl = make_plan(dtype != AKVS_F32, R, P, S, cap, n_q_heads / n_kv_heads, n_kv_heads, head_dim, q_off != nullptr);
-  const int64_t need = parts_bytes(pl, R, n_q_heads, head_dim);
+  const int64_t rows = part_rows(pl, R, n_q_heads), need = parts_bytes(rows, head_dim);
   if (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255) || scratch_size < need) return AKVS_ERR_WORKSPACE;
   const int64_t ctx_n = P > 0 ? ((P - 1) * ctx_ld + row) * es : 0;
   const int64_t own_n = cap > 0 ? ((S - 1) * own_seq_ld + (cap - 1) * own_ld + row) * es : 0;
@@ -918,7 +931,6 @@ extern "C" int32_t akvs_op_attention_shared(int32_t dtype, const void* q, int64_
   p.sk = own_k; p.sv = own_v; p.S = S; p.cap = cap; p.s_ld = own_ld; p.s_seq = own_seq_ld; p.s_len = own_len; p.q_off = q_off;
   p.out = out; p.lse = lse;
   p.splits = pl.splits; p.split_len = pl.split_len; p.own_splits = pl.own_splits;
-  const int64_t rows = (int64_t)(pl.splits + pl.own_splits) * R * n_q_heads;
   p.part_o = reinterpret_cast<float*>(scratch);
   p.part_ml = reinterpret_cast<float2*>(reinterpret_cast<char*>(scratch) + akvs_align_up(rows * head_dim * 4, 256));
   p.scale_log2 = LOG2E / sqrtf((float)head_dim);
