@@ -509,6 +509,8 @@ def op_qk_norm_rope(q, k, q_gain, k_gain, pos, eps, base, q_out=None, k_out=None
     pos [n]; rows may be strided (column ranges of one projection).  q_out / k_out may be q / k."""
     w = "akvs_op_qk_norm_rope"
     dev, dt, qs, ks = _current(w, q.get_device()), q.dtype, q.shape, k.shape
+    if len(qs) != 3 or len(ks) != 3:
+        _refuse(w, -2)
     q_out = torch.empty_like(q, memory_format=_PACKED) if q_out is None else q_out
     k_out = torch.empty_like(k, memory_format=_PACKED) if k_out is None else k_out
     if not (dev == k.get_device() == q_gain.get_device() == k_gain.get_device() == pos.get_device() == q_out.get_device()
@@ -518,7 +520,7 @@ def op_qk_norm_rope(q, k, q_gain, k_gain, pos, eps, base, q_out=None, k_out=None
             and q_gain.dtype == k_gain.dtype == torch.float32):
         _refuse(w, -4)
     n, nq, hd = qs
-    if not (len(ks) == 3 and ks[0] == n and ks[2] == hd and q_out.shape == qs and k_out.shape == ks and pos.shape == (n,)
+    if not (ks[0] == n and ks[2] == hd and q_out.shape == qs and k_out.shape == ks and pos.shape == (n,)
             and q_gain.shape == k_gain.shape == (hd,) and q_gain.is_contiguous() and k_gain.is_contiguous()
             and pos.is_contiguous()):
         _refuse(w, -2)
@@ -543,6 +545,8 @@ def op_attention_shared(q, ctx_k, ctx_v, own_k, own_v, own_len, q_off=None, out=
     `lse` held (zeros where this call allocates them)."""
     w = "akvs_op_attention_shared"
     dev, dt, qs, cs, os_ = _current(w, q.get_device()), q.dtype, q.shape, ctx_k.shape, own_k.shape
+    if len(qs) != 3 or len(cs) != 3 or len(os_) != 4:
+        _refuse(w, -2)
     (R, nq, hd), (P, nkv, _), (S, cap, _, _) = qs, cs, os_
     if out is None or lse is None:
         fresh = torch.empty if q_off is None and R == S else torch.zeros
@@ -587,6 +591,8 @@ def op_attention_mass(q, k, lse, k_lo, k_hi, mass=None, out=None):
     `mass`."""
     w = "akvs_op_attention_mass"
     dev, dt, qs, ks = _current(w, q.get_device()), q.dtype, q.shape, k.shape
+    if len(qs) != 3 or len(ks) != 3:
+        _refuse(w, -2)
     (R, nq, hd), (T, nkv, _) = qs, ks
     if out is None:
         out = lse.new_empty((nkv, T)) if mass is None else torch.empty_like(mass, memory_format=_PACKED)
@@ -619,6 +625,8 @@ def op_evict(mass, k, v, budget, n_sink=0, n_recent=0):
     k_out, v_out [L][budget][n_kv][hd], mass_out [L][n_kv][budget]), tokens ascending."""
     w = "akvs_op_evict"
     dev, dt, ks, kst = _current(w, k.get_device()), k.dtype, k.shape, k.stride()
+    if len(ks) != 4:
+        _refuse(w, -2)
     L, T, nkv, hd = ks
     if not (dev == v.get_device() == mass.get_device()):
         _refuse(w)
