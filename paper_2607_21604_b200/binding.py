@@ -504,6 +504,13 @@ def _ld(where, shape, stride):
     return stride[0] if n > 1 else heads * hd
 
 
+def _alike(where, shape, x, y):
+    """Whether two tensors of this shape have the same strides where they mean something: K and V share
+    theirs."""
+    if any(a != b for n, a, b in zip(shape, x, y) if n > 1):
+        _refuse(where, -2)
+
+
 def op_qk_norm_rope(q, k, q_gain, k_gain, pos, eps, base, q_out=None, k_out=None):
     """RMSNorm of every head of q [n][n_q][hd] and k [n][n_kv][hd] (gains float [hd]), then RoPE at
     pos [n]; rows may be strided (column ranges of one projection).  q_out / k_out may be q / k."""
@@ -540,9 +547,9 @@ def op_attention_shared_scratch(dtype, R, P, S, cap, n_q, n_kv, hd, device="cuda
 
 def op_attention_shared(q, ctx_k, ctx_v, own_k, own_v, own_len, q_off=None, out=None, lse=None, scratch=None):
     """Attention of q [R][n_q][hd] over the shared context [P][n_kv][hd] and each sequence's own
-    tokens [S][cap][n_kv][hd], of which own_len [S] are filled.  q_off [S+1] gives the rows of each
-    sequence (None: one row each).  Returns (out, lse); rows of no sequence keep what `out` and
-    `lse` held (zeros where this call allocates them)."""
+    tokens [S][cap][n_kv][hd], of which own_len [S] are filled.  K and V of a pair have the
+    same strides.  q_off [S+1] gives the rows of each sequence (None: one row each).  Returns (out,
+    lse); rows of no sequence keep what `out` and `lse` held (zeros where this call allocates them)."""
     w = "akvs_op_attention_shared"
     dev, dt, qs, cs, os_ = _current(w, q.get_device()), q.dtype, q.shape, ctx_k.shape, own_k.shape
     if len(qs) != 3 or len(cs) != 3 or len(os_) != 4:
@@ -558,11 +565,15 @@ def op_attention_shared(q, ctx_k, ctx_v, own_k, own_v, own_len, q_off=None, out=
     if not (dt in _CODE and dt == ctx_k.dtype == ctx_v.dtype == own_k.dtype == own_v.dtype == out.dtype
             and lse.dtype == torch.float32 and own_len.dtype == torch.int32):
         _refuse(w, -4)
-    cst, ost = ctx_k.stride(), own_k.stride()
     if not (cs[2] == hd and ctx_v.shape == cs and os_[2:] == (nkv, hd) and own_v.shape == os_ and own_len.shape == (S,)
-            and ctx_v.stride() == cst and own_v.stride() == ost and out.shape == qs and lse.shape == (R, nq)
-            and out.is_contiguous() and lse.is_contiguous() and own_len.is_contiguous()):
+            and out.shape == qs and lse.shape == (R, nq) and out.is_contiguous() and lse.is_contiguous()
+            and own_len.is_contiguous()):
         _refuse(w, -2)
+    cst, ost, c2, o2 = ctx_k.stride(), own_k.stride(), ctx_v.stride(), own_v.stride()
+    if c2 != cst or o2 != ost:
+        _alike(w, cs, cst, c2)
+        _alike(w, os_, ost, o2)
+    o_ld = _ld(w, os_[1:], ost[1:])
     off = None
     if q_off is not None:
         if q_off.get_device() != dev:
@@ -578,10 +589,9 @@ def op_attention_shared(q, ctx_k, ctx_v, own_k, own_v, own_len, q_off=None, out=
     elif scratch.get_device() != dev or not scratch.is_contiguous():
         _refuse(w)
     _chk(lib.akvs_op_attention_shared(_CODE[dt], q.data_ptr(), _ld(w, qs, q.stride()), R, ctx_k.data_ptr(),
-                                      ctx_v.data_ptr(), _ld(w, cs, cst), P, own_k.data_ptr(), own_v.data_ptr(),
-                                      _ld(w, os_[1:], ost[1:]), ost[0], S, cap, own_len.data_ptr(), off, nq, nkv, hd,
-                                      out.data_ptr(), lse.data_ptr(), scratch.data_ptr(), scratch.nbytes,
-                                      _raw_stream(dev)), w)
+                                      ctx_v.data_ptr(), _ld(w, cs, cst), P, own_k.data_ptr(), own_v.data_ptr(), o_ld,
+                                      ost[0] if S > 1 else cap * o_ld, S, cap, own_len.data_ptr(), off, nq, nkv, hd, out.data_ptr(),
+                                      lse.data_ptr(), scratch.data_ptr(), scratch.nbytes, _raw_stream(dev)), w)
     return out, lse
 
 
@@ -620,9 +630,10 @@ def op_attention_mass(q, k, lse, k_lo, k_hi, mass=None, out=None):
 
 
 def op_evict(mass, k, v, budget, n_sink=0, n_recent=0):
-    """Keeps `budget` tokens per layer and kv head of k, v [L][T][n_kv][hd] by mass [L][n_kv][T]: the
-    first n_sink, the last n_recent and the heaviest others.  Returns (idx [L][n_kv][budget],
-    k_out, v_out [L][budget][n_kv][hd], mass_out [L][n_kv][budget]), tokens ascending."""
+    """Keeps `budget` tokens per layer and kv head of k, v [L][T][n_kv][hd] (the same strides for both) by
+    mass [L][n_kv][T]: the first n_sink, the last n_recent and the heaviest others.  Returns
+    (idx [L][n_kv][budget], k_out, v_out [L][budget][n_kv][hd], mass_out [L][n_kv][budget]), tokens
+    ascending."""
     w = "akvs_op_evict"
     dev, dt, ks, kst = _current(w, k.get_device()), k.dtype, k.shape, k.stride()
     if len(ks) != 4:
@@ -632,16 +643,18 @@ def op_evict(mass, k, v, budget, n_sink=0, n_recent=0):
         _refuse(w)
     if not (dt in _CODE and dt == v.dtype and mass.dtype == torch.float32):
         _refuse(w, -4)
-    if not (v.shape == ks and v.stride() == kst and mass.shape == (L, nkv, T) and mass.is_contiguous() and budget <= T):
+    if not (v.shape == ks and mass.shape == (L, nkv, T) and mass.is_contiguous() and budget <= T):
         _refuse(w, -2)
     if budget < 0:
         _refuse(w)
+    if v.stride() != kst:
+        _alike(w, ks, kst, v.stride())
+    tok_ld = _ld(w, ks[1:], kst[1:])
     mass_out = mass.new_empty((L, nkv, budget))
     idx = torch.empty_like(mass_out, dtype=torch.int32)
     k_out = k.new_empty((L, budget, nkv, hd))
     v_out = torch.empty_like(k_out)
-    tok_ld = _ld(w, ks[1:], kst[1:])
     _chk(lib.akvs_op_evict(_CODE[dt], mass.data_ptr(), k.data_ptr(), v.data_ptr(), kst[0] if L > 1 else T * tok_ld,
-                           tok_ld, L, T, nkv, hd, budget, n_sink, n_recent, idx.data_ptr(), k_out.data_ptr(),
-                           v_out.data_ptr(), mass_out.data_ptr(), _raw_stream(dev)), w)
+                           tok_ld, L, T, nkv, hd, budget, n_sink, n_recent, idx.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
+                           mass_out.data_ptr(), _raw_stream(dev)), w)
     return idx, k_out, v_out, mass_out
