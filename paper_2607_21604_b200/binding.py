@@ -480,8 +480,10 @@ def op_quantize(x, bits):
 
 _CODE = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 _PACKED = torch.contiguous_format
-_device = torch._C._cuda_getDevice                     # the current device, without the lookup of its properties
-_raw_stream = torch._C._cuda_getCurrentRawStream       # the current stream's handle, without a Stream object
+# The current device and the current stream's handle, by the short ways where this torch has them: without
+# the lookup of device properties and without a Stream object.
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
 def _refuse(where, code=-1):
