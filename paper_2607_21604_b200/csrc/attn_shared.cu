@@ -80,6 +80,15 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// Two values of a row of the output.  float16 saturates where rounded weights carry a mean of the largest V
+// past the type's end, but an infinity stays one (pack2 alone would make it the largest finite value).
+template <typename T> __device__ __forceinline__ uint32_t round2(float a, float b) { return pack2<T>(a, b); }
+template <> __device__ __forceinline__ uint32_t round2<f16>(float a, float b) {
+  auto end = [](float x) { return fabsf(x) > 65504.f && fabsf(x) < INFINITY ? copysignf(65504.f, x) : x; };
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(end(b)), "f"(end(a)));
+  return r;
+}
 template <typename T> __device__ __forceinline__ float2 unpack2(uint32_t w);
 template <> __device__ __forceinline__ float2 unpack2<bf16>(uint32_t w) {
   return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
@@ -722,7 +731,7 @@ join_kernel(const __grid_constant__ SharedParams p) {
         for (int i = 0; i < V; ++i) dst[i] = o[i] * inv;
       } else {
 #pragma unroll
-        for (int i = 0; i < V; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = pack2<T>(o[i] * inv, o[i + 1] * inv);
+        for (int i = 0; i < V; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = round2<T>(o[i] * inv, o[i + 1] * inv);
       }
       if (lane == 0) p.lse[at] = l == 0.f ? -INFINITY : (mx + log2f(l)) * LN2;
     }

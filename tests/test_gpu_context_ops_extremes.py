@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from test_gpu_context_ops import BF16, F16, F32, TINY, TYPES, gen, half, ints, mass_case, rnd
+from test_gpu_context_ops import BF16, F16, F32, TINY, TYPES, gen, half, ints, mass_case, rnd, shared_case
 
 pytestmark = pytest.mark.gpu
 
@@ -108,3 +108,29 @@ def test_attention_of_far_scores(akvs, dt, qv, kv):
     k, v = far_keys(n, nkv, hd, dt, kv), rnd(g, n, nkv, hd, dt=dt)
     lo, hi = ints([0] * 50), ints([n - 1] * 50)
     check_far(akvs.op_attention(q, k, v, lo, hi), weighty(v), dt)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("S", [1, 40])
+@pytest.mark.parametrize("where", ["context", "own"])
+def test_shared_infinite_values_show(akvs, dt, hd, S, where):
+    """An infinity in a V that a row sees gives infinity or NaN in its column, and leaves the others alone."""
+    c = shared_case(S + hd, dt, hd, 8, 2, 700, 40, [40] * S, [1] * S)
+    q, ck, cv, sk, sv, lens, off = c
+    clean = akvs.op_attention_shared(q, ck, cv, sk, sv, ints(lens))
+    for bad in (math.inf, -math.inf):
+        (cv[300] if where == "context" else sv[:, 7])[..., 5] = bad
+        out, lse = akvs.op_attention_shared(q, ck, cv, sk, sv, ints(lens))
+        assert not out[..., 5].isfinite().any()
+        out[..., 5] = clean[0][..., 5]
+        assert torch.equal(out, clean[0]) and torch.equal(lse, clean[1])
+
+
+@pytest.mark.parametrize("S", [1, 40])
+def test_shared_largest_float16_values_stay_finite(akvs, S):
+    """The mean of the type's largest value is that value, give or take a rounding of the weights."""
+    q, ck, cv, sk, sv, lens, _ = shared_case(S, F16, 128, 8, 2, 700, 40, [40] * S, [1] * S)
+    cv.fill_(65504), sv.fill_(65504)
+    out, _ = akvs.op_attention_shared(q, ck, cv, sk, sv, ints(lens))
+    assert out.isfinite().all() and (out >= 65504 * (1 - 2.0 ** -10)).all()
