@@ -354,7 +354,8 @@ int32_t akvs_op_qk_norm_rope(int32_t dtype, const void* q, int64_t q_ld, const v
  * see never reaches it, NaN and infinities included (an infinity in a V that it does see gives
  * infinity or NaN, of float16 too).  Scores are scaled by 1/sqrt(head_dim).
  * Products q . k, sums of weights and sums of weights times V are float: where one leaves that range (V
- * beyond 3e38 over the number of keys, say) the result is infinite or NaN.
+ * beyond 3e38 over the number of keys, say) the result is infinite or NaN.  float16 holds a weight to
+ * 2^-32 of its row's largest.
  *   out [R][n_q][hd], contiguous; lse float [R][n_q]: log of the row's sum of exponentials.
  * A row that sees nothing gives zeros and lse = -inf; rows of no sequence are left as they were.
  * Values of own_len outside [0, cap] and of q_off outside [0, R] are clamped, a range that runs

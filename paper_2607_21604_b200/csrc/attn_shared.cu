@@ -40,6 +40,10 @@ constexpr int ST = 3;                         // stages of a warp's ring, 16 key
 constexpr int MAX_OWN_SPLITS = 64;
 constexpr float NO_MAX = -FLT_MAX;            // running maximum before any key: below every finite score (in log2
                                               // units they are products with less than 0.2), and exp2(-inf - NO_MAX) = 0
+// How far below the largest score the reference of the exponentials is, in log2 units: float16 ends at
+// 2^-24, and with 2^7 for the largest weight all weights are held to 2^-32 of it (without, 30000 keys of
+// 2^-26 beside one of 1 lost a quarter of what they add to the output).
+template <typename T> constexpr float BELOW = std::is_same<T, f16>::value ? 7.f : 0.f;
 constexpr float LN2 = 0.69314718f, LOG2E = 1.4426950408889634f;
 
 struct SharedParams {
@@ -145,7 +149,7 @@ struct WarpTile {
   uint32_t qb[NT][KC][4];                     // row 8 x + gr, chunk 4 c + t
   int limit[NT][2];                           // rows 8 x + 2 t + e see the keys below these
   float o[NT][VC][4][4];                      // row 8 x + 2 t + e, column 64 c + 8 gr + 2 i + s at [x][c][i][2 s + e]
-  float mx[NT][2], sum[NT][2];
+  float mx[NT][2], sum[NT][2];                // reference of the exponentials (the largest score less BELOW), their sum
 
   template <typename Lim>
   __device__ __forceinline__ void begin(const SharedParams& p, const Tile& tl, int end, const Lim& lim) {
@@ -207,7 +211,7 @@ struct WarpTile {
         top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 4));
         top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
         top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
-        m_new[e] = fmaxf(mx[x][e], top);
+        m_new[e] = fmaxf(mx[x][e], top - BELOW<T>);
       }
       if (__any_sync(0xFFFFFFFFu, m_new[0] != mx[x][0] || m_new[1] != mx[x][1])) {
         const float f[2] = {ex2(mx[x][0] - m_new[0]), ex2(mx[x][1] - m_new[1])};

@@ -134,3 +134,39 @@ def test_shared_largest_float16_values_stay_finite(akvs, S):
     cv.fill_(65504), sv.fill_(65504)
     out, _ = akvs.op_attention_shared(q, ck, cv, sk, sv, ints(lens))
     assert out.isfinite().all() and (out >= 65504 * (1 - 2.0 ** -10)).all()
+
+
+LIGHT = -26                                                   # log2 of a light key's weight
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("hd,S,P,cap", [(64, 1000, 30000, 0), (128, 1000, 30000, 0), (128, 3, 30000, 0), (64, 200, 0, 4000), (128, 40, 20, 15000)])
+def test_shared_one_key_above_many_light_ones(akvs, dt, hd, S, P, cap):
+    """A key that draws nearly all weight and whose V is zero: what remains are the small weights of all
+    others.  float16 holds a weight to 2^-32 of the row's largest."""
+    nq, nkv = 16, 4
+    light = round(LIGHT * math.log(2) * math.sqrt(hd)) / 4    # exact in every type
+
+    def keys(n, first, heavy):
+        k, v = torch.zeros((n, nkv, hd), dtype=dt, device="cuda"), rnd(gen(n), n, nkv, hd, dt=dt).abs()
+        k[..., 0] = light
+        if heavy:
+            k[first], v[first] = 0, 0
+        return k, v
+
+    q = torch.zeros((S, nq, hd), dtype=dt, device="cuda")
+    q[..., 0] = 4
+    ck, cv = keys(P, 40, P > 20)
+    k1, v1 = keys(cap, 40, P <= 20)
+    sk, sv = (x[None].expand(S, cap, nkv, hd).contiguous() for x in (k1, v1))
+    out, lse = akvs.op_attention_shared(q, ck, cv, sk, sv, ints([cap] * S))
+    w = math.exp(4 * light / math.sqrt(hd))
+    total, v = 1 + (P + cap - 1) * w, torch.cat([cv, v1]).double()
+    ref = (v.sum(0) * w / total).repeat_interleave(nq // nkv, 0)
+    held = 2.0 ** -32 * v.abs().sum(0).repeat_interleave(nq // nkv, 0) if dt == F16 else 0.0
+    # scores of 18 are right to 2^-19; a weight may be rounded once to the 16-bit type; n additions to the
+    # row's sum and n to the output, each rounded by up to 2^-24 of the sum
+    n = P + cap
+    tol = half(dt) * ref + (2.0 ** -18 + 2 * n * 2.0 ** -24 + (0 if dt == F32 else half(dt))) * ref + held + TINY[dt]
+    assert ((out.double() - ref).abs() <= tol).all(), ((out.double() - ref).abs() / ref).max()
+    assert (lse.double() - math.log(total)).abs().max() <= n * 2.0 ** -24 + 2.0 ** -20
