@@ -338,6 +338,9 @@ int32_t akvs_op_quantize(int32_t dtype, const void* x, int32_t n, int32_t n_kv_h
  * [hd] and k [n][n_kv][hd] may be column ranges of one projection's output (q_ld, k_ld); gains
  * are float [head_dim]; all arithmetic is float, with one rounding at the end.  q_out / k_out
  * may be q / k with the same stride.  One of the head counts may be 0.
+ * For models that norm every query and key head, whose cached keys the caller has normed alike.  The
+ * model of akvs_model_desc has no such norm: over K that akvs_encode_units or akvs_prefill_corrected
+ * left, new rows take akvs_op_rope.
  * head_dim 32, 64, 128 or 256 (else AKVS_ERR_UNSUPPORTED); eps >= 0, rope_base > 0, finite. */
 int32_t akvs_op_qk_norm_rope(int32_t dtype, const void* q, int64_t q_ld, const void* k, int64_t k_ld,
                              const float* q_gain, const float* k_gain, const int32_t* pos, int32_t n,
