@@ -110,16 +110,17 @@ def attention(q, k, v, q_pos, k_pos, k_first=None, dtype=np.float64, row_block=1
     scale = dtype(1.0 / math.sqrt(hd))
     for r0 in range(0, R, row_block):
         r1 = min(R, r0 + row_block)
-        visible = (k_pos[None, :] <= q_pos[r0:r1, None]) & (k_pos[None, :] >= lo[r0:r1, None])
+        hidden = (k_pos[None, :] > q_pos[r0:r1, None]) | (k_pos[None, :] < lo[r0:r1, None])
 
         def one_head(hq):
             hk = hq // g
-            s = (q[r0:r1, hq, :] @ k[:, hk, :].T) * scale
-            s = np.where(visible, s, -np.inf)
-            s = s - np.max(s, axis=1, keepdims=True)
-            p = np.exp(s)
-            p = p / np.sum(p, axis=1, keepdims=True)
-            out[r0:r1, hq, :] = p @ v[:, hk, :]
+            s = q[r0:r1, hq, :] @ k[:, hk, :].T          # in place from here on: the score matrix is large
+            s *= scale
+            s[hidden] = -np.inf
+            s -= np.max(s, axis=1, keepdims=True)
+            np.exp(s, out=s)
+            s /= np.sum(s, axis=1, keepdims=True)
+            out[r0:r1, hq, :] = s @ v[:, hk, :]
 
         if ATTENTION_WORKERS > 1 and nq > 1:
             with ThreadPoolExecutor(ATTENTION_WORKERS) as ex:
