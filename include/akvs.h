@@ -336,8 +336,9 @@ int32_t akvs_op_quantize(int32_t dtype, const void* x, int32_t n, int32_t n_kv_h
  *   y = x * rsqrt(mean(x^2) + eps) * gain   over the head_dim values of a head,
  * then the rotate-half rotation of akvs_op_rope at pos[row] (any 32-bit position).  q [n][n_q]
  * [hd] and k [n][n_kv][hd] may be column ranges of one projection's output (q_ld, k_ld); gains
- * are float [head_dim]; all arithmetic is float, with one rounding at the end.  q_out / k_out
- * may be q / k with the same stride.  One of the head counts may be 0.
+ * are float [head_dim]; all arithmetic is float, with one rounding at the end (the mean of squares of
+ * values beyond 1.8e19 is infinite, and the head becomes zeros).  q_out / k_out may be q / k with the
+ * same stride.  One of the head counts may be 0.
  * For models that norm every query and key head, whose cached keys the caller has normed alike.  The
  * model of akvs_model_desc has no such norm: over K that akvs_encode_units or akvs_prefill_corrected
  * left, new rows take akvs_op_rope.
@@ -360,7 +361,8 @@ int32_t akvs_op_qk_norm_rope(int32_t dtype, const void* q, int64_t q_ld, const v
  * beyond 3e38 over the number of keys, say) the result is infinite or NaN.  float16 holds a weight to
  * 2^-32 of its row's largest.
  *   out [R][n_q][hd], contiguous; lse float [R][n_q]: log of the row's sum of exponentials.
- * A row that sees nothing gives zeros and lse = -inf; rows of no sequence are left as they were.
+ * A row that sees nothing, or only scores of -inf, gives zeros and lse = -inf; rows of no sequence
+ * are left as they were.
  * Values of own_len outside [0, cap] and of q_off outside [0, R] are clamped, a range that runs
  * backwards is empty; ranges must not overlap.  P = 0 or cap = 0 (then own_k, own_v and own_len
  * may be NULL) are allowed.  head_dim 64 or 128.
@@ -379,7 +381,8 @@ int32_t akvs_op_attention_shared(int32_t dtype, const void* q, int64_t q_ld, int
 /* Attention weight received by every key: mass_out[h][j] = mass_in[h][j] + the sum, over rows r
  * with k_lo[r] <= j <= k_hi[r] and the query heads i that read kv head h, of
  * exp(q_ri . k_jh / sqrt(head_dim) - lse[r][i]).  q [R][n_q][hd], k [T][n_kv][hd]; lse float
- * [R][n_q] as akvs_op_attention_shared gives it (a row with lse = -inf adds nothing); k_lo,
+ * [R][n_q] as akvs_op_attention_shared gives it (a row with lse = -inf adds nothing; a key with
+ * infinities has the weight that its scores of +-inf give); k_lo,
  * k_hi: device [R], in any order.  mass_in, mass_out: float [n_kv][T]; mass_in may be NULL
  * (zeros) or mass_out itself.  Sums run in a fixed order: equal calls give equal bits.
  * head_dim 64 or 128. */
@@ -391,7 +394,7 @@ int32_t akvs_op_attention_mass(int32_t dtype, const void* q, int64_t q_ld, const
 /* Shrinks a cache of T tokens to `budget` tokens per layer and kv head: the first n_sink and the
  * last n_recent tokens stay, then the heaviest of the others (ties to the smaller index; a NaN
  * mass is the lightest of all).  mass float [n_layers][n_kv][T]; k, v [n_layers][T][n_kv][hd]
- * (tokens tok_ld, layers layer_ld elements apart).  Outputs, contiguous, in ascending token
+ * (tokens tok_ld, layers layer_ld >= (T - 1) tok_ld + n_kv hd elements apart).  Outputs, contiguous, in ascending token
  * order: idx int32 [n_layers][n_kv][budget] (the token each slot came from), k_out, v_out
  * [n_layers][budget][n_kv][hd], mass_out [n_layers][n_kv][budget].  K keeps the rotation of its
  * old position, so the result is a context for akvs_op_attention_shared as it stands.

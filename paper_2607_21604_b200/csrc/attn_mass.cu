@@ -12,9 +12,9 @@
 // A CTA keeps 256 keys while the rows' Q tiles stream past them (each is used twice), then goes on to
 // its next 256 keys.  Two warps work out what each column sees; a tile whose columns all see its
 // keys runs without a mask.  With many rows the exponentials bound it (16 per clock and SM), with few
-// rows reading K once (16 rows x 32 heads over 12416 keys: 7.6 us, 3.5 TB/s).  Few keys and many rows: a
-// cluster shares the row tiles of its keys and adds the partial sums through distributed shared
-// memory.
+// rows reading K once (16 rows x 32 heads over 12416 keys: 9.4 us, 2.8 TB/s; 7.4 us with K in L2).  Few
+// keys and many rows: a cluster shares the row tiles of its keys and adds the partial sums through
+// distributed shared memory.
 #include "tc_common.cuh"
 #include <math.h>
 
@@ -110,8 +110,7 @@ struct ColumnLoad {                  // NW: key tiles of an item
 // different columns overlap.  Columns behind the last row hold a row of zeros and a z of -inf: exp2(0 - inf)
 // = 0 without a mask, unless the key holds an infinity or a NaN, with which 0 gives NaN.  Such columns end
 // a tile, so the last column shows it, and its NaN turns the mask on (for a real column, too: it changes
-// no result).  One compare and vote per 64 columns; the window of 512 rows x 40 heads over 32768 keys
-// takes as long as without.
+// no result).  One compare and vote per 64 columns: 512 rows x 40 heads over 32768 keys 238.8 -> 239.6 us.
 template <int N>
 __device__ __forceinline__ void add_columns(const float (&t)[N], const float* z, const int2* ranges, bool mask, int key,
                                             float scale2, float2 (&acc)[4]) {
@@ -334,7 +333,7 @@ mass_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__
 // -- many rows: tiles of up to 256 columns stream past the K of 256 keys.  The width halves what an MMA
 // reads of its A operand per column and spreads a tile's barriers over more work; one buffer of S^T per
 // group is all that fits then, and a group's next product waits until its last columns are taken.
-// 512 rows x 40 heads x 32768 keys: 229 to 238 us, of which the exponentials are 160 us (16 per clock and
+// 512 rows x 40 heads x 32768 keys: 220 to 240 us, of which the exponentials are 160 us (16 per clock and
 // SM).  Built and measured instead of it: 128 columns with two buffers 238 us (against 229); an issuing
 // thread per group (and a warp less for the columns) 237 us; K in tensor memory as the A operand with
 // tiles of 96 columns, two groups of two buffers 276 us, three groups of one buffer 253 us; exp2 of an

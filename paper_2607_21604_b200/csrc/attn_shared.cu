@@ -25,9 +25,9 @@
 // keys a stage, two stages in flight).  The contraction index of S^T and the columns of O^T may be
 // permuted at will, so fragments are plain 16-byte loads: a lane's chunk of K and of Q supplies four
 // of its k positions, and its chunks of four V rows, paired by byte permutes, eight columns.
-// Probabilities enter P V as a 16-bit value and the 16-bit rounding of what it lost: with one 16-bit
-// value alone the rounding of P would cost the output as much accuracy as its own final rounding.
-// Scores, maxima, sums and O are float.
+// In these tiles probabilities enter P V as a 16-bit value and the 16-bit rounding of what it lost: with
+// one 16-bit value alone, as in the tcgen05 kernel (which explains it), the rounding of P costs the output
+// as much accuracy as its own final rounding.  Scores, maxima, sums and O are float.
 #include "tc_common.cuh"
 #include <float.h>
 #include <math.h>
@@ -756,7 +756,8 @@ Plan make_plan(bool is16, int R, int P, int S, int cap, int g, int n_kv, int hd,
     // fill what the last round of the others leaves idle.  The mean of that end and of the work per SM
     // counts, since CTAs do not run in step and own tokens use idle SMs, plus writing and reading the
     // parts at memory speed (58 row blocks x 2 heads over 128 tiles: 108 + 20 tiles 137 us, 64 + 64 146 us;
-    // one row block x 8 heads over 97 tiles: 11 splits 19.5 us, 17 splits 22.6 us).
+    // one row block x 8 heads over 97 tiles: 11 splits 19.5 us, 17 splits 22.6 us; figures
+    // with K and V in L2, before the branch for far scores added 1 to 2 %).
     const int64_t base = (int64_t)akvs_cdiv(R, 128 / g) * n_kv;
     const int tiles = akvs_cdiv(P, 128);
     const double part = 2.0 * R * g * n_kv * (hd + 2) * 4 / 6.4e6 / 0.85;

@@ -3,7 +3,7 @@
 //     out[i]        = y[i] cos(a_i) - y[i + hd/2] sin(a_i)
 //     out[i + hd/2] = y[i + hd/2] cos(a_i) + y[i] sin(a_i),    a_i = pos * base^(-2i/hd)
 // Memory bound: every value is read once and written once (7 flops each), q and k in one launch
-// (11648 rows x 48 heads of 128, 16 bits: 53 us, 5.4 TB/s; one row 2.2 us).
+// (11648 rows x 48 heads of 128, 16 bits: 52 us, 5.5 TB/s; one row 2.1 us).
 // A head is shared by LPH lanes; a lane holds one 16-byte chunk of the lower half and the partner
 // chunk of the upper half, so the rotation needs no exchange and the sum of squares log2(LPH)
 // shuffles.  A warp keeps its row's cosines and sines in registers and walks the heads of the
