@@ -832,9 +832,13 @@ int64_t part_rows_bound(bool is16, int R, int P, int cap, int g, int n_kv) {
   // tcgen05: at most 3 * 148 CTAs or one split, base >= r * n_q / 128
   if (is16 && (int64_t)R * g > MT)
     ctx = most(ctx, least(least(akvs_cdiv(P, 128), most(1, 3 * 148 / n_kv)) * R * n_q, most((int64_t)R * n_q, 3 * 148 * 128)));
+  // Own tokens: `own` splits of S sequences of r rows have S * n_kv * z * own <= 296, or are one split.  One row
+  // each: r = S, g <= MT * z.  Ragged 16 bits: r * g <= MT * S, or one split (wide).  Ragged float: z >= r * g / (8 S),
+  // or z = 64, where 4 splits of one kv head or 2 of two are the most.
   int own = cap > 0;
   while (own > 0 && own < MAX_OWN_SPLITS && (int64_t)n_kv * own * 2 <= 296 && cap / (own * 2) >= 128) own *= 2;
-  return ctx + own * (int64_t)R * n_q;
+  const int64_t all = (int64_t)R * n_q, deep = is16 || n_kv > 2 ? 1 : 4 / n_kv;
+  return ctx + least(own * all, most(deep * all, 296 * MT));
 }
 
 template <typename T, int HD, int NT, bool WIDE>
@@ -924,8 +928,9 @@ extern "C" int32_t akvs_op_attention_shared(int32_t dtype, const void* q, int64_
       (cap > 0 && (!aligned16(own_k) || !aligned16(own_v) || own_ld * es % 16 || own_seq_ld * es % 16)))
     return AKVS_ERR_INVALID_ARG;
   if ((int64_t)R * n_q_heads > 0x7fffffff || (int64_t)S * MAX_OWN_SPLITS > 0x7fffffff) return AKVS_ERR_TOO_LARGE;
-  const Plan pl = make_plan(dtype != AKVS_F32, R, P, S, cap, n_q_heads / n_kv_heads, n_kv_heads, head_dim, q_off != nullptr);
-  const int64_t rows = part_rows(pl, R, n_q_heads), need = parts_bytes(rows, head_dim);
+  const int32_t used = q_off ? R : S;             // rows behind the last sequence's get no parts
+  const Plan pl = make_plan(dtype != AKVS_F32, used, P, S, cap, n_q_heads / n_kv_heads, n_kv_heads, head_dim, q_off != nullptr);
+  const int64_t rows = part_rows(pl, used, n_q_heads), need = parts_bytes(rows, head_dim);
   if (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255) || scratch_size < need) return AKVS_ERR_WORKSPACE;
   const int64_t ctx_n = P > 0 ? ((P - 1) * ctx_ld + row) * es : 0;
   const int64_t own_n = cap > 0 ? ((S - 1) * own_seq_ld + (cap - 1) * own_ld + row) * es : 0;
@@ -940,7 +945,7 @@ extern "C" int32_t akvs_op_attention_shared(int32_t dtype, const void* q, int64_
       if (bytes_overlap(outs[i], out_n[i], outs[o], out_n[o])) return AKVS_ERR_INVALID_ARG;
   }
   SharedParams p;
-  p.q = q; p.q_ld = q_ld; p.R = R; p.n_q = n_q_heads; p.n_kv = n_kv_heads; p.g = n_q_heads / n_kv_heads;
+  p.q = q; p.q_ld = q_ld; p.R = used; p.n_q = n_q_heads; p.n_kv = n_kv_heads; p.g = n_q_heads / n_kv_heads;
   p.pk = ctx_k; p.pv = ctx_v; p.P = P; p.p_ld = ctx_ld;
   p.sk = own_k; p.sv = own_v; p.S = S; p.cap = cap; p.s_ld = own_ld; p.s_seq = own_seq_ld; p.s_len = own_len; p.q_off = q_off;
   p.out = out; p.lse = lse;

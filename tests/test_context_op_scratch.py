@@ -38,7 +38,7 @@ def test_scratch_grows_with_every_size(b):  # noqa: F811
     def log(hi):
         return int(round(2 ** rng.uniform(0, hi))) - 1
 
-    for _ in range(4000):
+    for _ in range(12000):
         nkv = rng.choice((1, 2, 3, 8, 40))
         c = dict(dtype=rng.choice((0, 1, 2)), R=1 + log(9), S=log(9), P=log(17), cap=log(13), nkv=nkv,
                  nq=nkv * rng.choice((1, 2, 4, 5, 8, 16, 17, 100, 128)), hd=rng.choice((64, 128)))
@@ -48,6 +48,14 @@ def test_scratch_grows_with_every_size(b):  # noqa: F811
         for ragged in (False, True):
             if small["S"] > 0 and (ragged or small["R"] >= small["S"]):
                 assert enough(b, small, have, ragged), (small, c, ragged)
+
+
+@pytest.mark.parametrize("dtype,nkv", [(0, 8), (1, 8), (2, 1), (0, 1)])
+def test_scratch_of_many_rows_is_in_proportion(b, dtype, nkv):  # noqa: F811
+    """Many rows need few splits: two parts of each row, or up to five of a single float head."""
+    c = dict(dtype=dtype, R=8192, S=1, P=32768, cap=8192, nkv=nkv, nq=4 * nkv, hd=128)
+    parts = 5 if dtype == 0 and nkv == 1 else 2
+    assert size(b, c) <= parts * 1.05 * 8192 * 4 * nkv * 130 * 4 + 40e6
 
 
 def test_scratch_of_calls_that_are_too_large(b):  # noqa: F811

@@ -98,3 +98,19 @@ def test_shared_error_on_the_whole(akvs, dt, hd, S):
     err, rounding = rms(out.double() - ref), rms(ref.to(dt).double() - ref)
     bound = 2.0 ** -18 * rms(ref) if dt == F32 else (1.05 if 4 * S <= 16 else 1.5) * rounding
     assert err <= bound, (err, bound, math.log2(err / rms(ref)))
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("S,behind", [(1, 1), (2, 40), (50, 10), (50, 300)])
+def test_shared_rows_behind_the_last_sequence(akvs, dt, S, behind):
+    """One row each and rows that belong to no sequence, NaN here: those stay as they were, and the others
+    are what they are without them, to the bit."""
+    lens = [(7 * s) % 30 + 1 for s in range(S)]
+    q, ck, cv, sk, sv, _, _ = shared_case(S, dt, 128, 8, 2, 2000, 600, lens, [1] * S)
+    more = torch.cat([q, torch.full((behind, 8, 128), math.nan, device="cuda", dtype=dt)])
+    out, lse = torch.full_like(more, 9.0), torch.full(more.shape[:2], 9.0, device="cuda")
+    scratch = akvs.op_attention_shared_scratch(dt, S + behind + 5, 2500, S + 2, 700, 8, 2, 128)       # of a larger call
+    akvs.op_attention_shared(more, ck, cv, sk, sv, ints(lens), None, out, lse, scratch)
+    want = akvs.op_attention_shared(q, ck, cv, sk, sv, ints(lens))
+    assert torch.equal(out[:S], want[0]) and torch.equal(lse[:S], want[1])
+    assert (out[S:] == 9).all() and (lse[S:] == 9).all()
