@@ -382,8 +382,8 @@ int32_t akvs_op_attention_shared(int32_t dtype, const void* q, int64_t q_ld, int
  * with k_lo[r] <= j <= k_hi[r] and the query heads i that read kv head h, of
  * exp(q_ri . k_jh / sqrt(head_dim) - lse[r][i]).  q [R][n_q][hd], k [T][n_kv][hd]; lse float
  * [R][n_q] as akvs_op_attention_shared gives it (a row with lse = -inf adds nothing; a key with
- * infinities has the weight that its scores of +-inf give); k_lo,
- * k_hi: device [R], in any order.  mass_in, mass_out: float [n_kv][T]; mass_in may be NULL
+ * infinities has the weight that its scores of +-inf give; score and lse are float, so a weight may be
+ * off by 2^-22 |score| of itself); k_lo, k_hi: device [R], in any order.  mass_in, mass_out: float [n_kv][T]; mass_in may be NULL
  * (zeros) or mass_out itself.  Sums run in a fixed order: equal calls give equal bits.
  * head_dim 64 or 128. */
 int32_t akvs_op_attention_mass(int32_t dtype, const void* q, int64_t q_ld, const void* k, int64_t k_ld,

@@ -114,3 +114,12 @@ def test_shared_rows_behind_the_last_sequence(akvs, dt, S, behind):
     want = akvs.op_attention_shared(q, ck, cv, sk, sv, ints(lens))
     assert torch.equal(out[:S], want[0]) and torch.equal(lse[:S], want[1])
     assert (out[S:] == 9).all() and (lse[S:] == 9).all()
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("rows,cap", [([16], 2500), ([30, 2], 1300), ([64], 900), ([1, 1, 70, 1, 1, 1], 400)])
+def test_shared_many_new_rows_over_long_slots(akvs, dt, rows, cap):
+    """Few sequences of many rows each over many own tokens, or one such among single rows."""
+    lens = [cap - 3 * s for s in range(len(rows))]
+    c = shared_case(cap, dt, 128, 8, 2, 40, cap, lens, rows)
+    check_shared(akvs.op_attention_shared(*c[:5], ints(lens), ints(c[6])), *c)
