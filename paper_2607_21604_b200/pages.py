@@ -34,7 +34,8 @@ class PagePool:
 
     def grow(self, seqs, n=1):
         """Room for n more tokens (a number, or one per sequence) in each of `seqs`, which become part of their
-        lengths.  A last page that others hold too is copied first.  Raises, and changes nothing, where pages run out."""
+        lengths.  A last page that others hold too is copied first.  Raises, and changes nothing, where pages run out or a
+        copy is refused."""
         seqs = list(seqs)
         ns = [n] * len(seqs) if isinstance(n, int) else list(n)
         if len(ns) != len(seqs) or len(set(seqs)) != len(seqs) or any(x < 0 for x in ns):
@@ -46,19 +47,28 @@ class PagePool:
             if shared:
                 left[have[-1]] -= 1                   # the last of those that branch keeps the page
             plan.append((s, x, shared, -(-(length + x) // PAGE_TOKENS) - len(have)))
-        if sum(more + shared for _, _, shared, more in plan) > len(self.free):
+        need = sum(more + shared for _, _, shared, more in plan)
+        if need > len(self.free):
             raise AkvsError(-8, "PagePool.grow")
-        src, dst = [], []
+        # The copies first: where one is refused, the account is as it was.
+        taken, src, dst = self.free[len(self.free) - need:], [], []       # the last is taken first
+        pages = {}
         for s, x, shared, more in plan:
+            pages[s] = list(self.pages[s])
             if shared:
-                old, new = self.pages[s][-1], self._take()
-                self.users[old] -= 1
-                self.pages[s][-1] = new
-                src.append(old)
-                dst.append(new)
-            self.pages[s] += [self._take() for _ in range(more)]
-            self.length[s] += x
+                src.append(pages[s][-1])
+                pages[s][-1] = taken.pop()
+                dst.append(pages[s][-1])
+            pages[s] += [taken.pop() for _ in range(more)]
         self._copy(src, dst)
+        del self.free[len(self.free) - need:]
+        for s, x, shared, more in plan:
+            for page in pages[s][len(pages[s]) - more - shared:]:
+                self.users[page] = 1
+            self.pages[s] = pages[s]
+            self.length[s] += x
+        for page in src:
+            self.users[page] -= 1
 
     def fork(self, seq, n=1):
         """n sequences that go on from where `seq` is; all of them share what it holds."""
@@ -107,11 +117,6 @@ class PagePool:
         table = torch.tensor(rows, dtype=torch.int32).reshape(len(seqs), width)
         lens = torch.tensor([self.length[s] for s in seqs], dtype=torch.int32)
         return table.to(self.pool.device), lens.to(self.pool.device)
-
-    def _take(self):
-        page = self.free.pop()
-        self.users[page] = 1
-        return page
 
     def _drop(self, pages):
         for page in pages:

@@ -244,3 +244,36 @@ def test_pool_any_history(pool, b):  # noqa: F811
         _check(pool)
         for s, pages in want.items():
             assert pool.pool[0, pool.pages[s], 0].tolist() == pool.pool[1, pool.pages[s], 5].tolist() == pages
+
+
+def _state(p):
+    return {s: list(x) for s, x in p.pages.items()}, dict(p.length), list(p.users), list(p.free)
+
+
+def test_pool_keeps_its_account_when_a_copy_is_refused(pool, b, monkeypatch):  # noqa: F811
+    """A call whose copy is refused changes nothing and can be repeated."""
+    import paper_2607_21604_b200.pages as pages
+    a, gap = pool.open(), pool.open()
+    pool.grow([a], 70)
+    pool.grow([gap], 130)
+    pool.pool[:, 1] = 7
+    (x,) = pool.fork(a)
+    state, copy = _state(pool), pages.binding.op_pages_copy
+
+    def refuse(*_):
+        raise b.AkvsError(-1, "akvs_op_pages_copy")
+    monkeypatch.setattr(pages.binding, "op_pages_copy", refuse)
+    with pytest.raises(b.AkvsError):
+        pool.grow([a, x], [100, 1])
+    assert _state(pool) == state
+    monkeypatch.setattr(pages.binding, "op_pages_copy", copy)
+    pool.grow([a, x], [100, 1])
+    assert (pool.length[a], pool.length[x]) == (170, 71)
+    assert pool.pages[a][1] != pool.pages[x][1] and (pool.pool[:, [pool.pages[s][1] for s in (a, x)]] == 7).all()
+    _check(pool)
+    pool.close(gap)                                   # pages 2 to 4: those behind them would move
+    state = _state(pool)
+    monkeypatch.setattr(pages.binding, "op_pages_copy", refuse)
+    with pytest.raises(b.AkvsError):
+        pool.compact()
+    assert _state(pool) == state
