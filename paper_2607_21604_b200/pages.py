@@ -72,11 +72,11 @@ class PagePool:
 
     def fork(self, seq, n=1):
         """n sequences that go on from where `seq` is; all of them share what it holds."""
-        new = []
+        new, pages, length = [], self.pages[seq], self.length[seq]
         for _ in range(n):
             s = self.open()
-            self.pages[s], self.length[s] = list(self.pages[seq]), self.length[seq]
-            for page in self.pages[s]:
+            self.pages[s], self.length[s] = list(pages), length
+            for page in pages:
                 self.users[page] += 1
             new.append(s)
         return new

@@ -277,3 +277,13 @@ def test_pool_keeps_its_account_when_a_copy_is_refused(pool, b, monkeypatch):  #
     with pytest.raises(b.AkvsError):
         pool.compact()
     assert _state(pool) == state
+
+
+def test_pool_fork_of_no_sequence(pool):
+    """Nothing is opened for a sequence that there is not."""
+    a = pool.open()
+    pool.grow([a], 5)
+    state = _state(pool)
+    with pytest.raises(KeyError):
+        pool.fork(a + 1, 2)
+    assert _state(pool) == state
