@@ -453,7 +453,8 @@ typedef struct akvs_rope_desc {
 
 /* q [n][n_q][hd], k [n][n_kv][hd] (row strides q_ld, k_ld: column ranges of one projection will do) at pos[row], any
  * 32-bit position.  q_out / k_out may be q / k with the same stride.  One of the head counts may be 0.  All
- * arithmetic on values is float with one rounding at the end.  Keys in a cache and new queries have to be turned
+ * arithmetic on values is float with one rounding at the end; a finite float16 result beyond the type's end saturates, an
+ * infinity stays one (or NaN, as the formula gives).  Keys in a cache and new queries have to be turned
  * alike: over K of akvs_encode_units or akvs_prefill_corrected that is layout HALF, rot_dim = head_dim, PLAIN.
  * head_dim a multiple of 8 up to 256 (else AKVS_ERR_UNSUPPORTED); rot_dim even, 2 .. head_dim, 4 and more for NTK (else
  * AKVS_ERR_SHAPE); base, factor, orig_ctx, high positive and finite, 0 <= low < high, for YARN base > 1 and low > 0 (else

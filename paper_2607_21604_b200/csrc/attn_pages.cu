@@ -97,17 +97,6 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) { return __fmul2_rn(a
 __device__ __forceinline__ float part2(float2 a, int e) { return e ? a.y : a.x; }
 __device__ __forceinline__ float2 half2f(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
 __device__ __forceinline__ float2 bf2f(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
-// Two values of a row of the output; float16 saturates but keeps an infinity.
-template <typename T> __device__ __forceinline__ uint32_t round2(float a, float b) {
-  if constexpr (std::is_same<T, f16>::value) {
-    auto end = [](float x) { return fabsf(x) > 65504.f && fabsf(x) < INFINITY ? copysignf(65504.f, x) : x; };
-    uint32_t r;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(end(b)), "f"(end(a)));
-    return r;
-  } else {
-    return pack2<T>(a, b);
-  }
-}
 
 template <int TR> __host__ __device__ __forceinline__ int tiles_of(int n, int g) { return (n * g + TR - 1) / TR; }
 
@@ -743,7 +732,7 @@ pages_join_kernel(const __grid_constant__ PagesParams p) {
       for (int i = 0; i < V; ++i) dst[i] = o[i] * inv;
     } else {
 #pragma unroll
-      for (int i = 0; i < V; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = round2<T>(o[i] * inv, o[i + 1] * inv);
+      for (int i = 0; i < V; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = pack2_inf<T>(o[i] * inv, o[i + 1] * inv);
     }
     if (lane == 0) p.lse[row] = l == 0.f ? -INFINITY : (mx + log2f(l)) * LN2;
   }

@@ -151,6 +151,14 @@ __device__ __forceinline__ void st16(f16* p, const float (&o)[8]) {
   *reinterpret_cast<uint4*>(p) = v;
 }
 
+// Where infinities of the inputs have to reach the output: finite values saturate, an infinity stays one.
+__device__ __forceinline__ float f16_end(float x) { return fabsf(x) > 65504.f && fabsf(x) < INFINITY ? copysignf(65504.f, x) : x; }
+__device__ __forceinline__ uint32_t pack_f16x2_inf(float a, float b) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(f16_end(b)), "f"(f16_end(a)));
+  return r;
+}
+
 template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b);
 template <> __device__ __forceinline__ uint32_t pack2<bf16>(float a, float b) { return pack_bf16x2(a, b); }
 template <> __device__ __forceinline__ uint32_t pack2<f16>(float a, float b) { return pack_f16x2(a, b); }
@@ -164,6 +172,23 @@ template <> __device__ __forceinline__ bf16 from_f<bf16>(float x) { return __flo
 template <> __device__ __forceinline__ f16 from_f<f16>(float x) {
   const uint32_t r = pack_f16x2(x, 0.f);
   return __ushort_as_half((unsigned short)(r & 0xFFFFu));
+}
+
+// The same three, but a float16 infinity stays one.
+template <typename T> __device__ __forceinline__ uint32_t pack2_inf(float a, float b) {
+  if constexpr (std::is_same<T, f16>::value) return pack_f16x2_inf(a, b);
+  else return pack2<T>(a, b);
+}
+template <typename T> __device__ __forceinline__ T from_f_inf(float x) {
+  if constexpr (std::is_same<T, f16>::value) return __float2half_rn(f16_end(x));
+  else return from_f<T>(x);
+}
+template <typename T> __device__ __forceinline__ void st16_inf(T* p, const float (&o)[VecOf<T>::N]) {
+  if constexpr (std::is_same<T, f16>::value)
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack_f16x2_inf(o[0], o[1]), pack_f16x2_inf(o[2], o[3]), pack_f16x2_inf(o[4], o[5]),
+                                              pack_f16x2_inf(o[6], o[7]));
+  else
+    st16(p, o);
 }
 
 __device__ __forceinline__ float warp_sum(float v) {

@@ -74,14 +74,6 @@ __device__ __noinline__ void drain(uint64_t* bar, uint32_t parity) {
   volatile int never = 0;
   tc::mbar_wait(bar, parity, &never);
 }
-// One value of the output: float16 saturates but keeps an infinity.
-template <typename T> __device__ __forceinline__ T round1(float x) {
-  if constexpr (std::is_same<T, f16>::value) {
-    return __float2half_rn(fabsf(x) > 65504.f && fabsf(x) < INFINITY ? copysignf(65504.f, x) : x);
-  } else {
-    return from_f<T>(x);
-  }
-}
 
 // Shared memory of a CTA: two stages of weights ([pair][8 blocks], 8 groups), two of x.
 template <int NT, int PIECES> struct LqSmem {
@@ -307,7 +299,7 @@ linear_q4_kernel(const __grid_constant__ LinearQ4Params p) {
     for (int k = 0; k < splits; ++k) s += *cluster.map_shared_rank(red + r * LD + f, k);
     const int64_t at = (int64_t)row * p.N + n;
     if (p.h_out) p.h_out[at] = p.h[at] + s;
-    else reinterpret_cast<T*>(p.y)[at] = round1<T>(s);
+    else reinterpret_cast<T*>(p.y)[at] = from_f_inf<T>(s);
   }
   cluster.sync();                                     // nobody leaves while others read
 }
@@ -554,7 +546,7 @@ linear_q4_few_kernel(const __grid_constant__ LinearQ4Params p) {
       if (part != 0 || n >= p.N) continue;
       const int64_t at = (int64_t)r * p.N + n;
       if (p.h_out) p.h_out[at] = p.h[at] + s;
-      else reinterpret_cast<T*>(p.y)[at] = round1<T>(s);
+      else reinterpret_cast<T*>(p.y)[at] = from_f_inf<T>(s);
     }
   }
 }
@@ -1042,14 +1034,14 @@ linear_q4_tc_kernel(const __grid_constant__ TcParams p) {
       const float4 h = *reinterpret_cast<const float4*>(p.h + at);
       *reinterpret_cast<float4*>(p.h_out + at) = make_float4(h.x + s[0], h.y + s[1], h.z + s[2], h.w + s[3]);
     } else if (p.fours) {
-      alignas(8) T y[4] = {round1<T>(s[0]), round1<T>(s[1]), round1<T>(s[2]), round1<T>(s[3])};
+      alignas(8) T y[4] = {from_f_inf<T>(s[0]), from_f_inf<T>(s[1]), from_f_inf<T>(s[2]), from_f_inf<T>(s[3])};
       *reinterpret_cast<uint2*>(reinterpret_cast<T*>(p.y) + at) = *reinterpret_cast<const uint2*>(y);
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if (n + e >= p.N) break;
         if (p.h_out) p.h_out[at + e] = p.h[at + e] + s[e];
-        else reinterpret_cast<T*>(p.y)[at + e] = round1<T>(s[e]);
+        else reinterpret_cast<T*>(p.y)[at + e] = from_f_inf<T>(s[e]);
       }
     }
   };

@@ -110,7 +110,7 @@ rope_scaled_kernel(const __grid_constant__ RopeParams p) {
         o[2 * i] = a[2 * i] * cs[i] - a[2 * i + 1] * sn[i];
         o[2 * i + 1] = a[2 * i + 1] * cs[i] + a[2 * i] * sn[i];
       }
-      st16(y, o);
+      st16_inf(y, o);
     } else {
       float a[V], b[V], oa[V], ob[V];
       unpack16<T>(a4, a);
@@ -120,8 +120,8 @@ rope_scaled_kernel(const __grid_constant__ RopeParams p) {
         oa[i] = a[i] * cs[i] - b[i] * sn[i];
         ob[i] = b[i] * cs[i] + a[i] * sn[i];
       }
-      st16(y, oa);
-      st16(y + half, ob);
+      st16_inf(y, oa);
+      st16_inf(y + half, ob);
     }
   }
 }
@@ -157,8 +157,8 @@ rope_scaled_values_kernel(const __grid_constant__ RopeParams p) {
       if (i >= half) break;
       const int ia = INTER ? 2 * i : i, ib = INTER ? 2 * i + 1 : i + half;
       const float a = to_f(x[ia]), b = to_f(x[ib]);
-      y[ia] = from_f<T>(a * cs[k] - b * sn[k]);
-      y[ib] = from_f<T>(b * cs[k] + a * sn[k]);
+      y[ia] = from_f_inf<T>(a * cs[k] - b * sn[k]);
+      y[ib] = from_f_inf<T>(b * cs[k] + a * sn[k]);
     }
     for (int i = p.rot + lane; i < p.hd; i += 32) y[i] = x[i];
   }

@@ -732,3 +732,29 @@ def test_append_codes_at_their_edges(akvs, dt):
     at = at + torch.arange(8, device="cuda")[:, None, None] * 32 + torch.arange(2, device="cuda")[:, None] * 4 + torch.arange(2, device="cuda")
     v = blocks[(tok // 64)[:, None], at.reshape(2 * n, 32)]
     assert torch.equal(v, codes.reshape(2 * n, 32))
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("hd,rot", [(128, 128), (128, 64), (128, 20), (72, 70)])
+def test_rope_scaled_infinities(akvs, dt, layout, hd, rot):
+    """An infinity reaches both values of its pair and no other; a finite float16 beyond the type's end saturates."""
+    g = gen(hd + rot)
+    x, rope = rnd(g, 5, 3, hd, dt=dt), akvs.Rope(1e4, rot, layout=layout)
+    pos = ints([3, 100, 2001, 7, 1])
+    i, j = (5, 5 + rot // 2) if layout == "half" else (4, 5)
+    x[0, 1, i], x[1, 2, j], x[2, 0, i] = math.inf, -math.inf, math.nan
+    if dt == F16:
+        x[3, 0, i] = x[3, 0, j] = 65504.0
+        x[4, 1, i] = 65504.0
+    got, _ = akvs.op_rope_scaled(x, x[:, :0], pos, rope)
+    ref, both = rope_ref(x, pos, rope)
+    assert int(ref.isinf().sum()) == 4 and int(ref.isnan().sum()) == 2       # (no cosine or sine here is near zero)
+    if dt == F16:
+        assert int((ref[3:].abs() > 65504).sum()) >= 1
+        ref = torch.where(ref.isfinite(), ref.clamp(-65504, 65504), ref)
+    assert torch.equal(got.isnan(), ref.isnan()) and torch.equal(got.isinf(), ref.isinf())
+    assert torch.equal(got[got.isinf()].double(), ref[ref.isinf()])
+    fine = ref.isfinite()
+    tol = half(dt) * ref.abs() + 2.0 ** -20 * both + TINY[dt]
+    assert ((got.double() - ref).abs()[fine] <= tol[fine]).all()
