@@ -477,7 +477,8 @@ int32_t akvs_op_pages_append(int32_t dtype, const void* k, int64_t k_ld, const v
                              int64_t page_ld, int32_t n_pages, void* stream);
 
 /* The values that stand in the pages, code * scale + minimum rounded once to dtype, for the same rows: k_out, v_out
- * [R][n_kv][hd], contiguous.  With rows for all tokens of a sequence this is a context for
+ * [R][n_kv][hd], contiguous.  A finite value beyond float16's end saturates, an infinity (a group whose minimum lies
+ * beyond it) stays one.  With rows for all tokens of a sequence this is a context for
  * akvs_op_attention_shared.  Rows that akvs_op_pages_append would ignore or drop are left as they were. */
 int32_t akvs_op_pages_read(int32_t dtype, const void* pool, int64_t page_ld, int32_t n_pages, const int32_t* table,
                            int64_t table_ld, int32_t width, const int32_t* row_off, const int32_t* seq_len, int32_t S,

@@ -210,7 +210,7 @@ pages_read_kernel(const __grid_constant__ RowsParams p) {
         float y[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) y[e] = fmaf((float)((word[u] >> (4 * (c + e))) & 15u), sm.x, sm.y);
-        st16(dst + c, y);
+        st16_inf(dst + c, y);                         // (a record's minimum may be infinite)
       }
     }
   }

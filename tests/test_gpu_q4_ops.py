@@ -758,3 +758,26 @@ def test_rope_scaled_infinities(akvs, dt, layout, hd, rot):
     fine = ref.isfinite()
     tol = half(dt) * ref.abs() + 2.0 ** -20 * both + TINY[dt]
     assert ((got.double() - ref).abs()[fine] <= tol[fine]).all()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_read_infinities(akvs, hd):
+    """Groups whose minimum is beyond float16 stand for infinities or NaN in every type; finite values beyond it saturate."""
+    x = rnd(gen(hd), 6, 2, hd)
+    x[0, 0, 3], x[1, 1, 3], x[2, 0, :64] = -1e5, math.nan, 1e5
+    x[3, 1, 5:64], x[3, 1, :5] = 65504.0, -65504.0     # scale 8736: code 15 stands for 65536 (and 1e5 of -x for itself)
+    x[4, 0, 7], x[5, 0, :] = -math.inf, -7e4
+    c = Cache(akvs, gen(1), [6], 2, hd, F32, x, -x)
+    for dt in TYPES:
+        ko, vo = (torch.full((6, 2, hd), 9, dtype=dt, device="cuda") for _ in range(2))
+        akvs.op_pages_read(c.pool, c.table, c.len, ko, vo, ints([0, 6]))
+        for got, which in ((ko, 0), (vo, 1)):
+            code, scale, least = c.records[which]
+            ref = code * scale + least                 # (0 * inf is NaN here as there)
+            if dt == F16:
+                assert int((ref[ref.isfinite()].abs() > 65504).sum()) == (59 if which == 0 else 6)
+                ref = torch.where(ref.isfinite(), ref.clamp(-65504, 65504), ref)
+            assert int(ref.isinf().sum()) > 64 and torch.equal(got.isnan(), ref.isnan()) and torch.equal(got.isinf(), ref.isinf())
+            assert torch.equal(got[got.isinf()].double(), ref[ref.isinf()])
+            fine = ref.isfinite()
+            assert ((got.double() - ref).abs()[fine] <= ((half(dt) + 2.0 ** -24) * ref.abs() + TINY[dt])[fine]).all()
