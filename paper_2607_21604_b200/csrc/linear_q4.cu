@@ -47,6 +47,7 @@ struct LinearQ4Params {
   float* h_out;
   int M, N, groups, pairs, groups_per_split;
   int team;                                           // warps that share a tile's columns
+  int splits;                                         // CTAs of a cluster
 };
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -84,7 +85,7 @@ template <int NT, int PIECES> struct LqSmem {
   static_assert(W % 128 == 0 && XALL % 16 == 0 && RED <= 2 * W, "");
 };
 
-// grid (splits, features / 128, rows / (8 NT)), the splits one cluster
+// grid rows / (8 NT) x features / 128 x splits, the splits one cluster
 template <typename T, int NT>
 __global__ void __launch_bounds__(LQ_THREADS, sizeof(T) == 4 ? 1 : 2)
 linear_q4_kernel(const __grid_constant__ LinearQ4Params p) {
@@ -94,12 +95,13 @@ linear_q4_kernel(const __grid_constant__ LinearQ4Params p) {
   __shared__ uint64_t full[2];
   __shared__ volatile int gave_up;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gr = lane >> 2, t = lane & 3;
-  const int row0 = blockIdx.z * ROWS, f0 = blockIdx.y * LQ_F + warp * 16;
-  const int g0 = blockIdx.x * p.groups_per_split, g1 = min(g0 + p.groups_per_split, p.groups), chunks = (g1 - g0 + XG - 1) / XG;
+  const int f_ranges = (p.N + LQ_F - 1) / LQ_F, unit = (int)blockIdx.x / p.splits, f_range = unit % f_ranges;
+  const int row0 = unit / f_ranges * ROWS, f0 = f_range * LQ_F + warp * 16;
+  const int g0 = (int)blockIdx.x % p.splits * p.groups_per_split, g1 = min(g0 + p.groups_per_split, p.groups), chunks = (g1 - g0 + XG - 1) / XG;
   const bool mine = f0 < p.N;
-  const int tiles = (p.N + 15) / 16, nt = min(LQ_WARPS, tiles - (int)blockIdx.y * LQ_WARPS);   // blocks side by side here
+  const int tiles = (p.N + 15) / 16, nt = min(LQ_WARPS, tiles - f_range * LQ_WARPS);   // blocks side by side here
   auto pairs = [&](int c) { return min(XG / 2, (g1 - g0 - c * XG + 1) / 2); };       // of a chunk
-  auto source = [&](int c, int k) { return p.w + block_of(blockIdx.y * LQ_WARPS, g0 / 2 + c * (XG / 2) + k, tiles, p.pairs) * LQ_BLOCK; };
+  auto source = [&](int c, int k) { return p.w + block_of(f_range * LQ_WARPS, g0 / 2 + c * (XG / 2) + k, tiles, p.pairs) * LQ_BLOCK; };
   pdl_trigger();
   // Weights on their way to L2 before this kernel may read anything: a hint, which what is written meanwhile outlives
   if (warp < 2 && lane < XG / 2 && warp < chunks && lane < pairs(warp))
@@ -292,7 +294,7 @@ linear_q4_kernel(const __grid_constant__ LinearQ4Params p) {
   const int splits = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   // 128 features x ROWS sums, shared out over the cluster's CTAs
   for (int i = rank * LQ_THREADS + threadIdx.x; i < ROWS * LQ_F; i += splits * LQ_THREADS) {
-    const int r = i / LQ_F, f = i % LQ_F, row = row0 + r, n = blockIdx.y * LQ_F + f;
+    const int r = i / LQ_F, f = i % LQ_F, row = row0 + r, n = f_range * LQ_F + f;
     if (row >= p.M || n >= p.N) continue;
     float s = 0.f;
 #pragma unroll 4
@@ -581,18 +583,17 @@ linear_q4_pack_kernel(const uint8_t* codes, const uint32_t* recs, int N, int gro
 template <typename T, int NT>
 int32_t launch(const LinearQ4Params& p0, cudaStream_t st) {
   LinearQ4Params p = p0;
-  const int tiles = akvs_cdiv(p.N, LQ_F), blocks = akvs_cdiv(p.M, 8 * NT);
-  if (tiles > 65535 || blocks > 65535) return AKVS_ERR_TOO_LARGE;
+  const int64_t units = (int64_t)akvs_cdiv(p.N, LQ_F) * akvs_cdiv(p.M, 8 * NT);
   // Ranges of columns, 512 of them or more each: as many as let every CTA run at once, two on an SM.
   using S = LqSmem<NT, sizeof(T) == 4 ? 3 : 1>;
   static std::atomic<uint64_t> smem_set{0};
   AKVS_CUDA(smem_opt_in((const void*)linear_q4_kernel<T, NT>, S::BYTES, smem_set));
   int splits = 1;
-  while (splits < 8 && (int64_t)tiles * blocks * splits * 2 <= 2 * 148 && akvs_cdiv(p.groups, splits * 2) >= XG) splits *= 2;
+  while (splits < 8 && units * splits * 2 <= 2 * 148 && akvs_cdiv(p.groups, splits * 2) >= XG) splits *= 2;
   p.groups_per_split = akvs_cdiv(akvs_cdiv(p.groups, splits), XG) * XG;
-  splits = akvs_cdiv(p.groups, p.groups_per_split);
+  p.splits = splits = akvs_cdiv(p.groups, p.groups_per_split);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(splits, tiles, blocks);
+  cfg.gridDim = dim3((unsigned)(units * splits));
   cfg.blockDim = dim3(LQ_THREADS);
   cfg.dynamicSmemBytes = S::BYTES;
   cfg.stream = st;
@@ -632,7 +633,7 @@ struct TcParams {
   void* y;
   const float* h;
   float* h_out;
-  int M, N, tiles16, pairs, pairs_per_split, rows_per_block, steps;
+  int M, N, tiles16, pairs, pairs_per_split, rows_per_block, steps, splits, f_ranges, blocks;
   bool fours;                                         // four results in a row lie together
 };
 
@@ -757,7 +758,7 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&r)[16]) {
                : "r"(taddr) : "memory");
 }
 
-// grid (splits, features / 256, row blocks), the splits one cluster.  Warps 0 - 7: codes to operands, a thread per
+// grid row blocks x features / 256 x splits, the splits one cluster.  Warps 0 - 7: codes to operands, a thread per
 // feature; 8 - 15: sums, a thread per feature; 16, 17: products of either tile; 18: copies.
 // A thread that issues products waits at one barrier a step (84 cycles even when it is open) and signals one: operands are
 // there and the place for the products is free; the warps that read the sums give back operands and x as well.  With codes and
@@ -777,7 +778,8 @@ linear_q4_tc_kernel(const __grid_constant__ TcParams p) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // The order of stages, for all roles: two steps of codes for every pair of groups, and after the last pair of 64 groups, or
   // of this range, two steps of their minima.  Stage i uses slots 2 (i % 2) and the next one of operands.
-  const int p0 = blockIdx.x * p.pairs_per_split, p1 = min(p0 + p.pairs_per_split, p.pairs);
+  const int unit = (int)blockIdx.x / p.splits, f_range = unit % p.f_ranges, block = unit / p.f_ranges;
+  const int p0 = (int)blockIdx.x % p.splits * p.pairs_per_split, p1 = min(p0 + p.pairs_per_split, p.pairs);
   auto ends = [&](int pr) { return (pr & 31) == 31 || pr + 1 == p1; };
   const int n_stages = p1 - p0 + (p1 + 31) / 32 - p0 / 32;
   if (threadIdx.x == 0) {
@@ -806,15 +808,15 @@ linear_q4_tc_kernel(const __grid_constant__ TcParams p) {
   const uint32_t tmem = tmem_base;
   auto d_col = [&](int tile, int b) { return tmem + (uint32_t)((tile * ND + b) * NB); };
   auto a_col = [&](int tile, int b) { return tmem + 256u + (uint32_t)((tile * NA + b) * 32); };
-  const uint8_t* xt = p.xt + (int64_t)blockIdx.z * p.steps * S::X;
+  const uint8_t* xt = p.xt + (int64_t)block * p.steps * S::X;
   const uint32_t full0 = tc::smem_u32(full), empty0 = tc::smem_u32(empty);
   float2 acc[NB / 2];
 
   if (warp == 18) {
     // ---- copies: a stage of codes is the blocks of 256 features, one piece, and two steps of x
     if (tc::elect_one()) {
-      const uint8_t* w0 = p.w + block_of(blockIdx.y * 16, 0, p.tiles16, p.pairs) * LQ_BLOCK;
-      const int bytes = min(16, p.tiles16 - (int)blockIdx.y * 16) * LQ_BLOCK;
+      const uint8_t* w0 = p.w + block_of(f_range * 16, 0, p.tiles16, p.pairs) * LQ_BLOCK;
+      const int bytes = min(16, p.tiles16 - f_range * 16) * LQ_BLOCK;
       auto weights = [&](int st, int pr, bool minima) {
         tc::mbar_expect_tx(&full[st], 2 * S::X + (minima ? 0 : bytes));
         if (!minima) bulk_copy(ring + st * S::BYTES + 2 * S::X, w0 + (int64_t)pr * bytes, bytes, &full[st]);
@@ -1020,14 +1022,14 @@ linear_q4_tc_kernel(const __grid_constant__ TcParams p) {
     }
   } else if (warp < 8) {
     for (int i = threadIdx.x; i < splits * NB; i += 256)
-      pws[i] = __ldcg(p.pow + ((int64_t)(i / NB) * gridDim.z + blockIdx.z) * NB + i % NB);
+      pws[i] = __ldcg(p.pow + ((int64_t)(i / NB) * p.blocks + block) * NB + i % NB);
   }
   cluster.sync();
   pdl_trigger();
   // number i of four features of a row: its place in shared memory, and the results
   auto place = [&](int i) { return i / (TC_F / 4) * LD + i % (TC_F / 4) * 4; };
   auto put = [&](int i, const float (&s)[4]) {
-    const int row = blockIdx.z * p.rows_per_block + i / (TC_F / 4), n = blockIdx.y * TC_F + i % (TC_F / 4) * 4;
+    const int row = block * p.rows_per_block + i / (TC_F / 4), n = f_range * TC_F + i % (TC_F / 4) * 4;
     if (row >= p.M || n >= p.N) return;
     const int64_t at = (int64_t)row * p.N + n;
     if (p.fours && p.h_out) {
@@ -1135,7 +1137,6 @@ int32_t launch_tc(const LinearQ4Params& l, void* scratch, cudaStream_t st) {
   AKVS_CUDA(smem_opt_in((const void*)linear_q4_tc_kernel<T, NB>, S::SMEM, smem_set));
   TcParams p;
   const int blocks = tc_blocks(l.M), tiles = akvs_cdiv(l.N, TC_F);
-  if (tiles > 65535 || blocks > 65535) return AKVS_ERR_TOO_LARGE;
   p.w = l.w; p.y = l.y; p.h = l.h; p.h_out = l.h_out; p.M = l.M; p.N = l.N; p.pairs = l.pairs;
   p.tiles16 = akvs_cdiv(l.N, 16);
   p.fours = l.N % 4 == 0 && (l.h_out ? (reinterpret_cast<uintptr_t>(l.h) | reinterpret_cast<uintptr_t>(l.h_out)) % 16 == 0
@@ -1156,13 +1157,15 @@ int32_t launch_tc(const LinearQ4Params& l, void* scratch, cudaStream_t st) {
     if (cost < best) { best = cost; splits = k; }
   }
   p.pairs_per_split = akvs_cdiv(l.pairs, splits);
-  splits = akvs_cdiv(l.pairs, p.pairs_per_split);
+  p.splits = splits = akvs_cdiv(l.pairs, p.pairs_per_split);
+  p.f_ranges = tiles;
+  p.blocks = blocks;
   AKVS_CUDA(launch_pdl(linear_q4_rows_kernel<T, NB>, dim3(blocks * NB, splits), dim3(ROWS_THREADS), 0, st, reinterpret_cast<const T*>(l.x),
                        l.x_ld, l.M, p.rows_per_block, l.groups, l.pairs, p.pairs_per_split, reinterpret_cast<uint8_t*>(scratch),
                        const_cast<float*>(p.pow)));
   AKVS_LAUNCHED();
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(splits, tiles, blocks);
+  cfg.gridDim = dim3((unsigned)((int64_t)splits * tiles * blocks));
   cfg.blockDim = dim3(TC_THREADS);
   cfg.dynamicSmemBytes = S::SMEM;
   cfg.stream = st;
@@ -1191,6 +1194,16 @@ Path path_of(int dtype, int M, int N, int K) {
   return Path::clusters;
 }
 
+// What a grid's one dimension holds, with up to 8 ranges of columns; beyond that lie only calls whose x or y no GPU holds.
+bool fits_a_grid(int dtype, int M, int N, int K) {
+  switch (path_of(dtype, M, N, K)) {
+    case Path::few: return true;
+    case Path::clusters: return (int64_t)akvs_cdiv(M, 8) * akvs_cdiv(N, LQ_F) <= 0x7fffffff / 8;
+    default:
+      return (int64_t)tc_blocks(M) * akvs_cdiv(N, TC_F) <= 0x7fffffff / 8 && tc_blocks(M) < 1 << 25 && (double)tc_blocks(M) * (K + 4096.0) < 1e14;
+  }
+}
+
 int32_t linear(int32_t dtype, const void* x, int64_t x_ld, const void* w, int64_t w_bytes, void* y, const float* h, float* h_out,
                int32_t M, int32_t N, int32_t K, void* scratch, int64_t scratch_size, void* stream) {
   if (dtype != AKVS_F32 && dtype != AKVS_BF16 && dtype != AKVS_F16) return AKVS_ERR_UNSUPPORTED;
@@ -1204,10 +1217,11 @@ int32_t linear(int32_t dtype, const void* x, int64_t x_ld, const void* w, int64_
   if (!aligned16(x) || !aligned16(w) || x_ld * es % 16 || reinterpret_cast<uintptr_t>(out) % (h_out ? 4 : es) ||
       reinterpret_cast<uintptr_t>(h) % 4)
     return AKVS_ERR_INVALID_ARG;
+  const int64_t room = akvs_op_linear_q4_scratch_bytes(dtype, M, N, K);
+  if (room < 0) return AKVS_ERR_TOO_LARGE;
   const int64_t x_n = ((M - 1) * x_ld + K) * es, out_n = (int64_t)M * N * (h_out ? 4 : es);
   if (bytes_overlap(x, x_n, out, out_n) || bytes_overlap(w, need, out, out_n) || (h_out && h != h_out && bytes_overlap(h, out_n, out, out_n)))
     return AKVS_ERR_INVALID_ARG;
-  const int64_t room = akvs_op_linear_q4_scratch_bytes(dtype, M, N, K);
   if (room > 0) {
     if (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 255) || scratch_size < room) return AKVS_ERR_WORKSPACE;
     if (bytes_overlap(x, x_n, scratch, room) || bytes_overlap(w, need, scratch, room) || bytes_overlap(out, out_n, scratch, room) ||
@@ -1244,7 +1258,8 @@ extern "C" int64_t akvs_linear_q4_bytes(int32_t N, int32_t K) {
 }
 
 extern "C" int64_t akvs_op_linear_q4_scratch_bytes(int32_t dtype, int32_t M, int32_t N, int32_t K) {
-  if ((dtype != AKVS_F32 && dtype != AKVS_BF16 && dtype != AKVS_F16) || M < 0 || akvs_linear_q4_bytes(N, K) < 0) return -1;
+  if ((dtype != AKVS_F32 && dtype != AKVS_BF16 && dtype != AKVS_F16) || M < 0 || akvs_linear_q4_bytes(N, K) < 0 || !fits_a_grid(dtype, M, N, K))
+    return -1;
   return path_of(dtype, M, N, K) == Path::tc ? tc_scratch(M, K) : 0;
 }
 

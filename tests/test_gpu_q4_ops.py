@@ -781,3 +781,28 @@ def test_read_infinities(akvs, hd):
             assert torch.equal(got[got.isinf()].double(), ref[ref.isinf()])
             fine = ref.isfinite()
             assert ((got.double() - ref).abs()[fine] <= ((half(dt) + 2.0 ** -24) * ref.abs() + TINY[dt])[fine]).all()
+
+
+@pytest.mark.parametrize("dt,M,N", [(F32, 9, 65535 * 128 + 200), (F16, 17, 65535 * 256 + 200), (F32, 65535 * 8 + 9, 24), (BF16, 65535 * 64 + 33, 24)])
+def test_linear_many_blocks(akvs, dt, M, N):
+    """More than 65535 ranges of features, or blocks of rows: the first, the last and some others."""
+    g, K = gen(M + N), 64
+    codes = torch.randint(0, 256, (N, 1, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    meta = torch.rand((N, 1, K // 64, 2), generator=g, device="cuda").to(F16)
+    x = rnd(g, M, K, dt=dt)
+    lw = akvs.LinearQ4.from_codes(codes, meta)
+    assert akvs.lib.akvs_op_linear_q4_scratch_bytes({F32: 0, BF16: 1, F16: 2}[dt], M, N, K) >= 0
+    y = akvs.op_linear_q4(x, lw)
+
+    def some(n):
+        return torch.cat([torch.arange(min(n, 150), device="cuda"), torch.randint(0, n, (200,), generator=g, device="cuda"),
+                          torch.arange(max(0, n - 500), n, device="cuda")])
+    rows, feats = some(M), some(N)
+    c = torch.stack([codes[feats, 0] & 15, codes[feats, 0] >> 4], -1).reshape(len(feats), K).double()
+    s, m = (meta[feats, 0, :, i].double().repeat_interleave(64, 1) for i in (0, 1))
+    ref, mag = x[rows].double() @ (c * s + m).T, x[rows].double().abs() @ (15 * s + m.abs()).T
+    got = y[rows][:, feats]
+    assert ((got.double() - ref).abs() <= half(dt) * ref.abs() + linear_tol(K) * mag + TINY[dt]).all()
+    h = torch.full((M, N), 3.0, device="cuda")
+    akvs.op_linear_q4_residual(x, lw, h)
+    assert ((h[rows][:, feats].double() - ref - 3).abs() <= half(F32) * (ref + 3).abs() + linear_tol(K) * mag).all()

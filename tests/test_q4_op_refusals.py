@@ -287,3 +287,15 @@ def test_pool_fork_of_no_sequence(pool):
     with pytest.raises(KeyError):
         pool.fork(a + 1, 2)
     assert _state(pool) == state
+
+
+def test_linear_beyond_a_grid(b):  # noqa: F811
+    """More blocks than a launch has: refused by both, the call and its scratch size.  Sizes that a GPU holds are not."""
+    f = b.lib.akvs_op_linear_q4_scratch_bytes
+    last = 2 ** 31 - 1
+    for dt, M, N, K in ((0, last, 2 ** 30, 64), (1, last, 2 ** 30, 64), (2, 2 ** 30, 2 ** 31 - 256, 64), (1, last, 64, 2 ** 31 - 64)):
+        assert f(dt, M, N, K) == -1
+        change = dict(dtype=dt, M=M, N=N, K=K, x_ld=K, w_bytes=2 ** 62, x=_at(0), w=2 ** 62, y=2 ** 60, scratch=_at(1), scratch_bytes=2 ** 62)
+        assert b.lib.akvs_op_linear_q4(*{**LINEAR, **change}.values()) == TOO_LARGE
+    for dt, M, N, K in ((0, 9, 2 ** 31 - 256, 64), (0, 2 ** 24, 64, 64), (1, 17, 2 ** 31 - 256, 64), (2, 2 ** 26, 1, 64), (0, 8, 2 ** 31 - 256, 64)):
+        assert f(dt, M, N, K) >= 0
