@@ -183,12 +183,20 @@ template <typename T> __device__ __forceinline__ T from_f_inf(float x) {
   if constexpr (std::is_same<T, f16>::value) return __float2half_rn(f16_end(x));
   else return from_f<T>(x);
 }
+// (Looked for in all values at once: 11648 interleaved rows of 48 heads, half of each turned, 57.4 us; with two comparisons for
+// each value 59.8, where infinities end at 65504 55.6.)
 template <typename T> __device__ __forceinline__ void st16_inf(T* p, const float (&o)[VecOf<T>::N]) {
-  if constexpr (std::is_same<T, f16>::value)
-    *reinterpret_cast<uint4*>(p) = make_uint4(pack_f16x2_inf(o[0], o[1]), pack_f16x2_inf(o[2], o[3]), pack_f16x2_inf(o[4], o[5]),
-                                              pack_f16x2_inf(o[6], o[7]));
-  else
-    st16(p, o);
+  if constexpr (std::is_same<T, f16>::value) {
+    float top = fabsf(o[0]);
+#pragma unroll
+    for (int i = 1; i < 8; ++i) top = fmaxf(top, fabsf(o[i]));
+    if (__builtin_expect(top == INFINITY, 0)) {
+      *reinterpret_cast<uint4*>(p) = make_uint4(pack_f16x2_inf(o[0], o[1]), pack_f16x2_inf(o[2], o[3]), pack_f16x2_inf(o[4], o[5]),
+                                                pack_f16x2_inf(o[6], o[7]));
+      return;
+    }
+  }
+  st16(p, o);
 }
 
 __device__ __forceinline__ float warp_sum(float v) {
