@@ -47,8 +47,21 @@ struct LinearQ4Params {
   float* h_out;
   int M, N, groups, pairs, groups_per_split;
   int team;                                           // warps that share a tile's columns
-  int splits;                                         // CTAs of a cluster
 };
+
+// A grid of clusters side by side along the features, and of blocks of rows over the two short dimensions.
+dim3 row_grid(int64_t ctas, int blocks) { return dim3((unsigned)ctas, blocks < 65535 ? blocks : 65535, akvs_cdiv(blocks, 65535)); }
+__device__ __forceinline__ int row_block() { return (int)(blockIdx.z * 65535u + blockIdx.y); }
+__device__ __forceinline__ int cluster_number() {
+  uint32_t x;
+  asm("mov.u32 %0, %%clusterid.x;" : "=r"(x));
+  return (int)x;
+}
+__device__ __forceinline__ int cluster_rank() {
+  uint32_t x;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(x));
+  return (int)x;
+}
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
@@ -85,7 +98,7 @@ template <int NT, int PIECES> struct LqSmem {
   static_assert(W % 128 == 0 && XALL % 16 == 0 && RED <= 2 * W, "");
 };
 
-// grid rows / (8 NT) x features / 128 x splits, the splits one cluster
+// grid (features / 128 x splits, rows / (8 NT)), the splits one cluster
 template <typename T, int NT>
 __global__ void __launch_bounds__(LQ_THREADS, sizeof(T) == 4 ? 1 : 2)
 linear_q4_kernel(const __grid_constant__ LinearQ4Params p) {
@@ -95,9 +108,9 @@ linear_q4_kernel(const __grid_constant__ LinearQ4Params p) {
   __shared__ uint64_t full[2];
   __shared__ volatile int gave_up;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gr = lane >> 2, t = lane & 3;
-  const int f_ranges = (p.N + LQ_F - 1) / LQ_F, unit = (int)blockIdx.x / p.splits, f_range = unit % f_ranges;
-  const int row0 = unit / f_ranges * ROWS, f0 = f_range * LQ_F + warp * 16;
-  const int g0 = (int)blockIdx.x % p.splits * p.groups_per_split, g1 = min(g0 + p.groups_per_split, p.groups), chunks = (g1 - g0 + XG - 1) / XG;
+  const int f_range = cluster_number(), row0 = row_block() * ROWS, f0 = f_range * LQ_F + warp * 16;
+  if (row_block() > (p.M - 1) / ROWS) return;         // (a whole cluster)
+  const int g0 = cluster_rank() * p.groups_per_split, g1 = min(g0 + p.groups_per_split, p.groups), chunks = (g1 - g0 + XG - 1) / XG;
   const bool mine = f0 < p.N;
   const int tiles = (p.N + 15) / 16, nt = min(LQ_WARPS, tiles - f_range * LQ_WARPS);   // blocks side by side here
   auto pairs = [&](int c) { return min(XG / 2, (g1 - g0 - c * XG + 1) / 2); };       // of a chunk
@@ -583,17 +596,17 @@ linear_q4_pack_kernel(const uint8_t* codes, const uint32_t* recs, int N, int gro
 template <typename T, int NT>
 int32_t launch(const LinearQ4Params& p0, cudaStream_t st) {
   LinearQ4Params p = p0;
-  const int64_t units = (int64_t)akvs_cdiv(p.N, LQ_F) * akvs_cdiv(p.M, 8 * NT);
+  const int tiles = akvs_cdiv(p.N, LQ_F), blocks = akvs_cdiv(p.M, 8 * NT);
   // Ranges of columns, 512 of them or more each: as many as let every CTA run at once, two on an SM.
   using S = LqSmem<NT, sizeof(T) == 4 ? 3 : 1>;
   static std::atomic<uint64_t> smem_set{0};
   AKVS_CUDA(smem_opt_in((const void*)linear_q4_kernel<T, NT>, S::BYTES, smem_set));
   int splits = 1;
-  while (splits < 8 && units * splits * 2 <= 2 * 148 && akvs_cdiv(p.groups, splits * 2) >= XG) splits *= 2;
+  while (splits < 8 && (int64_t)tiles * blocks * splits * 2 <= 2 * 148 && akvs_cdiv(p.groups, splits * 2) >= XG) splits *= 2;
   p.groups_per_split = akvs_cdiv(akvs_cdiv(p.groups, splits), XG) * XG;
-  p.splits = splits = akvs_cdiv(p.groups, p.groups_per_split);
+  splits = akvs_cdiv(p.groups, p.groups_per_split);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(units * splits));
+  cfg.gridDim = row_grid((int64_t)tiles * splits, blocks);
   cfg.blockDim = dim3(LQ_THREADS);
   cfg.dynamicSmemBytes = S::BYTES;
   cfg.stream = st;
@@ -633,7 +646,7 @@ struct TcParams {
   void* y;
   const float* h;
   float* h_out;
-  int M, N, tiles16, pairs, pairs_per_split, rows_per_block, steps, splits, f_ranges, blocks;
+  int M, N, tiles16, pairs, pairs_per_split, rows_per_block, steps, blocks;
   bool fours;                                         // four results in a row lie together
 };
 
@@ -758,7 +771,7 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&r)[16]) {
                : "r"(taddr) : "memory");
 }
 
-// grid row blocks x features / 256 x splits, the splits one cluster.  Warps 0 - 7: codes to operands, a thread per
+// grid (features / 256 x splits, row blocks), the splits one cluster.  Warps 0 - 7: codes to operands, a thread per
 // feature; 8 - 15: sums, a thread per feature; 16, 17: products of either tile; 18: copies.
 // A thread that issues products waits at one barrier a step (84 cycles even when it is open) and signals one: operands are
 // there and the place for the products is free; the warps that read the sums give back operands and x as well.  With codes and
@@ -778,8 +791,9 @@ linear_q4_tc_kernel(const __grid_constant__ TcParams p) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // The order of stages, for all roles: two steps of codes for every pair of groups, and after the last pair of 64 groups, or
   // of this range, two steps of their minima.  Stage i uses slots 2 (i % 2) and the next one of operands.
-  const int unit = (int)blockIdx.x / p.splits, f_range = unit % p.f_ranges, block = unit / p.f_ranges;
-  const int p0 = (int)blockIdx.x % p.splits * p.pairs_per_split, p1 = min(p0 + p.pairs_per_split, p.pairs);
+  const int f_range = cluster_number(), block = row_block();
+  if (block >= p.blocks) return;                      // (a whole cluster)
+  const int p0 = cluster_rank() * p.pairs_per_split, p1 = min(p0 + p.pairs_per_split, p.pairs);
   auto ends = [&](int pr) { return (pr & 31) == 31 || pr + 1 == p1; };
   const int n_stages = p1 - p0 + (p1 + 31) / 32 - p0 / 32;
   if (threadIdx.x == 0) {
@@ -1157,15 +1171,14 @@ int32_t launch_tc(const LinearQ4Params& l, void* scratch, cudaStream_t st) {
     if (cost < best) { best = cost; splits = k; }
   }
   p.pairs_per_split = akvs_cdiv(l.pairs, splits);
-  p.splits = splits = akvs_cdiv(l.pairs, p.pairs_per_split);
-  p.f_ranges = tiles;
+  splits = akvs_cdiv(l.pairs, p.pairs_per_split);
   p.blocks = blocks;
   AKVS_CUDA(launch_pdl(linear_q4_rows_kernel<T, NB>, dim3(blocks * NB, splits), dim3(ROWS_THREADS), 0, st, reinterpret_cast<const T*>(l.x),
                        l.x_ld, l.M, p.rows_per_block, l.groups, l.pairs, p.pairs_per_split, reinterpret_cast<uint8_t*>(scratch),
                        const_cast<float*>(p.pow)));
   AKVS_LAUNCHED();
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((int64_t)splits * tiles * blocks));
+  cfg.gridDim = row_grid((int64_t)tiles * splits, blocks);
   cfg.blockDim = dim3(TC_THREADS);
   cfg.dynamicSmemBytes = S::SMEM;
   cfg.stream = st;
@@ -1194,7 +1207,7 @@ Path path_of(int dtype, int M, int N, int K) {
   return Path::clusters;
 }
 
-// What a grid's one dimension holds, with up to 8 ranges of columns; beyond that lie only calls whose x or y no GPU holds.
+// What a grid holds, with up to 8 ranges of columns; beyond that lie only calls whose x or y no GPU holds.
 bool fits_a_grid(int dtype, int M, int N, int K) {
   switch (path_of(dtype, M, N, K)) {
     case Path::few: return true;
