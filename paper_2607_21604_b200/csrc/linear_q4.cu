@@ -22,6 +22,7 @@
 // cluster share the features and add their sums over distributed shared memory, in the order of the ranges.  16 rows of
 // 14336 x 4096 in 17.7 us (1.9 TB/s of weights), bound by the instructions that turn codes into operands and by its start.
 #include <cooperative_groups.h>
+#include "linear_rule.h"
 #include "tc_common.cuh"
 
 namespace cg = cooperative_groups;
@@ -1120,14 +1121,14 @@ int64_t tc_scratch(int M, int K) {
   return (int64_t)tc_blocks(M) * nb * (128ll * (2 * pairs + lq_min_steps(groups)) + 8 * 4) + 256;
 }
 
-// How many clusters of k CTAs of the kernel run at once, asked once per device and size.
+// How many clusters of k CTAs of the kernel run at once (0: a cluster of that size does not), asked once per device and size.
 template <typename T, int NB>
 int32_t clusters_at_a_time(int k, int& fit) {
-  static std::atomic<int> known[64][9];
+  static std::atomic<int> known[64][LQ_MAX_RANGES + 1];              // one more than fit
   int dev = 0;
   AKVS_CUDA(cudaGetDevice(&dev));
-  fit = known[dev & 63][k].load(std::memory_order_relaxed);
-  if (fit > 0) return AKVS_OK;
+  fit = known[dev & 63][k].load(std::memory_order_relaxed) - 1;
+  if (fit >= 0) return AKVS_OK;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(k, 148);
   cfg.blockDim = dim3(TC_THREADS);
@@ -1138,9 +1139,12 @@ int32_t clusters_at_a_time(int k, int& fit) {
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  AKVS_CUDA((cudaOccupancyMaxActiveClusters(&fit, linear_q4_tc_kernel<T, NB>, &cfg)));
-  if (fit < 1) return AKVS_ERR_CUDA;
-  known[dev & 63][k].store(fit, std::memory_order_relaxed);
+  if (cudaOccupancyMaxActiveClusters(&fit, linear_q4_tc_kernel<T, NB>, &cfg) != cudaSuccess) {
+    cudaGetLastError();                               // not an error of this call: other sizes may do
+    fit = 0;
+  }
+  fit = fit < 0 ? 0 : fit;
+  known[dev & 63][k].store(fit + 1, std::memory_order_relaxed);
   return AKVS_OK;
 }
 
@@ -1160,16 +1164,11 @@ int32_t launch_tc(const LinearQ4Params& l, void* scratch, cudaStream_t st) {
   p.xt = reinterpret_cast<uint8_t*>(scratch);
   const int64_t x_bytes = (int64_t)blocks * p.steps * S::X;
   p.pow = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(scratch) + x_bytes);
-  // One CTA an SM.  Ranges of columns, four pairs of groups or more each, as many as give the shortest run: rounds of
-  // clusters (what fits at a time depends on how many SMs a part of the GPU has) times steps, with 20 for start and end.
-  int splits = 1;
-  double best = 1e300;
-  for (int k = 1; k <= 8 && (k == 1 || l.pairs / k >= 4); ++k) {
-    int fit = 0;
-    AKVS_TRY((clusters_at_a_time<T, NB>(k, fit)));
-    const double cost = (double)akvs_cdiv((int64_t)tiles * blocks, fit) * (2 * akvs_cdiv(l.pairs, k) + 20);
-    if (cost < best) { best = cost; splits = k; }
-  }
+  // One CTA an SM; how many clusters fit at a time depends on how many SMs a part of the GPU has.
+  int fit[LQ_MAX_RANGES + 1] = {};
+  for (int k = 1; k <= LQ_MAX_RANGES && (k == 1 || l.pairs / k >= 4); ++k) AKVS_TRY((clusters_at_a_time<T, NB>(k, fit[k])));
+  int splits = lq_ranges((int64_t)tiles * blocks, l.pairs, fit);
+  if (splits == 0) return AKVS_ERR_CUDA;
   p.pairs_per_split = akvs_cdiv(l.pairs, splits);
   splits = akvs_cdiv(l.pairs, p.pairs_per_split);
   p.blocks = blocks;
