@@ -93,7 +93,7 @@ __device__ __noinline__ void drain(uint64_t* bar, uint32_t parity) {
 // Shared memory of a CTA: two stages of weights ([pair][8 blocks], 8 groups), two of x.
 template <int NT, int PIECES> struct LqSmem {
   static constexpr int PAIR = LQ_WARPS * LQ_BLOCK, W = XG / 2 * PAIR, X = XG * NT * PIECES * 1024;
-  static constexpr int XM = NT * 2 * 32 * 4, XP = NT * 8 * 4;         // sums of x as operands, powers of two of the rows
+  static constexpr int XM = NT * 2 * 32 * 4 * (PIECES > 1 ? 2 : 1), XP = NT * 8 * 4;     // sums of x as operands, powers of two of the rows
   static constexpr int XALL = X + XM + XP, BYTES = 2 * W + 2 * XALL;
   static constexpr int RED = (LQ_F + 4) * 4 * 8 * NT;                 // the sums, where the weights were
   static_assert(W % 128 == 0 && XALL % 16 == 0 && RED <= 2 * W, "");
@@ -181,11 +181,17 @@ linear_q4_kernel(const __grid_constant__ LinearQ4Params p) {
       s += __shfl_xor_sync(0xFFFFFFFFu, s, 1);
       s += __shfl_xor_sync(0xFFFFFFFFu, s, 2);
       if (lane == 0) *reinterpret_cast<float*>(xb + S::X + S::XM + (rr * 8 + warp) * 4) = __uint_as_float((uint32_t)(127 - up) << 23);
-      // the group's sum, below 2^21, as two float16 of a sixty-fourth of it: k = 2 (g % 4), 2 (g % 4) + 1 of half g / 4
+      // the group's sum, below 2^21, as two float16 of a sixty-fourth of it: k = 2 (g % 4), 2 (g % 4) + 1 of half g / 4.  Two hold
+      // it to 2^-23 of itself, a float's last bit, or to 2^-33 of the largest value of the columns staged: enough beside 16-bit x; float
+      // rows have a third.
       if (t == 0) {
         const float m = s * 0x1p-6f;
         const __half hi = __float2half_rn(m), lo = __float2half_rn(m - __half2float(hi));
-        *reinterpret_cast<__half2*>(xb + S::X + ((rr * 2 + (lane >> 4)) * 32 + warp * 4 + ((lane >> 2) & 3)) * 4) = __halves2half2(hi, lo);
+        uint8_t* at = xb + S::X + ((rr * 2 + (lane >> 4)) * 32 + warp * 4 + ((lane >> 2) & 3)) * 4;
+        *reinterpret_cast<__half2*>(at) = __halves2half2(hi, lo);
+        if (PIECES > 1)
+          *reinterpret_cast<__half2*>(at + NT * 256) =
+              __halves2half2(__float2half_rn(m - __half2float(hi) - __half2float(lo)), __float2half_rn(0.f));
       }
 #pragma unroll
       for (int wd = 0; wd < 2; ++wd) {
@@ -247,6 +253,11 @@ linear_q4_kernel(const __grid_constant__ LinearQ4Params p) {
         for (int e = 0; e < 4; ++e) sum[n][e] = low[n][e] = 0.f;
         const uint32_t* xm = reinterpret_cast<const uint32_t*>(xb + S::X) + n * 64 + lane;
         mma16816(low[n], am[0], am[1], am[2], am[3], xm[0], xm[32]);
+        if (PIECES > 1) {
+          float own[4] = {0.f, 0.f, 0.f, 0.f};
+          mma16816(own, am[0], am[1], am[2], am[3], xm[NT * 64], xm[NT * 64 + 32]);
+          add4(low[n], own);
+        }
       }
 #pragma unroll
       for (int g = 0; g < XG; ++g) {

@@ -806,3 +806,16 @@ def test_linear_many_blocks(akvs, dt, M, N):
     h = torch.full((M, N), 3.0, device="cuda")
     akvs.op_linear_q4_residual(x, lw, h)
     assert ((h[rows][:, feats].double() - ref - 3).abs() <= half(F32) * (ref + 3).abs() + linear_tol(K) * mag).all()
+
+
+@pytest.mark.parametrize("M", [5, 9, 40])
+def test_linear_float_sums_of_x(akvs, M):
+    """The sums of x that minima are multiplied by keep all bits of a float: rows with one value of 24 bits, weights without
+    extent.  (Every step is exact; half a last bit is left for the one sum.)"""
+    g = gen(M)
+    lw = akvs.LinearQ4(torch.ones((130, 64), device="cuda"))
+    value = torch.randint(1 << 23, 1 << 24, (M,), generator=g, device="cuda").float() * 2.0 ** torch.randint(-30, 8, (M,), generator=g, device="cuda")
+    x = torch.zeros((M, 64), device="cuda")
+    x[torch.arange(M), torch.randint(0, 64, (M,), generator=g, device="cuda")] = value
+    y = akvs.op_linear_q4(x, lw)
+    assert ((y.double() - value[:, None].double()).abs() <= 2.0 ** -24 * value[:, None].double()).all()
