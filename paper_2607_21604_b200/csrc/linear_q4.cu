@@ -3,10 +3,13 @@
 // Memory bound by the weights (36 bytes per 64 of them) while the rows are few.  A code becomes an operand of a product by
 // an AND alone: in the low bits of a float16 it is the subnormal c 2^-24, 4 bits higher 16 times that, both exact in the
 // tensor cores; x is scaled by the power of two that brings the largest value of a row and range of columns to [2^14,
-// 2^15), where float16 loses nothing above 2^-39 of it (float rows enter as three float16 pieces, all 24 bits; a
-// piece's products are summed by themselves and added in float, since the tensor cores cut off what lies below the last bit
-// of a sum: 1e-6 off instead of 2e-6).  A group's products are summed by themselves and scaled in float, so that weights are
-// what their codes and records say and nothing is rounded but sums.
+// 2^15), where float16 loses nothing above 2^-39 of it (odd columns, which enter with a sixteenth: 2^-35).  A group's products are
+// summed by themselves and scaled in float, so that weights are what their codes and records say and nothing is rounded but sums.
+// Float rows enter as three float16 pieces, which hold all 24 bits of a value down to 2^-15 of the largest and lose what lies
+// below 2^-39 of that.  A piece's products are summed by themselves and added in float, and codes take the highest bits that a
+// subnormal has (an AND and a shift): the tensor cores line products up by their exponents before they cut sums off, and a
+// subnormal's leading zeros are lost with it (root mean square errors of up to 1.3e-6 of y with the AND alone, up to 0.5e-6 so,
+// at the same speed; the 8 or 11 bits of 16-bit rows: 0.4e-6).
 //
 // Weights are laid out once (akvs_op_linear_q4_pack): blocks of 16 features x 2 groups, 1152 bytes; those of 256 features
 // side by side, and so on along the columns, so that every kernel reads long pieces.  A feature's 64 bytes of codes are
@@ -76,6 +79,18 @@ __device__ __forceinline__ void bulk_copy(void* dst, const void* src, uint32_t b
 __device__ __forceinline__ void add4(float (&d)[4], const float (&x)[4]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) d[e] += x[e];
+}
+// Eight codes as operands, for the values (0 4) (2 6) and (1 5) (3 7).  16-bit rows: an AND alone, c 2^-24 and 16 c 2^-24.  Float
+// rows (TOP): in the highest bits that a subnormal has, 64 c 2^-24.
+template <bool TOP> __device__ __forceinline__ void operands(uint32_t w, uint32_t (&first)[2], uint32_t (&second)[2]) {
+  if constexpr (TOP) {
+    first[0] = (w << 6) & 0x03C003C0u; first[1] = (w >> 2) & 0x03C003C0u;
+    second[0] = (w << 2) & 0x03C003C0u; second[1] = (w >> 6) & 0x03C003C0u;
+  } else {
+    const uint32_t w8 = w >> 8;
+    first[0] = w & 0x000F000Fu; first[1] = w8 & 0x000F000Fu;
+    second[0] = w & 0x00F000F0u; second[1] = w8 & 0x00F000F0u;
+  }
 }
 // the same with nothing to add to
 __device__ __forceinline__ void mma16816_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -197,7 +212,7 @@ linear_q4_kernel(const __grid_constant__ LinearQ4Params p) {
       for (int wd = 0; wd < 2; ++wd) {
         float y[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = f[8 * wd + e] * ((e & 1) ? 0.0625f : 1.f);
+        for (int e = 0; e < 8; ++e) y[e] = f[8 * wd + e] * (PIECES == 1 && (e & 1) ? 0.0625f : 1.f);
 #pragma unroll
         for (int pc = 0; pc < PIECES; ++pc) {
           uint32_t q[4];
@@ -274,7 +289,9 @@ linear_q4_kernel(const __grid_constant__ LinearQ4Params p) {
         for (int n = 0; n < NT; ++n) d[n][0] = d[n][1] = d[n][2] = d[n][3] = 0.f;
 #pragma unroll
         for (int wd = 0; wd < 2; ++wd) {
-          const uint32_t a = wa[wd], b = wb2[wd], a8 = a >> 8, b8 = b >> 8;
+          uint32_t a0[2], a1[2], b0[2], b1[2];
+          operands<(PIECES > 1)>(wa[wd], a0, a1);
+          operands<(PIECES > 1)>(wb2[wd], b0, b1);
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -282,8 +299,8 @@ linear_q4_kernel(const __grid_constant__ LinearQ4Params p) {
               const uint4 q = *reinterpret_cast<const uint4*>(xb + ((((g * NT + n) * PIECES + pc) * 2 + wd) * 32 + lane) * 16);
               float own[4] = {0.f, 0.f, 0.f, 0.f};
               float(&to)[4] = PIECES > 1 ? own : d[n];
-              mma16816(to, a & 0x000F000Fu, b & 0x000F000Fu, a8 & 0x000F000Fu, b8 & 0x000F000Fu, q.x, q.y);
-              mma16816(to, a & 0x00F000F0u, b & 0x00F000F0u, a8 & 0x00F000F0u, b8 & 0x00F000F0u, q.z, q.w);
+              mma16816(to, a0[0], b0[0], a0[1], b0[1], q.x, q.y);
+              mma16816(to, a1[0], b1[0], a1[1], b1[1], q.z, q.w);
               if (PIECES > 1) add4(d[n], own);
             }
         }
@@ -300,7 +317,7 @@ linear_q4_kernel(const __grid_constant__ LinearQ4Params p) {
         const float2 pw = *reinterpret_cast<const float2*>(xb + S::X + S::XM + (8 * n + 2 * t) * 4);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          acc[n][e] = fmaf(fmaf(sum[n][e], 0x1p24f, low[n][e] * 0x1p6f), e & 1 ? pw.y : pw.x, acc[n][e]);
+          acc[n][e] = fmaf(fmaf(sum[n][e], PIECES > 1 ? 0x1p18f : 0x1p24f, low[n][e] * 0x1p6f), e & 1 ? pw.y : pw.x, acc[n][e]);
       }
     }
     if (c + 1 < chunks) convert_x(c + 1);
@@ -447,11 +464,11 @@ linear_q4_few_kernel(const __grid_constant__ LinearQ4Params p) {
       }
       int up = 141 - (int)(__float_as_uint(top) >> 23);               // brings the largest value to [2^14, 2^15)
       up = top == 0.f || !(top < INFINITY) ? 0 : min(up, 126);
-      const float even = __uint_as_float((uint32_t)(up + 127) << 23), odd = even * 0.0625f;
+      const float even = __uint_as_float((uint32_t)(up + 127) << 23), odd = PIECES > 1 ? even : even * 0.0625f;
       if (i >= all) continue;
       if (tt == 0) xsum[g * 8 + r] = s;
       // 2^24 for the codes beside it.  (x beyond 2^117 leaves the floats here, and the row becomes infinities or NaN.)
-      if ((u & 7) == 0) xpow[(u >> 3) * 8 + r] = __uint_as_float((uint32_t)(127 - up) << 23) * 0x1p24f;
+      if ((u & 7) == 0) xpow[(u >> 3) * 8 + r] = __uint_as_float((uint32_t)(127 - up) << 23) * (PIECES > 1 ? 0x1p18f : 0x1p24f);
 #pragma unroll
       for (int wd = 0; wd < 2; ++wd) {
         float y[8];
@@ -519,17 +536,18 @@ linear_q4_few_kernel(const __grid_constant__ LinearQ4Params p) {
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
           for (int wd = 0; wd < 2; ++wd) {
-            const uint32_t a = h ? (wd ? ca.w : ca.z) : (wd ? ca.y : ca.x), b = h ? (wd ? cb.w : cb.z) : (wd ? cb.y : cb.x);
-            const uint32_t a8 = a >> 8, b8 = b >> 8;
+            uint32_t a0[2], a1[2], b0[2], b1[2];
+            operands<(PIECES > 1)>(h ? (wd ? ca.w : ca.z) : (wd ? ca.y : ca.x), a0, a1);
+            operands<(PIECES > 1)>(h ? (wd ? cb.w : cb.z) : (wd ? cb.y : cb.x), b0, b1);
 #pragma unroll
             for (int pc = 0; pc < PIECES; ++pc) {
               const uint4 v = x[h][pc][wd];
               const bool first = wd == 0 && pc == 0;
               float own[4];
               float(&to)[4] = PIECES > 1 && !first ? own : d[f][h];
-              if (first || PIECES > 1) mma16816_first(to, a & 0x000F000Fu, b & 0x000F000Fu, a8 & 0x000F000Fu, b8 & 0x000F000Fu, v.x, v.y);
-              else mma16816(to, a & 0x000F000Fu, b & 0x000F000Fu, a8 & 0x000F000Fu, b8 & 0x000F000Fu, v.x, v.y);
-              mma16816(to, a & 0x00F000F0u, b & 0x00F000F0u, a8 & 0x00F000F0u, b8 & 0x00F000F0u, v.z, v.w);
+              if (first || PIECES > 1) mma16816_first(to, a0[0], b0[0], a0[1], b0[1], v.x, v.y);
+              else mma16816(to, a0[0], b0[0], a0[1], b0[1], v.x, v.y);
+              mma16816(to, a1[0], b1[0], a1[1], b1[1], v.z, v.w);
               if (PIECES > 1 && !first) add4(d[f][h], own);
             }
           }
