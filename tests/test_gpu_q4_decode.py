@@ -106,3 +106,71 @@ def test_answers_in_four_bits(dtype, layout):
         # about six roundings of half a step a layer, added up like independent ones, under the 1e-2 (floats: 2e-3) of the
         # prefill's tests
         assert ((h - ref).norm(dim=-1) <= case.tol * ref.norm(dim=-1)).all(), ((h - ref).norm(dim=-1) / ref.norm(dim=-1))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_answers_over_moved_and_cut_pages(dtype):
+    """Answers go on over pages that a compaction moved, and one of them from where it was cut within a page that another
+    still holds: the same bits as before the move, and the values of the tokens that are left."""
+    import paper_2607_21604_b200 as akvs
+    L, nq, nkv, hd, T = 2, 8, 2, 128, 150
+    g = torch.Generator(device="cuda").manual_seed(17)
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda").to(dtype)  # noqa: E731
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    pool = akvs.PagePool(L, 30, nkv, hd)
+    first, context = pool.open(), pool.open()
+    pool.grow([first], 300)                            # the lowest pages; it leaves before the others do
+    pool.grow([context], T)
+    table, lens = pool.table([context])
+    for l in range(L):
+        akvs.op_pages_append(rnd(T, nkv, hd), rnd(T, nkv, hd), pool[l], table, lens, ints(0, T))
+
+    def step(seqs):
+        """A new token of each; its row of every layer."""
+        pool.grow(seqs)
+        table, lens = pool.table(seqs)
+        for l in range(L):
+            akvs.op_pages_append(rnd(len(seqs), nkv, hd), rnd(len(seqs), nkv, hd), pool[l], table, lens)
+
+    def attend(seqs, q):
+        table, lens = pool.table(seqs)
+        return [akvs.op_attention_pages(q[l], pool[l], table, lens, nkv) for l in range(L)]
+
+    def values(seq):
+        table, lens = pool.table([seq])
+        n, out = pool.length[seq], []
+        for l in range(L):
+            kv = [torch.empty((n, nkv, hd), device="cuda") for _ in range(2)]
+            akvs.op_pages_read(pool[l], table, lens, *kv, ints(0, n))
+            out.append(kv)
+        return out
+
+    answers = pool.fork(context, 3)
+    pool.close(context)
+    step(answers)
+    q = rnd(L, 3, nq, hd)
+    before, held = attend(answers, q), [values(s) for s in answers]
+    pool.close(first)
+    assert pool.compact() > 0
+    assert all(torch.equal(a, b) for x, y in zip(attend(answers, q), before) for a, b in zip(x, y))
+    step(answers)
+    for s, old in zip(answers, held):                  # the new token came behind what there was
+        assert all(torch.equal(a[:T + 1], b) for x, y in zip(values(s), old) for a, b in zip(x, y))
+    # a branch goes back to within the page that it shares with where it comes from
+    before, old = attend(answers, q), values(answers[0])
+    (branch,) = pool.fork(answers[0])
+    pool.cut(branch, T - 10)
+    assert pool.users[pool.pages[branch][-1]] == 2
+    step([branch])
+    assert all(torch.equal(a, b) for x, y in zip(attend(answers, q), before) for a, b in zip(x, y))
+    new = values(branch)
+    assert all(len(a) == T - 9 and torch.equal(a[:T - 10], b[:T - 10]) for x, y in zip(new, old) for a, b in zip(x, y))
+    got = attend([branch], q[:, :1])
+    for (o, lse), (k, v), x in zip(got, new, q[:, 0]):
+        k, v = (t.double().repeat_interleave(nq // nkv, 1) for t in (k, v))
+        s = torch.einsum("hd,thd->ht", x.double(), k) / math.sqrt(hd)
+        ref = torch.einsum("ht,thd->hd", s.softmax(-1), v)
+        # the output's rounding, and 2^-15 of the values it is a mean of, whose parts are below 4 times as large
+        tol = torch.finfo(dtype).eps / 2 * ref.abs() + 2.0 ** -15 * 4 * v.abs().amax() + 2.0 ** -25
+        assert ((o[0].double() - ref).abs() <= tol).all()
+        assert ((lse[0].double() - torch.logsumexp(s, -1)).abs() <= 2.0 ** -15).all()

@@ -849,3 +849,30 @@ def test_linear_float_is_exact_enough(akvs):
         ref, _ = linear_ref(akvs, x, w)
         err = (akvs.op_linear_q4(x, lw).double() - ref).square().mean().sqrt()
         assert err <= 2.0 ** -20 * ref.square().mean().sqrt(), M
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("nq,nkv", [(4, 2), (8, 2), (16, 1)])
+def test_attention_float_is_exact_enough(akvs, hd, nq, nkv):
+    """Root mean square errors of float rows, several a sequence: the bound of one row a sequence above."""
+    g = gen(hd + nq)
+    c = Cache(akvs, g, [2500, 700, 65], nkv, hd, F32)
+    off = [0, 7, 8, 40]
+    q = rnd(g, 40, nq, hd)
+    o, l = akvs.op_attention_pages(q, c.pool, c.table, c.len, nkv, ints(off))
+    ref, lse, mag, _ = attention_ref(c, q, off)
+    rms = lambda x: x.double().square().mean().sqrt()  # noqa: E731
+    assert rms(o - ref) <= 2.0 ** -20 * rms(mag)
+    assert rms(l - lse) <= 2.0 ** -20 * 8                  # scores and log-sum-exps are below 16 here
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("nq,nkv,hd", [(32, 8, 128), (8, 8, 64), (20, 4, 128)])
+def test_attention_questions(akvs, dt, nq, nkv, hd):
+    """Questions of 64 and 128 rows over a context, beside an answer's one row and a sequence that is no longer than its rows."""
+    g = gen(nq + hd)
+    for rows, lens in (([128], [1500]), ([64, 1, 100], [900, 333, 100]), ([65, 128], [65, 130])):
+        c = Cache(akvs, g, lens, nkv, hd, dt)
+        off = np.concatenate([[0], np.cumsum(rows)]).tolist()
+        q = rnd(g, off[-1], nq, hd, dt=dt, scale=1.5)
+        check_attention(akvs.op_attention_pages(q, c.pool, c.table, c.len, nkv, ints(off)), c, q, off)
