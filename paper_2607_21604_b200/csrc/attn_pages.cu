@@ -14,14 +14,17 @@
 // alone: c in the low bits of a 16-bit float is the subnormal c 2^-24 (float16, for K) or c 2^-133 (bfloat16, for
 // V), 4 bits higher it is 16 times that; both are exact in the tensor cores.  The powers of two go to the other
 // side: a row of q is scaled by a power of two so that its largest value lies in [2^14, 2^15), where float16 loses
-// nothing above 2^-39 of it; weights carry 2^100.
+// nothing above 2^-39 of it (odd values, which enter with a sixteenth: 2^-35); weights carry 2^100.
 // The tensor cores cut sums off below their last bit, so a long sum of codes, all of them positive, comes out low, and
 // the minima's term, which is as large, does not forgive that.  Odd tokens therefore enter with 15 - c (the complement,
 // in the AND's own instruction) and minus their weight, and 15 times the weight joins the minima's term: the sums stay
-// near zero (floats, 4000 tokens of about equal weight: 1.1e-5 off before).  For float rows the products of a piece are summed
-// by themselves and added in float, rounded instead of cut off (up to 11680 tokens: 0.9e-6 off instead of 2.6e-6, 4 % slower).
+// near zero (floats, 4000 tokens of about equal weight: 1.1e-5 off before).  The tensor cores also line products up by their
+// exponents, and the leading zeros of a subnormal are lost with it.  Float rows therefore take a code in higher bits (an AND and
+// a shift), and a piece's products are summed by themselves and added in float, rounded instead of cut off: root mean square
+// errors of up to 0.5e-6 of the output for up to 11680 tokens (1.4e-6 with the AND alone; 8 rows over 6000 tokens each 37.7 us
+// instead of 36.3).
 // A weight enters as a bfloat16 and the bfloat16 of what its rounding lost (2^-17 of itself; float rows: three of
-// them).  Up to 4 stacked rows (rows x query heads of a kv head) leave half of N free: there the columns 4 .. 7
+// them).  That is little beside the output's own rounding (float16: 7e-6 beside 2.1e-4).  Up to 4 stacked rows (rows x query heads of a kv head) leave half of N free: there the columns 4 .. 7
 // repeat the rows, and take the lost parts in the same product.
 //
 // Work: a CTA of 4 warps takes 16 of a page's 64 tokens per warp, straight from global memory into registers (the
@@ -91,6 +94,18 @@ __device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
   uint32_t y;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
+}
+// Eight codes of K as operands, for the values (0 4) (2 6) and (1 5) (3 7): an AND alone, c 2^-24 and 16 c 2^-24; for float rows
+// (TOP) in the highest bits that a subnormal has, 64 c 2^-24.
+template <bool TOP> __device__ __forceinline__ void keys(uint32_t w, uint32_t (&first)[2], uint32_t (&second)[2]) {
+  if constexpr (TOP) {
+    first[0] = w << 6 & 0x03C003C0u; first[1] = w >> 2 & 0x03C003C0u;
+    second[0] = w << 2 & 0x03C003C0u; second[1] = w >> 6 & 0x03C003C0u;
+  } else {
+    const uint32_t w8 = w >> 8;
+    first[0] = w & 0x000F000Fu; first[1] = w8 & 0x000F000Fu;
+    second[0] = w & 0x00F000F0u; second[1] = w8 & 0x00F000F0u;
+  }
 }
 __device__ __forceinline__ float2 twice(float x) { return make_float2(x, x); }
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) { return __fmul2_rn(a, b); }
@@ -188,7 +203,7 @@ template <typename T, int HD, int TR> struct RowTile {
         for (int w = 0; w < 2; ++w) {
           float y[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = f[g][8 * w + e] * mul * ((e & 1) ? 0.0625f : 1.f);
+          for (int e = 0; e < 8; ++e) y[e] = f[g][8 * w + e] * mul * (PIECES == 1 && (e & 1) ? 0.0625f : 1.f);
 #pragma unroll
           for (int pc = 0; pc < PIECES; ++pc)
 #pragma unroll
@@ -207,7 +222,7 @@ template <typename T, int HD, int TR> struct RowTile {
         const int m = PAIR ? (2 * t + e) & 3 : 2 * t + e, from = 4 * m;
         const int ju = j0 + 8 * x + m;
         lim[x][e] = ju < count ? min(sq.len, max(0, sq.len - (sq.n - 1 - ju / p.g))) : sq.len;
-        rfe[e] = __shfl_sync(0xFFFFFFFFu, __uint_as_float((uint32_t)(127 - up) << 23), from) * p.scale_log2 * 0x1p24f;
+        rfe[e] = __shfl_sync(0xFFFFFFFFu, __uint_as_float((uint32_t)(127 - up) << 23), from) * p.scale_log2 * (PIECES > 1 ? 0x1p18f : 0x1p24f);
 #pragma unroll
         for (int g = 0; g < G; ++g) qse[e][g] = __shfl_sync(0xFFFFFFFFu, s[g], from) * p.scale_log2;
       }
@@ -249,7 +264,9 @@ template <typename T, int HD, int TR> struct RowTile {
         for (int g = 0; g < G; ++g)
 #pragma unroll
           for (int n = 0; n < NP; ++n) {
-            const uint32_t a = st[n].k[0][2 * g + w], b = st[n].k[1][2 * g + w], a8 = a >> 8, b8 = b >> 8;
+            uint32_t a0[2], a1[2], b0[2], b1[2];
+            keys<(PIECES > 1)>(st[n].k[0][2 * g + w], a0, a1);
+            keys<(PIECES > 1)>(st[n].k[1][2 * g + w], b0, b1);
 #pragma unroll
             for (int x = 0; x < NT; ++x)
 #pragma unroll
@@ -257,8 +274,8 @@ template <typename T, int HD, int TR> struct RowTile {
                 const uint32_t(&q)[4] = qb[x][pc][g][w];
                 float own[4] = {0.f, 0.f, 0.f, 0.f};
                 float(&to)[4] = PIECES > 1 ? own : d[n][x][g];
-                mma16816<f16>(to, a & 0x000F000Fu, b & 0x000F000Fu, a8 & 0x000F000Fu, b8 & 0x000F000Fu, q[0], q[1]);
-                mma16816<f16>(to, a & 0x00F000F0u, b & 0x00F000F0u, a8 & 0x00F000F0u, b8 & 0x00F000F0u, q[2], q[3]);
+                mma16816<f16>(to, a0[0], b0[0], a0[1], b0[1], q[0], q[1]);
+                mma16816<f16>(to, a1[0], b1[0], a1[1], b1[1], q[2], q[3]);
                 if constexpr (PIECES > 1) add4(d[n][x][g], own);
               }
           }
@@ -374,8 +391,8 @@ template <typename T, int HD, int TR> struct RowTile {
           }
         }
       }
-    // the upper halves hold odd tokens
-    auto lo = [](uint32_t w) { return (w & 0x000F000Fu) ^ 0x000F0000u; };
+    // the upper halves hold odd tokens; float rows have all codes 4 bits up
+    auto lo = [](uint32_t w) { return PIECES > 1 ? (w << 4 & 0x00F000F0u) ^ 0x00F00000u : (w & 0x000F000Fu) ^ 0x000F0000u; };
     auto hi4 = [](uint32_t w) { return (w & 0x00F000F0u) ^ 0x00F00000u; };
 #pragma unroll
     for (int n = 0; n < NP; ++n)
@@ -425,7 +442,7 @@ template <typename T, int HD, int TR> struct RowTile {
           for (int e = 0; e < 4; ++e) {
             float y = o[x][g][j][e];
             if constexpr (PAIR) y += __shfl_xor_sync(0xFFFFFFFFu, y, 2);
-            o[x][g][j][e] = fmaf(y, e & 2 ? 0x1p29f : 0x1p33f, e & 1 ? om[x][g].y : om[x][g].x);
+            o[x][g][j][e] = fmaf(y, PIECES > 1 || (e & 2) ? 0x1p29f : 0x1p33f, e & 1 ? om[x][g].y : om[x][g].x);
           }
     }
   }

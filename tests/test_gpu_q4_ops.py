@@ -876,3 +876,20 @@ def test_attention_questions(akvs, dt, nq, nkv, hd):
         off = np.concatenate([[0], np.cumsum(rows)]).tolist()
         q = rnd(g, off[-1], nq, hd, dt=dt, scale=1.5)
         check_attention(akvs.op_attention_pages(q, c.pool, c.table, c.len, nkv, ints(off)), c, q, off)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("nq,nkv", [(2, 2), (8, 1), (4, 2)])
+def test_attention_float_against_its_output(akvs, hd, nq, nkv):
+    """Root mean square error of float rows against the output, which is a mean of thousands of values and smaller than they
+    are.  Terms and output both grow with the root of the number of tokens, so they are compared a token: a product's sum over 16
+    tokens is cut off by up to 2^-23 of itself, whose codes (8.2 steps with the complements) stand beside values of 3.3 steps:
+    3e-7; the additions of such sums, 20 a CTA, 1.5e-7; exp2, 2^-22 of a weight, 1.4e-7; scores, of 2^-22 at most, as much.
+    Independent, these are under 5e-7, and together at worst under 2^-20."""
+    g = gen(hd + nq)
+    lens = [5556, 2000, 1200]
+    c = Cache(akvs, g, lens, nkv, hd, F32)
+    q = rnd(g, 3, nq, hd, scale=1.5)
+    o, _ = akvs.op_attention_pages(q, c.pool, c.table, c.len, nkv)
+    ref, _, _, _ = attention_ref(c, q, [0, 1, 2, 3])
+    assert (o - ref).square().mean().sqrt() <= 2.0 ** -20 * ref.square().mean().sqrt()
