@@ -627,12 +627,11 @@ template <typename T, int NT>
 int32_t launch(const LinearQ4Params& p0, cudaStream_t st) {
   LinearQ4Params p = p0;
   const int tiles = akvs_cdiv(p.N, LQ_F), blocks = akvs_cdiv(p.M, 8 * NT);
-  // Ranges of columns, 512 of them or more each: as many as let every CTA run at once, two on an SM.
   using S = LqSmem<NT, sizeof(T) == 4 ? 3 : 1>;
   static std::atomic<uint64_t> smem_set{0};
   AKVS_CUDA(smem_opt_in((const void*)linear_q4_kernel<T, NT>, S::BYTES, smem_set));
-  int splits = 1;
-  while (splits < 8 && (int64_t)tiles * blocks * splits * 2 <= 2 * 148 && akvs_cdiv(p.groups, splits * 2) >= XG) splits *= 2;
+  static_assert(XG == 8, "ranges of 512 columns");
+  int splits = lq_cluster_ranges((int64_t)tiles * blocks, p.groups, sizeof(T) == 4 ? LQ_FIT_ONE : LQ_FIT_TWO);
   p.groups_per_split = akvs_cdiv(akvs_cdiv(p.groups, splits), XG) * XG;
   splits = akvs_cdiv(p.groups, p.groups_per_split);
   cudaLaunchConfig_t cfg = {};
@@ -1224,14 +1223,13 @@ int32_t launch_tc(const LinearQ4Params& l, void* scratch, cudaStream_t st) {
 }
 
 // Which kernel.  Few rows: one CTA per SM while x fits into its shared memory.  tcgen05: from 17 rows on; its start (x in
-// order, tensor memory, the cluster's sum) costs some 10 us, but a step less than the clusters', so from 112 M weights on it
-// also takes fewer rows that the first kernel does not (9 rows: 28672 x 4096 27.2 us against 30.2 us, 5120 x 27648 32.6
-// against 48.8 us, but 14336 x 4096 17.5 against 17.2).
+// order, tensor memory, the cluster's sum) costs some 10 us, but a step less than the clusters' where these have more columns than
+// their SMs can share, so it also takes fewer rows there.
 enum class Path { few, clusters, tc };
 Path path_of(int dtype, int M, int N, int K) {
   const int pairs = (K / 64 + 1) / 2;
   if (M <= 8 && few_smem(1, M, pairs, dtype == AKVS_F32 ? 3 : 1) <= FW_MAX_SMEM) return Path::few;
-  if (dtype != AKVS_F32 && (M > 16 || (int64_t)N * K >= 112ll << 20)) return Path::tc;
+  if (dtype != AKVS_F32 && (M > 16 || lq_prefers_tensor(M, N, K / 64))) return Path::tc;
   return Path::clusters;
 }
 
