@@ -21,11 +21,12 @@
 // near zero (floats, 4000 tokens of about equal weight: 1.1e-5 off before).  The tensor cores also line products up by their
 // exponents, and the leading zeros of a subnormal are lost with it.  Float rows therefore take a code in higher bits (an AND and
 // a shift), and a piece's products are summed by themselves and added in float, rounded instead of cut off: root mean square
-// errors of up to 0.5e-6 of the output for up to 11680 tokens (1.4e-6 with the AND alone; 8 rows over 6000 tokens each 37.7 us
-// instead of 36.3).
+// errors of up to 0.5e-6 of the output for up to 11680 tokens (1.4e-6 with the AND alone, and 4 % faster; 8 rows of 32 / 8 heads
+// over 6000 tokens each: 31 us).
 // A weight enters as a bfloat16 and the bfloat16 of what its rounding lost (2^-17 of itself; float rows: three of
-// them).  That is little beside the output's own rounding (float16: 7e-6 beside 2.1e-4).  Up to 4 stacked rows (rows x query heads of a kv head) leave half of N free: there the columns 4 .. 7
-// repeat the rows, and take the lost parts in the same product.
+// them).  That is little beside the output's own rounding (float16: 7e-6 beside 2.1e-4).  Up to 4 stacked rows (rows x query
+// heads of a kv head) leave half of N free: there the columns 4 .. 7 repeat the rows, and take the lost parts in the same
+// product.
 //
 // Work: a CTA of 4 warps takes 16 of a page's 64 tokens per warp, straight from global memory into registers (the
 // page's layout is that of the fragments), one page ahead, the pages after it on their way to L2.  All
@@ -35,6 +36,9 @@
 // 64 rows of 40 / 8 heads over 500 to 12416 tokens each (490 MB): 137 us, 3.6 TB/s of 6.56.  Not memory but the issue slots
 // (half of them taken) and the chains between products bound it: AND, shift and scale around every product of a few
 // rows.  One page at a time with 16 warps an SM, 1, 3, 4 and 6 pages between a load and its request, 2 and 4 CTAs an SM: 137 to 172.
+// Tiles of 16 rows and float rows leave room for 2 CTAs an SM, and the list is cut for as many (16 sequences of 8 rows over 6000
+// tokens each, 32 / 8 heads: 120 us cut for three, 95 so).  A tile reads all of its pages, so a question of 128 rows over 12000 tokens
+// takes 163 us; its 16-bit values read out and given to the shared attention take 56.
 // One row of 32 / 8 heads over 8576 tokens: 12.2 us, of which 9 are a chain of loads (length, page numbers, pages), a step or two
 // and the four warps' join, and 3 the second kernel.
 #include "pages.cuh"
@@ -44,7 +48,8 @@
 namespace {
 
 constexpr int PA_WARPS = 4, PA_THREADS = PA_WARPS * 32;
-constexpr int PA_CTAS = 148 * 3;                      // of all kv heads: what the SMs hold at a time
+constexpr int PA_CTAS = 148;                          // of all kv heads, times the CTAs that an SM holds
+constexpr int ctas_of_an_sm(int TR, int type_size) { return TR == 16 || type_size == 4 ? 2 : 3; }
 constexpr int AHEAD = 2;                              // pages between a load and the request that brings its page to L2
 constexpr float NO_MAX = -FLT_MAX;                    // reference before any key: exp2(-inf - NO_MAX) = 0
 constexpr float LN2 = 0.69314718f, LOG2E = 1.4426950408889634f;
@@ -574,7 +579,7 @@ __device__ __forceinline__ int64_t units_per_worker(int64_t total, int workers) 
 
 // grid (workers, kv heads)
 template <typename T, int HD, int TR>
-__global__ void __launch_bounds__(PA_THREADS, TR == 16 || sizeof(T) == 4 ? 2 : 3)
+__global__ void __launch_bounds__(PA_THREADS, ctas_of_an_sm(TR, sizeof(T)))
 attention_pages_kernel(const __grid_constant__ PagesParams p) {
   extern __shared__ __align__(16) float raw[];
   __shared__ int64_t sums[PA_WARPS], rest[PA_WARPS], start_unit, start_tile;
@@ -762,10 +767,10 @@ int tile_rows(int dtype, int R, int S, int g, bool ragged) {
   const int64_t stacked = ragged ? (int64_t)akvs_cdiv(R, S) * g : g;
   return stacked <= 4 ? 4 : stacked <= 8 ? 8 : 16;
 }
-int workers_of(int n_kv) { return n_kv >= PA_CTAS ? 1 : PA_CTAS / n_kv; }
+int workers_of(int n_kv, int per_sm) { return n_kv >= PA_CTAS * per_sm ? 1 : PA_CTAS * per_sm / n_kv; }
 // Slots x rows of a slot: a stretch per CTA and one more per tile that it ends in; at most this for any tile
 // size, so that the size grows with R and S.
-int64_t slot_rows(int R, int S, int n_kv, int g) { return (int64_t)(workers_of(n_kv) + S) * 16 + (int64_t)R * g; }
+int64_t slot_rows(int R, int S, int n_kv, int g) { return (int64_t)(workers_of(n_kv, 3) + S) * 16 + (int64_t)R * g; }
 int64_t scratch_need(int R, int S, int n_kv, int g, int hd) {
   const int64_t rows = slot_rows(R, S, n_kv, g) * n_kv;
   return akvs_align_up(rows * hd * 4, 256) + akvs_align_up(rows * 8, 256) + akvs_align_up(S * 16ll, 256) + 256;
@@ -839,8 +844,8 @@ extern "C" int32_t akvs_op_attention_pages(int32_t dtype, const void* q, int64_t
   p.part_o = reinterpret_cast<float*>(at);
   p.part_ml = reinterpret_cast<float2*>(at + akvs_align_up(rows * head_dim * 4, 256));
   p.plan = reinterpret_cast<longlong2*>(at + akvs_align_up(rows * head_dim * 4, 256) + akvs_align_up(rows * 8, 256));
-  p.workers = workers_of(n_kv_heads);
   const int tr = tile_rows(dtype, used, S, g, q_off != nullptr);
+  p.workers = workers_of(n_kv_heads, ctas_of_an_sm(tr, (int)es));
   p.slots = slot_rows(used, S, n_kv_heads, g) / tr;
   p.scale_log2 = LOG2E / sqrtf((float)head_dim);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
