@@ -518,7 +518,8 @@ int32_t akvs_op_linear_q4_pack(const void* codes, const void* meta, int32_t N, i
 
 /* y [M][N] = x [M][K] W^T, x rows x_ld apart, y contiguous of dtype; or h_out = h + x W^T, float [M][N], contiguous, h_out may
  * be h.  A weight is code * scale + minimum, unrounded; sums are float, in a fixed order (equal calls give equal bits).  A
- * row of x with an infinity, a NaN or a value of 2^117 and more gives NaN or infinities; a finite float16 result beyond the type's end saturates.
+ * row of x with an infinity or a NaN gives NaN or infinities, and so may one with a value of 2^117 and more; a finite float16 result
+ * beyond the type's end saturates.
  * Made for the rows of a decoding step; any M is allowed.
  * scratch: device, 256-byte aligned, akvs_op_linear_q4_scratch_bytes(...) bytes (else AKVS_ERR_WORKSPACE; NULL where that is 0); two
  * calls that may overlap on the GPU need two.  The size never shrinks when M or K grows; -1 for arguments that the calls refuse. */

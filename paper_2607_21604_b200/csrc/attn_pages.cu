@@ -10,19 +10,19 @@
 //
 // Memory bound: 144 bytes a token and kv head (head_dim 128) for the g query heads that share it, so a warp has
 // few rows and many codes.  Products are mma.sync m16n8k16 with the ROWS along N (S^T = K Q^T: 16 keys x 8 rows,
-// O^T += V^T P^T: 16 columns x 8 rows x 16 keys; P^T turned by movmatrix).  A code becomes an operand by an AND
-// alone: c in the low bits of a 16-bit float is the subnormal c 2^-24 (float16, for K) or c 2^-133 (bfloat16, for
-// V), 4 bits higher it is 16 times that; both are exact in the tensor cores.  The powers of two go to the other
-// side: a row of q is scaled by a power of two so that its largest value lies in [2^14, 2^15), where float16 loses
-// nothing above 2^-39 of it (odd values, which enter with a sixteenth: 2^-35); weights carry 2^100.
+// O^T += V^T P^T: 16 columns x 8 rows x 16 keys; P^T turned by movmatrix).  A code becomes an operand by an AND and half a
+// shift, as a float16 c 2^-21 or 16 c 2^-21 (K), or by an AND alone as a bfloat16 c 2^-133 or 16 c 2^-133 (V); all are exact in the
+// tensor cores.  The powers of two go to the other side: a row of q is scaled by a power of two so that its largest value lies in
+// [2^14, 2^15), where float16 loses nothing above 2^-39 of it (odd values, which enter with a sixteenth: 2^-35); weights carry
+// 2^100.
 // The tensor cores cut sums off below their last bit, so a long sum of codes, all of them positive, comes out low, and
 // the minima's term, which is as large, does not forgive that.  Odd tokens therefore enter with 15 - c (the complement,
 // in the AND's own instruction) and minus their weight, and 15 times the weight joins the minima's term: the sums stay
-// near zero (floats, 4000 tokens of about equal weight: 1.1e-5 off before).  The tensor cores also line products up by their
-// exponents, and the leading zeros of a subnormal are lost with it.  Float rows therefore take a code in higher bits (an AND and
-// a shift), and a piece's products are summed by themselves and added in float, rounded instead of cut off: root mean square
-// errors of up to 0.5e-6 of the output for up to 11680 tokens (1.4e-6 with the AND alone, and 4 % faster; 8 rows of 32 / 8 heads
-// over 6000 tokens each: 31 us).
+// near zero (floats, 4000 tokens of about equal weight: 1.1e-5 off before).  They also line products up by their exponents, and the
+// leading zeros of a subnormal are lost with it; so K's codes are not taken as an AND leaves them (scores of few float16 rows
+// were 1e-6 off), nor V's for float rows (16 c 2^-133 throughout).  For float rows a piece's products are summed by themselves and
+// added in float, rounded instead of cut off: root mean square errors of up to 0.6e-6 of the output for up to 11680 tokens
+// (1.4e-6 with the AND alone).  8 float rows of 32 / 8 heads over 6000 tokens each: 30 us.
 // A weight enters as a bfloat16 and the bfloat16 of what its rounding lost (2^-17 of itself; float rows: three of
 // them).  That is little beside the output's own rounding (float16: 7e-6 beside 2.1e-4).  Up to 4 stacked rows (rows x query
 // heads of a kv head) leave half of N free: there the columns 4 .. 7 repeat the rows, and take the lost parts in the same
@@ -99,18 +99,6 @@ __device__ __forceinline__ uint32_t turn8x8(uint32_t x) {
   uint32_t y;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
-}
-// Eight codes of K as operands, for the values (0 4) (2 6) and (1 5) (3 7): an AND alone, c 2^-24 and 16 c 2^-24; for float rows
-// (TOP) in the highest bits that a subnormal has, 64 c 2^-24.
-template <bool TOP> __device__ __forceinline__ void keys(uint32_t w, uint32_t (&first)[2], uint32_t (&second)[2]) {
-  if constexpr (TOP) {
-    first[0] = w << 6 & 0x03C003C0u; first[1] = w >> 2 & 0x03C003C0u;
-    second[0] = w << 2 & 0x03C003C0u; second[1] = w >> 6 & 0x03C003C0u;
-  } else {
-    const uint32_t w8 = w >> 8;
-    first[0] = w & 0x000F000Fu; first[1] = w8 & 0x000F000Fu;
-    second[0] = w & 0x00F000F0u; second[1] = w8 & 0x00F000F0u;
-  }
 }
 __device__ __forceinline__ float2 twice(float x) { return make_float2(x, x); }
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) { return __fmul2_rn(a, b); }
@@ -208,7 +196,7 @@ template <typename T, int HD, int TR> struct RowTile {
         for (int w = 0; w < 2; ++w) {
           float y[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = f[g][8 * w + e] * mul * (PIECES == 1 && (e & 1) ? 0.0625f : 1.f);
+          for (int e = 0; e < 8; ++e) y[e] = f[g][8 * w + e] * mul * (e & 1 ? CODE_ODD : 1.f);
 #pragma unroll
           for (int pc = 0; pc < PIECES; ++pc)
 #pragma unroll
@@ -227,7 +215,7 @@ template <typename T, int HD, int TR> struct RowTile {
         const int m = PAIR ? (2 * t + e) & 3 : 2 * t + e, from = 4 * m;
         const int ju = j0 + 8 * x + m;
         lim[x][e] = ju < count ? min(sq.len, max(0, sq.len - (sq.n - 1 - ju / p.g))) : sq.len;
-        rfe[e] = __shfl_sync(0xFFFFFFFFu, __uint_as_float((uint32_t)(127 - up) << 23), from) * p.scale_log2 * (PIECES > 1 ? 0x1p18f : 0x1p24f);
+        rfe[e] = __shfl_sync(0xFFFFFFFFu, __uint_as_float((uint32_t)(127 - up) << 23), from) * p.scale_log2 * CODE_BACK;
 #pragma unroll
         for (int g = 0; g < G; ++g) qse[e][g] = __shfl_sync(0xFFFFFFFFu, s[g], from) * p.scale_log2;
       }
@@ -270,8 +258,8 @@ template <typename T, int HD, int TR> struct RowTile {
 #pragma unroll
           for (int n = 0; n < NP; ++n) {
             uint32_t a0[2], a1[2], b0[2], b1[2];
-            keys<(PIECES > 1)>(st[n].k[0][2 * g + w], a0, a1);
-            keys<(PIECES > 1)>(st[n].k[1][2 * g + w], b0, b1);
+            code_operands(st[n].k[0][2 * g + w], a0, a1);
+            code_operands(st[n].k[1][2 * g + w], b0, b1);
 #pragma unroll
             for (int x = 0; x < NT; ++x)
 #pragma unroll

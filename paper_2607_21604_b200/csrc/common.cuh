@@ -199,6 +199,17 @@ template <typename T> __device__ __forceinline__ void st16_inf(T* p, const float
   st16(p, o);
 }
 
+// Eight 4-bit codes of a word as float16 operands, for the values (0 4) (2 6) and (1 5) (3 7): c 2^-21, and for the latter 16 c 2^-21,
+// whose partners enter with a sixteenth; all are exact.  An AND alone would give the subnormals c 2^-24, but the tensor cores
+// line products up by their exponents before they cut off what lies below the last bit of a sum, and a subnormal's leading
+// zeros are lost with it: 3 bits further up is as far as both go.
+constexpr float CODE_BACK = 0x1p21f, CODE_ODD = 0.0625f;      // of a product; factor of the latter's partners
+__device__ __forceinline__ void code_operands(uint32_t w, uint32_t (&first)[2], uint32_t (&second)[2]) {
+  const uint32_t lo = w << 3, hi = w >> 5;
+  first[0] = lo & 0x00780078u; first[1] = hi & 0x00780078u;
+  second[0] = lo & 0x07800780u; second[1] = hi & 0x07800780u;
+}
+
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);

@@ -1,15 +1,13 @@
 // Linear layers with 4-bit weights for the few rows of a decoding step: y = x W^T,
 //     w_nk = c_nk scale_ng + min_ng,  g = k / 64;     y_n = sum_g scale_ng (c_ng . x_g) + min_ng sum(x_g).
-// Memory bound by the weights (36 bytes per 64 of them) while the rows are few.  A code becomes an operand of a product by
-// an AND alone: in the low bits of a float16 it is the subnormal c 2^-24, 4 bits higher 16 times that, both exact in the
-// tensor cores; x is scaled by the power of two that brings the largest value of a row and range of columns to [2^14,
-// 2^15), where float16 loses nothing above 2^-39 of it (odd columns, which enter with a sixteenth: 2^-35).  A group's products are
-// summed by themselves and scaled in float, so that weights are what their codes and records say and nothing is rounded but sums.
-// Float rows enter as three float16 pieces, which hold all 24 bits of a value down to 2^-15 of the largest and lose what lies
-// below 2^-39 of that.  A piece's products are summed by themselves and added in float, and codes take the highest bits that a
-// subnormal has (an AND and a shift): the tensor cores line products up by their exponents before they cut sums off, and a
-// subnormal's leading zeros are lost with it (root mean square errors of up to 1.3e-6 of y with the AND alone, up to 0.5e-6 so,
-// at the same speed; the 8 or 11 bits of 16-bit rows: 0.4e-6).
+// Memory bound by the weights (36 bytes per 64 of them) while the rows are few.  A code becomes an operand of a product by an AND
+// and half a shift, as a float16 of few bits that is exact in the tensor cores (code_operands); x is scaled by the power of two
+// that brings the largest value of a row and range of columns to [2^14, 2^15), where float16 loses nothing above 2^-39 of it (odd
+// columns, which enter with a sixteenth: 2^-35).  A group's products are summed by themselves and scaled in float, so that weights
+// are what their codes and records say and nothing is rounded but sums.  Float rows enter as three float16 pieces, which hold all 24
+// bits of a value down to 2^-15 of the largest (odd columns: 2^-11); a piece's products are summed by themselves and added in float.
+// Root mean square errors of float results are up to 0.2e-6 of y for 16-bit rows and 0.5e-6 for float rows (with codes as an AND
+// leaves them, up to 1.4e-6 for float16 and float rows, and 0.5e-6 for bfloat16; 8 rows of 14336 x 4096 12.1 instead of 12.4 us).
 //
 // Weights are laid out once (akvs_op_linear_q4_pack): blocks of 16 features x 2 groups, 1152 bytes; those of 256 features
 // side by side, and so on along the columns, so that every kernel reads long pieces.  A feature's 64 bytes of codes are
@@ -79,18 +77,6 @@ __device__ __forceinline__ void bulk_copy(void* dst, const void* src, uint32_t b
 __device__ __forceinline__ void add4(float (&d)[4], const float (&x)[4]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) d[e] += x[e];
-}
-// Eight codes as operands, for the values (0 4) (2 6) and (1 5) (3 7).  16-bit rows: an AND alone, c 2^-24 and 16 c 2^-24.  Float
-// rows (TOP): in the highest bits that a subnormal has, 64 c 2^-24.
-template <bool TOP> __device__ __forceinline__ void operands(uint32_t w, uint32_t (&first)[2], uint32_t (&second)[2]) {
-  if constexpr (TOP) {
-    first[0] = (w << 6) & 0x03C003C0u; first[1] = (w >> 2) & 0x03C003C0u;
-    second[0] = (w << 2) & 0x03C003C0u; second[1] = (w >> 6) & 0x03C003C0u;
-  } else {
-    const uint32_t w8 = w >> 8;
-    first[0] = w & 0x000F000Fu; first[1] = w8 & 0x000F000Fu;
-    second[0] = w & 0x00F000F0u; second[1] = w8 & 0x00F000F0u;
-  }
 }
 // the same with nothing to add to
 __device__ __forceinline__ void mma16816_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -212,7 +198,7 @@ linear_q4_kernel(const __grid_constant__ LinearQ4Params p) {
       for (int wd = 0; wd < 2; ++wd) {
         float y[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = f[8 * wd + e] * (PIECES == 1 && (e & 1) ? 0.0625f : 1.f);
+        for (int e = 0; e < 8; ++e) y[e] = f[8 * wd + e] * (e & 1 ? CODE_ODD : 1.f);
 #pragma unroll
         for (int pc = 0; pc < PIECES; ++pc) {
           uint32_t q[4];
@@ -290,8 +276,8 @@ linear_q4_kernel(const __grid_constant__ LinearQ4Params p) {
 #pragma unroll
         for (int wd = 0; wd < 2; ++wd) {
           uint32_t a0[2], a1[2], b0[2], b1[2];
-          operands<(PIECES > 1)>(wa[wd], a0, a1);
-          operands<(PIECES > 1)>(wb2[wd], b0, b1);
+          code_operands(wa[wd], a0, a1);
+          code_operands(wb2[wd], b0, b1);
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -317,7 +303,7 @@ linear_q4_kernel(const __grid_constant__ LinearQ4Params p) {
         const float2 pw = *reinterpret_cast<const float2*>(xb + S::X + S::XM + (8 * n + 2 * t) * 4);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          acc[n][e] = fmaf(fmaf(sum[n][e], PIECES > 1 ? 0x1p18f : 0x1p24f, low[n][e] * 0x1p6f), e & 1 ? pw.y : pw.x, acc[n][e]);
+          acc[n][e] = fmaf(fmaf(sum[n][e], CODE_BACK, low[n][e] * 0x1p6f), e & 1 ? pw.y : pw.x, acc[n][e]);
       }
     }
     if (c + 1 < chunks) convert_x(c + 1);
@@ -464,11 +450,11 @@ linear_q4_few_kernel(const __grid_constant__ LinearQ4Params p) {
       }
       int up = 141 - (int)(__float_as_uint(top) >> 23);               // brings the largest value to [2^14, 2^15)
       up = top == 0.f || !(top < INFINITY) ? 0 : min(up, 126);
-      const float even = __uint_as_float((uint32_t)(up + 127) << 23), odd = PIECES > 1 ? even : even * 0.0625f;
+      const float even = __uint_as_float((uint32_t)(up + 127) << 23), odd = even * CODE_ODD;
       if (i >= all) continue;
       if (tt == 0) xsum[g * 8 + r] = s;
-      // 2^24 for the codes beside it.  (x beyond 2^117 leaves the floats here, and the row becomes infinities or NaN.)
-      if ((u & 7) == 0) xpow[(u >> 3) * 8 + r] = __uint_as_float((uint32_t)(127 - up) << 23) * (PIECES > 1 ? 0x1p18f : 0x1p24f);
+      // 2^21 for the codes beside it.  (x beyond 2^120 leaves the floats here, and the row becomes infinities or NaN.)
+      if ((u & 7) == 0) xpow[(u >> 3) * 8 + r] = __uint_as_float((uint32_t)(127 - up) << 23) * CODE_BACK;
 #pragma unroll
       for (int wd = 0; wd < 2; ++wd) {
         float y[8];
@@ -537,8 +523,8 @@ linear_q4_few_kernel(const __grid_constant__ LinearQ4Params p) {
 #pragma unroll
           for (int wd = 0; wd < 2; ++wd) {
             uint32_t a0[2], a1[2], b0[2], b1[2];
-            operands<(PIECES > 1)>(h ? (wd ? ca.w : ca.z) : (wd ? ca.y : ca.x), a0, a1);
-            operands<(PIECES > 1)>(h ? (wd ? cb.w : cb.z) : (wd ? cb.y : cb.x), b0, b1);
+            code_operands(h ? (wd ? ca.w : ca.z) : (wd ? ca.y : ca.x), a0, a1);
+            code_operands(h ? (wd ? cb.w : cb.z) : (wd ? cb.y : cb.x), b0, b1);
 #pragma unroll
             for (int pc = 0; pc < PIECES; ++pc) {
               const uint4 v = x[h][pc][wd];
@@ -657,7 +643,7 @@ int32_t launch(const LinearQ4Params& p0, cudaStream_t st) {
 // rows, a group of 64 columns a step:
 //     D[feature][row] = codes[feature][64] x[row][64]        A in tensor memory, B in shared memory, D in tensor memory
 //     acc[feature][row] += scale[feature] D                  a thread per feature, NB sums in registers
-// Warps of their own turn codes into operands (one AND each, stored to tensor memory, four steps ahead), issue products and
+// Warps of their own turn codes into operands (code_operands, stored to tensor memory, four steps ahead), issue products and
 // add them up.  The minima are a product too: 32 groups' minima
 // (float16, as they are) against 32 sums of x, each as two float16, make a step of the same form, two steps a stage.
 // x is brought into operand order once per call by a kernel of its own (scale of a row, permuted columns, the 128-byte
@@ -744,7 +730,7 @@ linear_q4_rows_kernel(const T* x, int64_t x_ld, int M, int rows_per_block, int g
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int lo = (i & 1) * 2 + (i >> 1);          // (0 4) (2 6) (1 5)/16 (3 7)/16
-      const float k = i < 2 ? 1.f : 0.0625f;
+      const float k = i < 2 ? 1.f : CODE_ODD;
       const __half2 hh = __floats2half2_rn(f[lo] * k, f[lo + 4] * k);
       q[i] = *reinterpret_cast<const uint32_t*>(&hh);
     }
@@ -1000,11 +986,11 @@ linear_q4_tc_kernel(const __grid_constant__ TcParams p) {
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
-          const uint32_t x = h == 0 ? (w ? k.c[t].y : k.c[t].x) : (w ? k.c[t].w : k.c[t].z), x8 = x >> 8;
-          uint32_t* at = a + (2 * t + w) * 4;
-          at[0] = x & 0x000F000Fu; at[1] = x8 & 0x000F000Fu; at[2] = x & 0x00F000F0u; at[3] = x8 & 0x00F000F0u;
+          uint32_t first[2], second[2], *at = a + (2 * t + w) * 4;
+          code_operands(h == 0 ? (w ? k.c[t].y : k.c[t].x) : (w ? k.c[t].w : k.c[t].z), first, second);
+          at[0] = first[0]; at[1] = first[1]; at[2] = second[0]; at[3] = second[1];
         }
-      put(a, __half2float(__ushort_as_half((unsigned short)((h == 0 ? k.r.x : k.r.y) & 0xFFFFu))) * 0x1p24f, h);
+      put(a, __half2float(__ushort_as_half((unsigned short)((h == 0 ? k.r.x : k.r.y) & 0xFFFFu))) * CODE_BACK, h);
     };
     // A pair's stage; `next` is read on the way.  The window of 64 groups' minima is this thread's own.
     auto pair = [&](const Codes& k, Codes& next, int pr) {
@@ -1274,7 +1260,7 @@ int32_t linear(int32_t dtype, const void* x, int64_t x_ld, const void* w, int64_
     const Path path = path_of(dtype, M, N, K);
     if (path == Path::few) {
       // As few rounds of teams as there can be: 16 warps share the columns where an SM has one tile, 8 up to two, 4 beyond
-      // (8 rows of 55296 x 5120: 41 us, with one team of 16 56).  Two tiles at a time read x half as often, where teams of
+      // (8 rows of 55296 x 5120: 39 us, with one team of 16 56).  Two tiles at a time read x half as often, where teams of
       // four have more than one round and x leaves the room (one row of 11008 x 2048: 5.6 us, with one tile 6.2).
       const int tiles = akvs_cdiv(N, 16);
       p.team = tiles <= 148 ? 16 : tiles <= 2 * 148 ? 8 : 4;
