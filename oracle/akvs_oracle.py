@@ -30,12 +30,14 @@ ratio in integer basis points.
   the paper naming only the formats.
 * Section 3.4 and the appendix on mean-explained residual energy: `residual_stats`.
 
-Run-time plumbing that changes no arithmetic: `ATTENTION_WORKERS` > 1 computes the query
-heads of one attention call in that many threads (each head is the same sequence of numpy
-calls on the same data, with products of one thread each where threadpoolctl is there: 16 heads
-whose products each start 16 threads take three times as long); `Model.w` converts a layer's weights to the working precision once
-and keeps the last layer converted, and `encode_units` walks layer by layer over all units so
-that this happens once per layer.
+Run-time plumbing: attention leaves out keys that no row of a block sees, whose weights are zeros; the
+sums without them may differ in their last bits (4e-16).  What follows changes no arithmetic.
+`ATTENTION_WORKERS` > 1 computes the query heads of one attention call in that many threads (each head is
+the same sequence of numpy calls on the same data; where threadpoolctl is there, products run in one
+thread each, a limit that holds for the whole process while the call lasts: 16 heads whose products
+each start 16 threads take three times as long); `Model.w` converts a layer's weights to the working
+precision once and keeps the last layer converted, and `encode_units` walks layer by layer over all
+units so that this happens once per layer.
 
 Arithmetic: float64 by default (`dtype=np.float32` gives the single-precision variant).
 The quantisers are the exception: their decisions are taken on float32 values (float16
