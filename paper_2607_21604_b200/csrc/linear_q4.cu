@@ -21,7 +21,7 @@
 //
 // The first one below, `clusters`: a CTA has 8 warps of 16 features each, which share x, and a range of columns; the CTAs of a
 // cluster share the features and add their sums over distributed shared memory, in the order of the ranges.  16 rows of
-// 14336 x 4096 in 17.7 us (1.9 TB/s of weights), bound by the instructions that turn codes into operands and by its start.
+// 14336 x 4096 in 17.9 us (1.8 TB/s of weights), bound by the instructions that turn codes into operands and by its start.
 #include <cooperative_groups.h>
 #include "linear_rule.h"
 #include "tc_common.cuh"
@@ -339,9 +339,9 @@ linear_q4_kernel(const __grid_constant__ LinearQ4Params p) {
 // 8 or 16.  A team walks FT feature tiles of 16 at a time, its warps share the columns.  x is brought into operand order once
 // per CTA; a warp streams its columns through a ring of its own, a pair of groups a stage, so nothing but the sums of the
 // tiles is exchanged, once per FT tiles, through shared memory.
-// 8 rows of 14336 x 4096: 12.5 us, 2.7 TB/s of weights (a cluster per 128 features, with x converted anew for each: 13.8); of
-// 55296 x 5120 39 us, 4.1 TB/s, and one row of it 29.5 us, 5.4 TB/s of 6.56 (teams of 16 alone: 56 and 37).  One row of 4096 x
-// 4096: 4.8 us, clusters 6.2.  Bound by start, x (2.7 us for 8 rows of 4096) and end where weights are small, then by issue, some
+// 8 rows of 14336 x 4096: 12.7 us, 2.6 TB/s of weights (a cluster per 128 features, with x converted anew for each: 13.8); of
+// 55296 x 5120 40 us, 4.0 TB/s, and one row of it 30 us, 5.3 TB/s of 6.56 (teams of 16 alone: 56 and 37).  One row of 4096 x
+// 4096: 4.5 us, 4.9 with weights from memory; clusters 6.2.  Bound by start, x (2.7 us for 8 rows of 4096) and end where weights are small, then by issue, some
 // 220 instructions for a pair of groups of two tiles, and by memory for one row.
 constexpr int FW_WARPS = 16, FW_THREADS = FW_WARPS * 32, FW_STAGES = 3;
 constexpr int FW_MAX_SMEM = 224 * 1024;
@@ -648,7 +648,7 @@ int32_t launch(const LinearQ4Params& p0, cudaStream_t st) {
 // (float16, as they are) against 32 sums of x, each as two float16, make a step of the same form, two steps a stage.
 // x is brought into operand order once per call by a kernel of its own (scale of a row, permuted columns, the 128-byte
 // swizzle); weights and x arrive by bulk copies, five or six pairs of groups ahead.
-// 64 rows of 5120 x 27648 take 37.0 us, 2.2 TB/s of weights, 490 TFLOP/s; of 28672 x 4096 30.5 us; 17 rows take 0.9 of that.  Bound by
+// 64 rows of 5120 x 27648 take 37.2 us, 2.2 TB/s of weights, 490 TFLOP/s; of 28672 x 4096 30.5 us; 17 rows take 0.9 of that.  Bound by
 // what happens in a step (some 700 clocks, of which the products take 260): codes to tensor memory and sums out of it, 16 warps'
 // instructions, waits; by 10 us of start and end, of which x takes 3 and the cluster's sum 3; and by the SMs that clusters of
 // one size leave idle (28 of 148 here).
@@ -1260,7 +1260,7 @@ int32_t linear(int32_t dtype, const void* x, int64_t x_ld, const void* w, int64_
     const Path path = path_of(dtype, M, N, K);
     if (path == Path::few) {
       // As few rounds of teams as there can be: 16 warps share the columns where an SM has one tile, 8 up to two, 4 beyond
-      // (8 rows of 55296 x 5120: 39 us, with one team of 16 56).  Two tiles at a time read x half as often, where teams of
+      // (8 rows of 55296 x 5120: 40 us, with one team of 16 56).  Two tiles at a time read x half as often, where teams of
       // four have more than one round and x leaves the room (one row of 11008 x 2048: 5.6 us, with one tile 6.2).
       const int tiles = akvs_cdiv(N, 16);
       p.team = tiles <= 148 ? 16 : tiles <= 2 * 148 ? 8 : 4;

@@ -9,11 +9,11 @@
 // row.  Angles are reduced to [-1/2, 1/2] turns in double and enter the cosine as a float and its
 // remainder: a float angle of a far position has no correct digits left.  All arithmetic on values is
 // float with one rounding at the store.
-// 11648 rows of 40 + 8 heads of 128, half of each turned, in 56.6 us: 5.1 TB/s, of 6.56 that a copy reaches (57.9 with CTAs
-// of 256 threads, 60 with three heads' loads ahead of their use, 63 with fewer heads a warp, which then form their
-// angles more often); one row in 1.8 us, the time of a launch.
+// 11648 rows of 40 + 8 heads of 128, half of each turned, in 58 us: 4.9 TB/s, of 6.56 that a copy reaches (1 us more with CTAs
+// of 256 threads, 3 with three heads' loads ahead of their use, 6 with fewer heads a warp, which then form their
+// angles more often; 2 of them look for infinities of float16); one row in 1.8 us, the time of a launch.
 // Rotated parts whose halves do not start on 16 bytes (rot = 20, say) take a kernel that moves single
-// values, a lane per pair.
+// values, a lane per pair: 172 us for those rows with 20 of 128 values turned.
 #include "common.cuh"
 #include <math.h>
 
