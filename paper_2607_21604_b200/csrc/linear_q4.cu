@@ -341,8 +341,8 @@ linear_q4_kernel(const __grid_constant__ LinearQ4Params p) {
 // tiles is exchanged, once per FT tiles, through shared memory.
 // 8 rows of 14336 x 4096: 12.7 us, 2.6 TB/s of weights (a cluster per 128 features, with x converted anew for each: 13.8); of
 // 55296 x 5120 40 us, 4.0 TB/s, and one row of it 30 us, 5.3 TB/s of 6.56 (teams of 16 alone: 56 and 37).  One row of 4096 x
-// 4096: 4.5 us, 4.9 with weights from memory; clusters 6.2.  Bound by start, x (2.7 us for 8 rows of 4096) and end where weights are small, then by issue, some
-// 220 instructions for a pair of groups of two tiles, and by memory for one row.
+// 4096: 4.5 us, 4.9 with weights from memory; clusters 6.2.  Bound by start, x (2.7 us for 8 rows of 4096) and end where weights
+// are small, then by issue, some 220 instructions for a pair of groups of two tiles, and by memory for one row.
 constexpr int FW_WARPS = 16, FW_THREADS = FW_WARPS * 32, FW_STAGES = 3;
 constexpr int FW_MAX_SMEM = 224 * 1024;
 __host__ __device__ constexpr int fw_ring(int FT) { return FW_WARPS * FW_STAGES * FT * LQ_BLOCK; }
@@ -1154,8 +1154,9 @@ int32_t clusters_at_a_time(int k, int& fit) {
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   if (cudaOccupancyMaxActiveClusters(&fit, linear_q4_tc_kernel<T, NB>, &cfg) != cudaSuccess) {
-    cudaGetLastError();                               // not an error of this call: other sizes may do
+    cudaGetLastError();                               // not an error of this call: other sizes may do; asked again the next time
     fit = 0;
+    return AKVS_OK;
   }
   fit = fit < 0 ? 0 : fit;
   known[dev & 63][k].store(fit + 1, std::memory_order_relaxed);
